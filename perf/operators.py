@@ -1,0 +1,604 @@
+"""Operators of a paged MXINT KV cache, as a program that serves ragged batches uses them.
+
+Kinds of case, each through the package's public entry points:
+
+``rope``    rotary positions on query rows (mxq.rope): interleaved or half layout, the whole head or a
+            part of it, angles of far positions (the table of cosines and sines is made once, in 64 bits).
+``append``  new keys (rotated on the way) and values into the pages, the queries rotated by the same call
+            (mxq.kv_append), and the written rows read back as the values that they stand for (mxq.kv_read).
+``read``    cached rows read back by slot (mxq.kv_read), as a program does that moves a prefix elsewhere.
+``attn``    attention of the new tokens of every sequence over its pages (mxq.attn_paged): one token (decode),
+            a few (drafted tokens that are verified), a chunk of a prompt, a whole prompt; with a sliding
+            window, a prefix that every token sees, scores capped by a tanh, a bias by distance.
+``step``    append, then attention over the same pages, as a layer's step does both.
+
+The cache: a page holds P tokens; per KV head and 32-value block b of width m_b, P runs of 4 m_b bytes (the
+block's packed mantissas), the blocks' planes in order; exponents [pages][heads][P][4], a byte per block.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+D = 128
+BLOCK = 32
+DEVICE = "cuda"
+
+
+# --------------------------------------------------------------------------
+# the cases
+
+def _attn(name, S, q, kv, Hq, Hkv, widths, page, **more):
+    c = {"kind": "attn", "S": S, "q": q, "kv": kv, "Hq": Hq, "Hkv": Hkv, "widths": widths, "page": page,
+         "ragged": "even", "out": "bf16", "window": 0, "prefix": 0, "cap": 0.0, "slopes": False}
+    c.update(more)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # the queries of a single token of a 70B layer: the smallest call, latency counts
+        {"name": "rope_m1", "kind": "rope", "T": 1, "H": 64, "rot": 128, "interleaved": False,
+         "positions": 4096},
+        # a 4096-token prompt, half of the head rotated in pairs, far positions, a view of fused rows
+        {"name": "rope_m4096_part", "kind": "rope", "T": 4096, "H": 32, "rot": 64, "interleaved": True,
+         "positions": 131072},
+        # one token of each of 64 sequences into a LLaMA-2-70B layer's cache
+        {"name": "append_b64", "kind": "append", "T": 64, "Hq": 64, "Hkv": 8, "widths": "4444",
+         "page": 16, "rot": 128, "interleaved": False, "positions": 8192},
+        # a long prompt's rows into a mixed-width cache, an odd count
+        {"name": "append_m4001_4468", "kind": "append", "T": 4001, "Hq": 32, "Hkv": 8, "widths": "4468",
+         "page": 64, "rot": 128, "interleaved": True, "positions": 32768},
+        # a prefix of 10000 tokens read back
+        {"name": "read_m10000", "kind": "read", "T": 10000, "Hkv": 8, "widths": "4444", "page": 32},
+        # a single chat session's decode step, an odd length, float32 for a float32 consumer
+        _attn("decode_b1_t1777", 1, 1, 1777, 64, 8, "4444", 16, out="f32"),
+        # a serving batch, lengths from a quarter to all of 8192, mixed widths
+        _attn("decode_b32_t8192", 32, 1, 8192, 64, 8, "4468", 64, ragged="spread"),
+        # five drafted tokens of eight sequences verified; capped scores, odd lengths
+        _attn("verify_b8_q5_t6001", 8, 5, 6001, 32, 8, "4444", 32, ragged="spread", cap=30.0),
+        # a chunk of a long prompt: 2048 new tokens after 14336 cached ones, the most work
+        _attn("chunk_q2048_t16384", 1, 2048, 16384, 64, 8, "4444", 64),
+        # three prompts of unlike length prefilled together, a window of 1024 and 16 tokens that all see
+        _attn("prefill_b3_window", 3, 2731, 2731, 32, 8, "4446", 16, ragged="spread", window=1024,
+              prefix=16),
+        # whole prompts with a head of keys for each query head and a bias by distance
+        _attn("prefill_b2_bias", 2, 2048, 2048, 40, 40, "8888", 128, slopes=True),
+        # a prompt chunk and 15 decoding sequences in one step of the 3-6-8 template: rows in, then attention
+        _attn("step_mixed_368", 16, 200, 3001, 32, 8, "3368", 64, kind="step", ragged="mixed", rot=128,
+              interleaved=False, positions=4096),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["rope", "append", "read", "attn", "attn", "attn", "attn", "step"])
+    widths = rng.choice(["4444", "4444", "4468", "3333", "8888", "4446", "3368", "6666", "3448"])
+    page = rng.choice([16, 32, 64, 128, 256])
+    Hkv = rng.choice([1, 2, 4, 8, 8, 16])
+    G = rng.choice([1, 2, 4, 5, 8, 8, 16])
+    rot = rng.choice([128, 128, 64, 32, 96])
+    far = rng.choice([4096, 32768, 131072])
+    pairs = rng.random() < 0.5
+    if kind == "rope":
+        return {"kind": kind, "T": _log(rng, 1, 8192), "H": rng.choice([1, 5, 8, 32, 40, 64]), "rot": rot,
+                "interleaved": pairs, "positions": far}
+    if kind == "append":
+        return {"kind": kind, "T": _log(rng, 1, 8192), "Hq": Hkv * min(G, 8), "Hkv": Hkv, "widths": widths,
+                "page": page, "rot": rot, "interleaved": pairs, "positions": far}
+    if kind == "read":
+        return {"kind": kind, "T": _log(rng, 1, 20000), "Hkv": Hkv, "widths": widths, "page": page}
+    shape = rng.choice(["decode", "decode", "verify", "chunk", "prefill"])
+    kv = _log(rng, 40, 16384)
+    S = _log(rng, 1, 32)
+    if shape == "decode":
+        q = 1
+    elif shape == "verify":
+        q = rng.randint(2, 9)
+    elif shape == "chunk":
+        q, S = _log(rng, 10, 1000), rng.randint(1, 4)
+    else:
+        q, S = _log(rng, 40, 3000), rng.randint(1, 3)
+    q = min(q, kv)
+    if shape == "prefill":
+        kv = q
+    # at most a quarter of the largest listed case's scores
+    G = min(G, 64 // Hkv if Hkv < 64 else 1)
+    while S > 1 and S * q * kv * Hkv * G > 512 * 16384 * 64:
+        S -= 1
+    more = {"ragged": rng.choice(["even", "spread", "spread"]) if S > 1 else "even",
+            "out": rng.choice(["bf16", "bf16", "f32"])}
+    if rng.random() < 0.25:
+        more["window"] = _log(rng, 16, 2048)
+    if rng.random() < 0.25:
+        more["prefix"] = _log(rng, 1, 300)
+    if rng.random() < 0.25:
+        more["cap"] = rng.choice([20.0, 30.0, 50.0])
+    if rng.random() < 0.25:
+        more["slopes"] = True
+    if kind == "step":
+        more.update(kind="step", rot=rot, interleaved=pairs, positions=far)
+    return _attn(None, S, q, kv, Hkv * G, Hkv, widths, page, **more)
+
+
+def _lengths(c):
+    """(new tokens, tokens in the cache after them) of each sequence: whole numbers from the case alone."""
+    S, q, kv = c["S"], c["q"], c["kv"]
+    if c["ragged"] == "even":
+        return [q] * S, [kv] * S
+    part = [0.25 + 0.75 * ((1 + 0.618034 * s) % 1.0 if s else 1.0) for s in range(S)]
+    if c["ragged"] == "mixed":                 # one chunk, the others decode
+        qs = [q] + [1] * (S - 1)
+    elif q == kv:                              # prompts from their start
+        qs = [max(1, round(q * f)) for f in part]
+    else:
+        qs = [q] * S
+    return qs, [max(n, round(kv * f)) if q != kv else n for n, f in zip(qs, part)]
+
+
+# --------------------------------------------------------------------------
+# inputs, made on the device from the seed alone
+
+def _gen(seed, k):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(1000003 * (seed + 1) + k)
+    return g
+
+
+def _randn(shape, seed, k):
+    return torch.randn(shape, generator=_gen(seed, k), device=DEVICE)
+
+
+def _keys(shape, seed, k):
+    """Normal values, two channels of each head eight times as large (keys of trained models have such)."""
+    x = _randn(shape, seed, k)
+    x[..., 5] *= 8
+    x[..., 77] *= 8
+    return x
+
+
+def _table(positions, rot):
+    f = 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device=DEVICE) / rot)
+    a = torch.arange(positions, dtype=torch.float64, device=DEVICE)[:, None] * f
+    return torch.stack([a.cos(), a.sin()], dim=-1).float()
+
+
+def _widths(c):
+    return [int(w) for w in c["widths"]]
+
+
+def _planes(widths):
+    """(width, first byte of a token's share of a page's row sums) of each block."""
+    at = [0]
+    for m in widths:
+        at.append(at[-1] + 4 * m)
+    return list(zip(widths, at)), at[-1]
+
+
+def _empty_cache(pages, Hkv, page, widths):
+    row = _planes(widths)[1]
+    return (torch.zeros((pages, Hkv, page * row), dtype=torch.uint8, device=DEVICE),
+            torch.zeros((pages, Hkv, page, 4), dtype=torch.uint8, device=DEVICE))
+
+
+def _filled_cache(pages, Hkv, page, widths, seed, k, keys):
+    c = _empty_cache(pages, Hkv, page, widths)
+    make = _keys if keys else _randn
+    step = max(1, (1 << 24) // (Hkv * page * D))         # a few pages at a time
+    for i, p in enumerate(range(0, pages, step)):
+        n = min(step, pages - p)
+        x = make((n, Hkv, page, D), seed, k + 1000 * (i + 1)).to(torch.bfloat16)
+        q, e = _quantize(x, widths)
+        c[1][p:p + n] = e
+        for b, (m, at) in enumerate(_planes(widths)[0]):
+            c[0][p:p + n, :, page * at:page * (at + 4 * m)] = _pack(q[..., b, :], m).flatten(2)
+    return c
+
+
+def prepare(case, seed):
+    c, kind = dict(case), case["kind"]
+    s = {"case": c}
+    if kind == "rope":
+        T, H = c["T"], c["H"]
+        fused = _randn((T, H + 2, D), seed, 1).to(torch.bfloat16)     # rows that hold more than the queries
+        s["x"] = fused[:, :H]
+        s["pos"] = torch.randint(0, c["positions"], (T,), generator=_gen(seed, 2), device=DEVICE).int()
+        s["table"] = _table(c["positions"], c["rot"])
+        return s
+    widths, page, Hkv = _widths(c), c["page"], c["Hkv"]
+    if kind in ("append", "read"):
+        T = c["T"]
+        pages = -(-T // page) + 3
+        order = torch.randperm(pages, generator=_gen(seed, 3), device=DEVICE)
+        if kind == "append" and T <= 256:                             # a token of each sequence: anywhere
+            s["slots"] = torch.randperm(pages * page, generator=_gen(seed, 4), device=DEVICE)[:T]
+            s["pos"] = torch.randint(0, c["positions"], (T,), generator=_gen(seed, 5), device=DEVICE).int()
+        else:                                                         # a run of tokens
+            t = torch.arange(T, device=DEVICE)
+            s["slots"] = order[t // page] * page + t % page
+            s["pos"] = ((t + seed % 1000) % c.get("positions", T)).int()
+        if kind == "read":
+            s["k"] = _filled_cache(pages, Hkv, page, widths, seed, 10, True)
+            s["v"] = _filled_cache(pages, Hkv, page, widths, seed, 20, False)
+            return s
+        s["k"], s["v"] = (_empty_cache(pages, Hkv, page, widths) for _ in range(2))
+        new = T
+    else:
+        qs, kvs = _lengths(c)
+        S, T, new = c["S"], sum(qs), sum(qs)
+        most = -(-max(kvs) // page)
+        pages = sum(-(-n // page) for n in kvs) + 2
+        order = torch.randperm(pages, generator=_gen(seed, 3), device=DEVICE).int()
+        table = torch.full((S, most), -1, dtype=torch.int32, device=DEVICE)
+        at, slots, pos = 0, [], []
+        for i, n in enumerate(kvs):
+            k = -(-n // page)
+            table[i, :k] = order[at:at + k]
+            at += k
+            j = torch.arange(n - qs[i], n, device=DEVICE)
+            slots.append(table[i].long()[j // page] * page + j % page)
+            pos.append(j.int())
+        s["table"], s["slots"], s["pos"] = table, torch.cat(slots), torch.cat(pos)
+        s["cu_q"] = torch.tensor([sum(qs[:i]) for i in range(S + 1)], dtype=torch.int32, device=DEVICE)
+        s["kv_len"] = torch.tensor(kvs, dtype=torch.int32, device=DEVICE)
+        s["max_q"], s["max_kv"] = max(qs), max(kvs)
+        s["k"] = _filled_cache(pages, Hkv, page, widths, seed, 10, True)
+        s["v"] = _filled_cache(pages, Hkv, page, widths, seed, 20, False)
+        s["scale"] = 1.0 / math.sqrt(D)
+        s["prefix"] = (torch.full((S,), c["prefix"], dtype=torch.int32, device=DEVICE)
+                       if c["prefix"] else None)
+        s["slopes"] = None
+        if c["slopes"]:
+            h = torch.arange(1, c["Hq"] + 1, device=DEVICE)
+            s["slopes"] = 2.0 ** (-8.0 * h / c["Hq"])
+        if kind == "attn":
+            s["q"] = _randn((T, c["Hq"], D), seed, 30).to(torch.bfloat16)
+            return s
+        s["pos"] = (s["pos"] % c["positions"]).int()
+    rows = _randn((new, c["Hq"] + 2 * Hkv, D), seed, 40)              # a fused projection's rows
+    rows[:, c["Hq"]:c["Hq"] + Hkv] = _keys((new, Hkv, D), seed, 41)
+    rows = rows.to(torch.bfloat16)
+    s["q"], s["k_new"], s["v_new"] = rows.split([c["Hq"], Hkv, Hkv], dim=1)
+    s["rope"] = _table(c["positions"], c["rot"])
+    return s
+
+
+# --------------------------------------------------------------------------
+# the framework's calls
+
+def _own_cache(s):
+    from paper_2607_17733_amd import mxq
+    if "cache" not in s:                                  # the handle that a program keeps
+        c = s["case"]
+        pages, Hkv = s["k"][0].shape[:2]
+        s["cache"] = mxq.PagedCache(mxq.Format(D, _widths(c)), Hkv, pages, c["page"], k=s["k"], v=s["v"])
+    return mxq, s["cache"]
+
+
+def _own_attn(s, q):
+    mxq, cache = _own_cache(s)
+    c = s["case"]
+    if "work" not in s:
+        n = mxq.attn_paged_work_bytes(cache, c["S"], q.shape[0], c["Hq"], s["max_q"], s["max_kv"])
+        s["work"] = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+    return mxq.attn_paged(q, cache, s["cu_q"], s["kv_len"], s["table"], s["max_q"], s["max_kv"], s["scale"],
+                          softcap=c["cap"], window=c["window"], prefix=s["prefix"], slopes=s["slopes"],
+                          dtype=torch.float32 if c["out"] == "f32" else torch.bfloat16, work=s["work"])
+
+
+def _own_run(s):
+    c, kind = s["case"], s["case"]["kind"]
+    if kind == "rope":
+        from paper_2607_17733_amd import mxq
+        return mxq.rope(s["x"], s["pos"], s["table"], interleaved=c["interleaved"])
+    if kind == "attn":
+        return _own_attn(s, s["q"])
+    mxq, cache = _own_cache(s)
+    if kind == "read":
+        return mxq.kv_read(cache, s["slots"])
+    q = mxq.kv_append(cache, s["k_new"], s["v_new"], s["slots"], pos=s["pos"], rope=s["rope"],
+                      interleaved=c["interleaved"], q=s["q"])
+    if kind == "append":
+        return (q,) + tuple(mxq.kv_read(cache, s["slots"]))
+    return q, _own_attn(s, q)
+
+
+# --------------------------------------------------------------------------
+# the plain forms
+
+def _plain_rope(x, pos, table, interleaved):
+    R = 2 * table.shape[1]
+    cs = table[pos.long()]
+    c, sn = cs[:, None, :, 0], cs[:, None, :, 1]
+    y = x.float()
+    if interleaved:
+        x1, x2 = y[..., 0:R:2], y[..., 1:R:2]
+        r = torch.stack([x1 * c - x2 * sn, x2 * c + x1 * sn], dim=-1).flatten(-2)
+    else:
+        x1, x2 = y[..., :R // 2], y[..., R // 2:R]
+        r = torch.cat([x1 * c - x2 * sn, x2 * c + x1 * sn], dim=-1)
+    return torch.cat([r, y[..., R:]], dim=-1).to(x.dtype)
+
+
+def _pow2(e):
+    """2^e in 32 bits for e in [-149, 254], as two factors that are both in range."""
+    h = e // 2
+    return torch.exp2(h.float()), torch.exp2((e - h).float())
+
+
+def _quantize(x, widths):
+    """bf16 [..., 128] -> (mantissas int32 [..., 4, 32], exponents uint8 [..., 4])."""
+    y = x.unflatten(-1, (len(widths), BLOCK))
+    E = (y.contiguous().view(torch.int16).int() & 0x7FFF).amax(-1) >> 7
+    m = torch.tensor(widths, device=x.device)
+    a, b = _pow2(127 + m - 2 - E)
+    lim = (2 ** (m - 1) - 1).float()[:, None]
+    q = torch.minimum(torch.maximum(torch.round(y.float() * a[..., None] * b[..., None]), -lim), lim)
+    return torch.where((E == 255)[..., None], 0, q.nan_to_num(0.0).int()), E.to(torch.uint8)
+
+
+def _pack(q, m):
+    """Mantissas [..., 32] of one block of width m -> its 4 m bytes."""
+    if m == 8:
+        return (q & 255).to(torch.uint8)
+    if m == 3:
+        f = (q & 7).unflatten(-1, (4, 8)) << (3 * torch.arange(8, device=q.device))
+        w = f.sum(-1)
+        return torch.stack([w & 255, (w >> 8) & 255, w >> 16], dim=-1).flatten(-2).to(torch.uint8)
+    low = (q[..., 0::2] & 15) | ((q[..., 1::2] & 15) << 4)
+    if m == 4:
+        return low.to(torch.uint8)
+    t = ((q >> 4) & 3).unflatten(-1, (2, 2, 4, 2))        # half of the block, half of that, byte, parity
+    top = t[..., 0, :, 0] << 6 | t[..., 0, :, 1] << 4 | t[..., 1, :, 0] << 2 | t[..., 1, :, 1]
+    return torch.cat([low, top.flatten(-2)], dim=-1).to(torch.uint8)
+
+
+def _unpack(p, m):
+    """The 4 m bytes [..., 4 m] of blocks of width m -> mantissas [..., 32]."""
+    if m == 8:
+        return p.view(torch.int8).int()
+    p = p.int()
+    if m == 3:
+        w = p.unflatten(-1, (4, 3))
+        w = w[..., 0] | w[..., 1] << 8 | w[..., 2] << 16
+        f = (w[..., None] >> (3 * torch.arange(8, device=p.device))) & 7
+        return ((f ^ 4) - 4).flatten(-2)
+    low = torch.stack([p[..., :16] & 15, p[..., :16] >> 4], dim=-1).flatten(-2)
+    if m == 4:
+        return (low ^ 8) - 8
+    t = p[..., 16:].unflatten(-1, (2, 4))
+    top = torch.stack([torch.stack([t >> 6, (t >> 4) & 3], -1), torch.stack([(t >> 2) & 3, t & 3], -1)], -3)
+    return ((low | top.flatten(-4) << 4) ^ 32) - 32
+
+
+def _views(cache, page, widths):
+    """Each block's plane of the pages, [pages, heads, page, 4 m]."""
+    return [(m, cache[0][:, :, page * at:page * (at + 4 * m)].unflatten(-1, (page, 4 * m)))
+            for m, at in _planes(widths)[0]]
+
+
+def _plain_append(cache, x, slots, page, widths):
+    q, e = _quantize(x, widths)
+    p, t = slots // page, slots % page
+    cache[1][p, :, t] = e
+    for b, (m, plane) in enumerate(_views(cache, page, widths)):
+        plane[p, :, t] = _pack(q[..., b, :], m)
+
+
+def _values(q, e, widths):
+    a, b = _pow2(e.int() - 127 - torch.tensor([m - 2 for m in widths], device=e.device))
+    return (q.float() * a[..., None] * b[..., None]).flatten(-2)
+
+
+def _plain_read(cache, slots, page, widths):
+    p, t = slots // page, slots % page
+    q = torch.stack([_unpack(plane[p, :, t], m) for m, plane in _views(cache, page, widths)], dim=-2)
+    return _values(q, cache[1][p, :, t], widths).to(torch.bfloat16)
+
+
+def _plain_pages(cache, table, page, widths):
+    """The sequences' cached values, [S, heads, tokens, 128]."""
+    p = table.long().clamp(min=0)
+    q = torch.stack([_unpack(plane[p], m) for m, plane in _views(cache, page, widths)], dim=-2)
+    return _values(q, cache[1][p], widths).transpose(1, 2).flatten(2, 3)
+
+
+def _plain_attn(s, q):
+    c, widths = s["case"], _widths(s["case"])
+    S, Hkv, G, nq = c["S"], c["Hkv"], c["Hq"] // c["Hkv"], s["max_q"]
+    k = _plain_pages(s["k"], s["table"], c["page"], widths)
+    v = _plain_pages(s["v"], s["table"], c["page"], widths)
+    n = (s["cu_q"][1:] - s["cu_q"][:-1]).long()
+    i = torch.arange(nq, device=q.device)
+    here = i < n[:, None]                                               # [S, nq]
+    row = torch.where(here, s["cu_q"][:-1, None].long() + i, 0)
+    x = q.float()[row].unflatten(2, (Hkv, G)).permute(0, 2, 3, 1, 4)     # [S, Hkv, G, nq, D]
+    w = torch.matmul(x.flatten(2, 3), k.transpose(-1, -2)).unflatten(2, (G, nq)) * s["scale"]
+    if c["cap"]:
+        w = c["cap"] * torch.tanh(w / c["cap"])
+    pos = (s["kv_len"].long() - n)[:, None] + i                          # [S, nq]
+    j = torch.arange(k.shape[2], device=q.device)
+    far = pos[..., None] - j                                            # [S, nq, tokens]
+    if s["slopes"] is not None:
+        w = w - s["slopes"].view(1, Hkv, G, 1, 1) * far.abs().float()[:, None, None]
+    see = far >= 0
+    if c["window"]:
+        see = see & (far < c["window"])
+    if s["prefix"] is not None:
+        see = see | (j < s["prefix"][:, None, None])
+    see = (see & (j < s["kv_len"][:, None, None]))[:, None, None]
+    w = torch.where(see, w, -math.inf)
+    top = w.amax(-1, keepdim=True)
+    p = torch.exp(w - torch.where(top == -math.inf, 0.0, top))
+    o = torch.matmul(p.flatten(2, 3), v).unflatten(2, (G, nq))
+    o = o / p.sum(-1, keepdim=True).clamp(min=1e-30)
+    o = o.permute(0, 3, 1, 2, 4).flatten(2, 3)[here]
+    return o if c["out"] == "f32" else o.to(torch.bfloat16)
+
+
+def run(state):
+    if own:
+        return _own_run(state)
+    s, c = state, state["case"]
+    if c["kind"] == "rope":
+        return _plain_rope(s["x"], s["pos"], s["table"], c["interleaved"])
+    if c["kind"] == "attn":
+        return _plain_attn(s, s["q"])
+    widths, page = _widths(c), c["page"]
+    if c["kind"] == "read":
+        return tuple(_plain_read(s[x], s["slots"], page, widths) for x in "kv")
+    q = _plain_rope(s["q"], s["pos"], s["rope"], c["interleaved"])
+    _plain_append(s["k"], _plain_rope(s["k_new"], s["pos"], s["rope"], c["interleaved"]), s["slots"], page,
+                  widths)
+    _plain_append(s["v"], s["v_new"], s["slots"], page, widths)
+    if c["kind"] == "append":
+        return (q,) + tuple(_plain_read(s[x], s["slots"], page, widths) for x in "kv")
+    return q, _plain_attn(s, q)
+
+
+# --------------------------------------------------------------------------
+# what a pass cannot do without
+
+def work(case):
+    c, kind = case, case["kind"]
+    if kind == "rope":
+        return {"bytes": c["T"] * (c["H"] * D * 4 + 4 + 4 * c["rot"]), "flops": 3 * c["T"] * c["H"] * c["rot"]}
+    row = sum(4 * m for m in _widths(c)) + 4                # a cached row's bytes
+    if kind == "read":
+        return {"bytes": c["T"] * (8 + 2 * c["Hkv"] * (row + 2 * D)), "flops": c["T"] * c["Hkv"] * 2 * D}
+    total = {"bytes": 0, "flops": 0}
+    if kind in ("append", "step"):
+        T = c["T"] if kind == "append" else sum(_lengths(c)[0])
+        heads = c["Hq"] + c["Hkv"]
+        total["bytes"] += T * (heads * 2 * D + c["Hkv"] * (2 * D + 2 * row) + 12 + 4 * c["rot"])
+        total["bytes"] += T * c["Hq"] * 2 * D
+        total["flops"] += 3 * T * heads * c["rot"] + 4 * T * c["Hkv"] * D
+        if kind == "append":                                # and the rows read back
+            total["bytes"] += T * 2 * c["Hkv"] * (row + 2 * D)
+            return total
+    for n, kv in zip(*_lengths(c)):
+        w, pre = c["window"] or kv, min(c["prefix"], kv)
+        pairs = used = 0
+        lo = max(0, kv - n - w + 1)                         # the first key of the first token's window
+        used = kv - max(lo, pre) + pre if pre < kv else kv
+        for p in range(kv - n, kv):
+            first = max(0, p - w + 1)
+            pairs += p + 1 - max(first, min(pre, p + 1)) + pre
+        total["bytes"] += used * c["Hkv"] * 2 * row + n * c["Hq"] * D * (2 + (4 if c["out"] == "f32" else 2))
+        total["flops"] += 4 * D * pairs * c["Hq"]
+    return total
+
+
+# --------------------------------------------------------------------------
+# the operators' values in 64 bits, from their definitions
+
+def _exact_rope(x, pos, rot, interleaved):
+    """Angles from the positions themselves; the table holds their cosines and sines in 32 bits."""
+    i = torch.arange(rot // 2, device=x.device, dtype=torch.float64)
+    turn = torch.polar(torch.ones((), dtype=torch.float64, device=x.device),
+                       pos.double()[:, None] * torch.pow(torch.full_like(i, 10000.0), -2 * i / rot))
+    y = x.double().clone()
+    a = 2 * i.long() if interleaved else i.long()
+    b = a + 1 if interleaved else a + rot // 2
+    z = torch.complex(y[..., a].contiguous(), y[..., b].contiguous()) * turn[:, None]
+    y[..., a], y[..., b] = z.real.contiguous(), z.imag.contiguous()
+    return y
+
+
+def _exact_quantized(x, widths):
+    """bf16 rows -> the values that their quantization stands for, in 64 bits."""
+    out = torch.empty(x.shape, dtype=torch.float64, device=x.device)
+    for b, m in enumerate(widths):
+        y = x[..., BLOCK * b:BLOCK * (b + 1)].double()
+        _, e = torch.frexp(y.abs().amax(-1, keepdim=True))
+        unit = torch.exp2((e - 1 - (m - 2)).double())       # the weight of a mantissa's last bit
+        most = 2 ** (m - 1) - 1
+        out[..., BLOCK * b:BLOCK * (b + 1)] = (y / unit).round().clamp(-most, most) * unit
+    return out
+
+
+def _exact_rows(cache, where, token, page, widths):
+    """The rows of one head [n, bytes] at pages `where`, places `token`, decoded bit by bit."""
+    n = where.shape[0]
+    out = torch.empty((n, D), dtype=torch.float64, device=where.device)
+    at = 0
+    for b, m in enumerate(widths):
+        i = page * at + token[:, None] * (4 * m) + torch.arange(4 * m, device=where.device)
+        p = cache[0][where[:, None], i].long()
+        el = torch.arange(BLOCK, device=where.device)
+        if m == 8:
+            v = p
+        elif m == 3:
+            bit = 3 * el
+            two = p[:, bit // 8] + 256 * p[:, (bit // 8 + 1).clamp(max=11)]
+            v = (two // 2 ** (bit % 8)) % 8
+        else:
+            v = (p[:, el // 2] // 16 ** (el % 2)) % 16
+            if m == 6:
+                u = el % 16
+                tops = p[:, 16 + 4 * (el // 16) + (u % 8) // 2]
+                v = v + 16 * ((tops // 2 ** (6 - 4 * (u // 8) - 2 * (u % 2))) % 4)
+        v = torch.where(v >= 2 ** (m - 1), v - 2 ** m, v).double()
+        unit = torch.exp2(cache[1][where, token, b].double() - 127 - (m - 2))
+        out[:, BLOCK * b:BLOCK * (b + 1)] = v * unit[:, None]
+        at += 4 * m
+    return out
+
+
+def _exact_attn(s, q, new=None):
+    """`new`: keys and values of the new tokens, where the cache does not hold them yet."""
+    c, widths, page = s["case"], _widths(s["case"]), s["case"]["page"]
+    out = torch.empty(q.shape, dtype=torch.float64, device=q.device)
+    qs, kvs = _lengths(c)
+    at, G = 0, c["Hq"] // c["Hkv"]
+    for r, (n, kv) in enumerate(zip(qs, kvs)):
+        t = torch.arange(kv, device=q.device)
+        where, token = s["table"][r].long()[t // page], t % page
+        p = torch.arange(kv - n, kv, device=q.device)[:, None]
+        see = (t <= p) & ((p - t < c["window"]) if c["window"] else True)
+        if c["prefix"]:
+            see = see | (t < c["prefix"])
+        for h in range(c["Hkv"]):
+            k, v = (_exact_rows((s[x][0][:, h], s[x][1][:, h]), where, token, page, widths) for x in "kv")
+            if new is not None:
+                k[kv - n:], v[kv - n:] = new[0][at:at + n, h], new[1][at:at + n, h]
+            for g in range(h * G, (h + 1) * G):
+                w = (q[at:at + n, g].double() @ k.T) * s["scale"]
+                if c["cap"]:
+                    w = c["cap"] * torch.tanh(w / c["cap"])
+                if c["slopes"]:
+                    w = w - s["slopes"][g].double() * (p - t).abs()
+                w = torch.where(see, w, -math.inf)
+                out[at:at + n, g] = torch.softmax(w, dim=-1) @ v
+        at += n
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    c, kind = s["case"], s["case"]["kind"]
+    if kind == "rope":
+        return _exact_rope(s["x"], s["pos"], c["rot"], c["interleaved"])
+    if kind == "attn":
+        return _exact_attn(s, s["q"])
+    widths, page = _widths(c), c["page"]
+    if kind == "read":
+        p, t = s["slots"] // page, s["slots"] % page
+        return tuple(torch.stack([_exact_rows((s[x][0][:, h], s[x][1][:, h]), p, t, page, widths)
+                                  for h in range(c["Hkv"])], dim=1) for x in "kv")
+    q = _exact_rope(s["q"], s["pos"], c["rot"], c["interleaved"])
+    # the rotated keys are bf16 values before they are quantized: that rounding is part of the definition
+    k = _exact_quantized(_exact_rope(s["k_new"], s["pos"], c["rot"], c["interleaved"]).to(torch.bfloat16),
+                         widths)
+    v = _exact_quantized(s["v_new"], widths)
+    if kind == "append":
+        return q, k, v
+    return q, _exact_attn(s, q.to(torch.bfloat16), (k, v))

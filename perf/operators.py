@@ -125,7 +125,8 @@ def draw(rng):
     if rng.random() < 0.25:
         more["slopes"] = True
     if kind == "step":
-        more.update(kind="step", rot=rot, interleaved=pairs, positions=far)
+        # (the queries are rounded to bf16 after their rotation: float32 of what follows means nothing)
+        more.update(kind="step", rot=rot, interleaved=pairs, positions=far, out="bf16")
     return _attn(None, S, q, kv, Hkv * G, Hkv, widths, page, **more)
 
 

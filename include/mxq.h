@@ -493,6 +493,166 @@ mxq_status mxq_attn_decode_static(const mxq_fmt *fmt, const uint16_t *q, int64_t
                                   const uint8_t *k_exp, const uint8_t *v_mant,
                                   const uint8_t *v_exp, float *o, void *stream);
 
+/*
+ * Rotary positions.  A table holds, for each position p < positions and each
+ * of the rot / 2 frequencies f_i, the float32 pair (cos, sin) of p * f_i (the
+ * angle and its cosine and sine in float64, times `mscale`, rounded once):
+ * table[(p * (rot / 2) + i) * 2 + {0, 1}].  A head's values in the pair
+ * (x1, x2) of frequency i become
+ *   y1 = bf16(x1 * c - x2 * s),  y2 = bf16(x2 * c + x1 * s)
+ * with float32 products, difference and sum, each rounded on its own (no fused
+ * multiply-add), so that every machine gets the same bits.  The pair is
+ * (x[i], x[i + rot / 2]) in MXQ_ROPE_HALVES and (x[2 i], x[2 i + 1]) in
+ * MXQ_ROPE_PAIRS; values at rot and above are copied.  A position outside
+ * [0, positions) has no angle: its rotated values are NaN.
+ *   table      DEVICE float [positions][rot / 2][2], 16-byte aligned.
+ *   positions  1 .. 2^31 - 1.
+ *   rot        even, 2 .. 512, at most the head's size.
+ *   layout     mxq_rope_layout.
+ */
+typedef enum { MXQ_ROPE_HALVES = 0, MXQ_ROPE_PAIRS = 1 } mxq_rope_layout;
+typedef struct {
+  const float *table;
+  int64_t positions;
+  int32_t rot;
+  int32_t layout;
+} mxq_rotary;
+
+/*
+ * mxq_rope_table: writes such a table (once, at model load) from the
+ * frequencies inv_freq HOST double [rot / 2] (read during the call), finite.
+ * mxq_rope: rotates bf16 rows x[t][h][0..D-1] at x + t * x_ts + h * x_hs
+ * (elements) into y, likewise strided, with the position pos[t] (DEVICE int32
+ * [T]).  y may be x itself with the same strides, else the two must not
+ * overlap.  1 <= D <= 4096, D even; x and y 4-byte aligned, strides even.
+ * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (negative counts, rot odd or out of
+ * range, D < rot, positions out of range, non-finite frequencies or mscale),
+ * MXQ_ERR_ALIGN (also for odd strides), MXQ_ERR_UNSUPPORTED (layout),
+ * MXQ_ERR_DEVICE.  T == 0 or H == 0 enqueues nothing.
+ */
+mxq_status mxq_rope_table(const double *inv_freq, int32_t rot, int64_t positions,
+                          double mscale, float *table, void *stream);
+mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_t H,
+                    int64_t D, int64_t x_ts, int64_t x_hs, const int32_t *pos,
+                    uint16_t *y, int64_t y_ts, int64_t y_hs, void *stream);
+
+/*
+ * A paged MXINT KV cache of one layer (Appendix A.2: K and V are quantized to
+ * MXINT, 32-element blocks along the head dimension of 128).  A page holds
+ * page_tokens tokens of every KV head; token `slot` lies in page
+ * slot / page_tokens, at place slot % page_tokens.  For page g and head h
+ *   mant: at (g * Hkv + h) * page_tokens * R, R = sum_b 4 m_b (the widths of
+ *         the format's four blocks): for each block b in order a plane of
+ *         page_tokens runs of 4 m_b bytes, run i being block b of the page's
+ *         token i, packed as in the packed rows (layout (C) above);
+ *   exp:  at ((g * Hkv + h) * page_tokens + i) * 4, byte b = the E of block b.
+ * So a wave reads one block of consecutive tokens as one contiguous run.
+ *   pages        >= 1, pages * page_tokens < 2^31.
+ *   Hkv          1 .. 65535.
+ *   page_tokens  a power of two, 16 .. 1024.
+ *   k_mant, v_mant  DEVICE, 16-byte aligned, pages * mxq_kv_page_bytes(...).
+ *   k_exp, v_exp    DEVICE, 16-byte aligned, pages * mxq_kv_page_exp_bytes(...).
+ * fmt: K = 128, perm NULL; round and clamp matter to mxq_kv_append only.
+ */
+typedef struct {
+  int64_t pages;
+  int64_t Hkv;
+  int32_t page_tokens;
+  int32_t reserved;        /* must be 0 */
+  uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+} mxq_paged_kv;
+
+/* Bytes of one page of K (V needs as many); negative mxq_status on bad arguments. */
+int64_t mxq_kv_page_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_tokens);
+int64_t mxq_kv_page_exp_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_tokens);
+
+/*
+ * mxq_kv_append: new tokens into the cache, the rotation applied on the way.
+ * Token t's keys k[t][h][0..127] (at k + t * k_ts + h * k_hs) are rotated as
+ * mxq_rope does (rope NULL: not at all) and quantized as mxq_quantize_rows
+ * does, its values v[t][h] quantized as they are, into slot slots[t].  With q
+ * (or NULL) the queries q[t][0..Hq-1] are rotated in the same launch into q_out
+ * [T][Hq][128] (q_out may be q itself if q is contiguous).  A token whose slot
+ * lies outside [0, pages * page_tokens) is padding: its keys and values are
+ * not stored.  The slots of a call are distinct, or the rows of a slot that is
+ * named twice are undefined.
+ *   slots  DEVICE int64 [T]; pos DEVICE int32 [T] (may be NULL without rope).
+ *   k, v, q, q_out  bf16, 16-byte aligned, strides multiples of 8 elements.
+ *   rope   rot a multiple of 16, at most 128.
+ * mxq_kv_read: the rows of the given slots as the bf16 values that they stand
+ * for, q * 2^(E - 127 - (m - 2)), which is exact, into k and v DEVICE bf16
+ * [n][Hkv][128], 16-byte aligned (either may be NULL); zeros for a slot
+ * outside the cache.
+ * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, counts, page_tokens, rot),
+ * MXQ_ERR_UNSUPPORTED (a permutation, layout), MXQ_ERR_NULL, MXQ_ERR_ALIGN (also
+ * for strides), MXQ_ERR_DEVICE.  T == 0 (n == 0) enqueues nothing.
+ */
+mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const uint16_t *k,
+                         int64_t k_ts, int64_t k_hs, const uint16_t *v, int64_t v_ts,
+                         int64_t v_hs, int64_t T, const int64_t *slots, const int32_t *pos,
+                         const mxq_rotary *rope, const uint16_t *q, int64_t Hq, int64_t q_ts,
+                         int64_t q_hs, uint16_t *q_out, void *stream);
+mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int64_t *slots,
+                       int64_t n, uint16_t *k, uint16_t *v, void *stream);
+
+/*
+ * Attention of new tokens over the paged cache, which holds them already
+ * (mxq_kv_append): chunks of prompts, whole prompts, drafted tokens and single
+ * tokens, mixed in one ragged batch.  Sequence s has kv_len[s] tokens in the
+ * pages table[s][0], table[s][1], ..., and its n = cu_q[s+1] - cu_q[s] query
+ * rows cu_q[s] .. are its last n tokens: row i stands at position
+ * p = kv_len[s] - n + i.  With the dequantized K and V, per query head h over
+ * KV head h / (Hq / Hkv),
+ *   x_j = scale * sum_d q[h][d] K[j][d];
+ *   x_j = softcap * tanh(x_j / softcap)           (softcap > 0);
+ *   x_j = x_j - slopes[h] * |p - j|               (slopes not NULL);
+ *   o[h] = sum_j softmax(x)_j V[j] over the tokens j < kv_len[s] that the row
+ *   sees: j <= p, and p - j < window (window > 0), or j < prefix[s] (prefix not
+ *   NULL: a prompt part, or attention sinks, that every row sees).
+ * A row that sees nothing gives zeros.  Rows of q outside every sequence are
+ * not read, and their rows of o stay as they are.
+ *   batch   S sequences; T rows of q and o; cu_q DEVICE int32 [S + 1], from 0
+ *           up, not decreasing, at most T; kv_len DEVICE int32 [S]; table DEVICE
+ *           int32, row s at table + s * ld_table, table_pages entries.  max_q >=
+ *           every n and max_kv >= every kv_len (HOST: they size the launch; rows
+ *           past max_q are not computed, longer lengths are cut).  A length also
+ *           ends after table_pages pages.  A table entry outside [0, pages) is
+ *           never followed: its tokens read as zero rows.
+ *   q       DEVICE bf16, row t, head h at q + t * q_ts + h * q_hs, 16-byte
+ *           aligned, strides multiples of 8.
+ *   o       DEVICE [T][Hq][128], bf16 or, with o_f32, float32, 16-byte aligned.
+ *   work    DEVICE, 16-byte aligned, work_bytes >= mxq_attn_paged_work_bytes:
+ *           partial results; needs no initialisation.  Calls that may overlap
+ *           in time must not share it.
+ * Every product is exact (bf16 query, bf16 K and V values), sums and softmax
+ * statistics are float32.  For a float32 output the probabilities enter the
+ * value product with all their 24 bits, for a bf16 one rounded to bf16; a
+ * probability is at most e^4 before the division by their sum, and a sum of
+ * probabilities times values past float32's range is infinite.  Calls repeat
+ * bit for bit.
+ * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, bad counts, Hq not a multiple
+ * of Hkv, Hq / Hkv > 64, non-finite scale or softcap, softcap < 0, window < 0,
+ * a short work buffer); MXQ_ERR_UNSUPPORTED (a permutation); MXQ_ERR_NULL;
+ * MXQ_ERR_ALIGN; MXQ_ERR_DEVICE.  S == 0, T == 0 or max_q == 0 enqueues nothing.
+ */
+typedef struct {
+  int64_t S, T, max_q, max_kv;
+  const int32_t *cu_q, *kv_len, *table;
+  int64_t ld_table, table_pages;
+} mxq_paged_batch;
+typedef struct {
+  float scale, softcap;
+  int64_t window;
+  const int32_t *prefix;   /* DEVICE int32 [S] or NULL */
+  const float *slopes;     /* DEVICE float [Hq] or NULL */
+} mxq_attn_opts;
+int64_t mxq_attn_paged_work_bytes(const mxq_fmt *fmt, const mxq_paged_kv *cache, int64_t S,
+                                  int64_t T, int64_t Hq, int64_t max_q, int64_t max_kv);
+mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
+                          const mxq_paged_batch *batch, const mxq_attn_opts *opts,
+                          const uint16_t *q, int64_t Hq, int64_t q_ts, int64_t q_hs, void *o,
+                          int o_f32, float *work, int64_t work_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,7 +5,8 @@ The compute path is the HIP library ``libmxq.so`` behind the C ABI in
 ``paper_2607_17733_amd.workloads`` draws the seeded synthetic inputs.
 """
 _BINDING = ("Format", "MxqError", "quantize_act", "quantize_rows", "pack_weights", "gemm",
-            "gemm_partials", "unpack_act", "unpack_weights", "lib")
+            "gemm_partials", "unpack_act", "unpack_weights", "lib", "rope_inv_freq", "rope_table",
+            "rope", "PagedCache", "kv_append", "kv_read", "attn_paged", "attn_paged_work_bytes")
 
 
 def __getattr__(name):

@@ -13,13 +13,11 @@
 
 namespace {
 
-using mxq::Segs;
-
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+}  // namespace
 
-constexpr int64_t kWeightTailPad = 64;
+namespace mxq {
 
 // Validate a format and derive its width segments (MXSens Section 4.1: one
 // width per block; the permutation groups same-width columns, ordered
@@ -54,6 +52,17 @@ mxq_status check_fmt(const mxq_fmt *f, Segs *s) {
   s->n3 = n3;
   return MXQ_OK;
 }
+
+}  // namespace mxq
+
+namespace {
+
+using mxq::check_fmt;
+using mxq::Segs;
+
+int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+constexpr int64_t kWeightTailPad = 64;
 
 int64_t row_used(const Segs &s) { return mxq::packed_row_used(s); }
 // packed section and per-row exponent section

@@ -131,4 +131,75 @@ hipError_t attn_static_scratch(float **ptr);
 int64_t attn_tokens_per_split(int64_t B, int64_t Hkv, int64_t T);
 hipError_t launch_attn_decode(const AttnArgs &args, hipStream_t s);
 
+// Validates a format and derives its width segments (api.cpp).
+struct Segs;
+mxq_status check_fmt(const mxq_fmt *f, Segs *s);
+
+// Rotary positions (rope.hip).
+constexpr int kRopeMaxRot = 512;
+struct RopeArgs {
+  const float *table;      // [positions][rot / 2][2]
+  int64_t positions;
+  int rot, pairs;
+};
+struct RopeRowsArgs {
+  RopeArgs rope;
+  const uint16_t *x;
+  uint16_t *y;
+  const int32_t *pos;
+  int64_t T, H, D, x_ts, x_hs, y_ts, y_hs;
+};
+hipError_t launch_rope_table(const double *inv_freq, int rot, int64_t positions, double mscale,
+                             float *table, hipStream_t s);
+hipError_t launch_rope(const RopeRowsArgs &args, hipStream_t s);
+
+// The paged KV cache (kv_paged.hip): head dimension 128, four blocks a row.
+struct PageGeo {
+  int m[4];                // widths
+  int off[4];              // a block's first byte in a packed row; its plane's is page * off
+  int row;                 // bytes of a packed row
+  int lg_page;             // log2 of the tokens per page
+  int64_t pages, Hkv;
+};
+struct KvAppendArgs {
+  PageGeo geo;
+  RopeArgs rope;           // table null: no rotation
+  const uint16_t *k, *v, *q;
+  uint16_t *q_out;
+  int64_t k_ts, k_hs, v_ts, v_hs, q_ts, q_hs;
+  int64_t T, Hq;           // Hq 0: no queries
+  const int64_t *slots;
+  const int32_t *pos;
+  uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+  int ties_away, full_clamp;
+};
+struct KvReadArgs {
+  PageGeo geo;
+  const uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+  const int64_t *slots;
+  int64_t n;
+  uint16_t *k, *v;         // either null
+};
+hipError_t launch_kv_append(const KvAppendArgs &args, hipStream_t s);
+hipError_t launch_kv_read(const KvReadArgs &args, hipStream_t s);
+
+// Attention over the paged cache (attn_paged.hip).
+struct AttnPagedArgs {
+  PageGeo geo;
+  const uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
+  const uint16_t *q;
+  int64_t q_ts, q_hs;
+  void *o;
+  int o_f32;
+  float *work;
+  const int32_t *cu_q, *kv_len, *table, *prefix;
+  const float *slopes;
+  int64_t ld_table, table_pages;
+  int64_t S, T, Hq, max_q, max_kv, window;
+  int G;
+  float scale, softcap;
+};
+int64_t attn_paged_work(const AttnPagedArgs &args);
+hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s);
+
 }  // namespace mxq

@@ -29,6 +29,31 @@ class _Fmt(ctypes.Structure):
                 ("perm", ctypes.c_void_p)]
 
 
+class _Rotary(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int64),
+                ("rot", ctypes.c_int32), ("layout", ctypes.c_int32)]
+
+
+class _PagedKv(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("Hkv", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k_mant", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_mant", ctypes.c_void_p), ("v_exp", ctypes.c_void_p)]
+
+
+class _PagedBatch(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int64), ("T", ctypes.c_int64), ("max_q", ctypes.c_int64),
+                ("max_kv", ctypes.c_int64), ("cu_q", ctypes.c_void_p),
+                ("kv_len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("table_pages", ctypes.c_int64)]
+
+
+class _AttnOpts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("window", ctypes.c_int64), ("prefix", ctypes.c_void_p),
+                ("slopes", ctypes.c_void_p)]
+
+
 _lib = None
 
 # name -> (restype, argtypes)
@@ -68,6 +93,16 @@ _SIGS = {
                                        _P, _P, _P, _P, _P, _P, _I64, _P]),
     "mxq_attn_decode_static": (ctypes.c_int, [_P, _P, _I64, _I64, _I64, _I64, ctypes.c_float,
                                               _P, _P, _P, _P, _P, _P]),
+    "mxq_rope_table": (ctypes.c_int, [_P, ctypes.c_int32, _I64, ctypes.c_double, _P, _P]),
+    "mxq_rope": (ctypes.c_int, [_P, _P, _I64, _I64, _I64, _I64, _I64, _P, _P, _I64, _I64, _P]),
+    "mxq_kv_page_bytes": (_I64, [_P, _I64, ctypes.c_int32]),
+    "mxq_kv_page_exp_bytes": (_I64, [_P, _I64, ctypes.c_int32]),
+    "mxq_kv_append": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P, _P,
+                                     _P, _I64, _I64, _I64, _P, _P]),
+    "mxq_kv_read": (ctypes.c_int, [_P, _P, _P, _I64, _P, _P, _P]),
+    "mxq_attn_paged_work_bytes": (_I64, [_P, _P, _I64, _I64, _I64, _I64, _I64]),
+    "mxq_attn_paged": (ctypes.c_int, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _P, ctypes.c_int,
+                                      _P, _I64, _P]),
 }
 
 
@@ -586,4 +621,290 @@ def attn_decode_static(q, k_cache, v_cache, fmt: Format, B: int, Hq: int, Hkv: i
                                         _ptr(k_cache[0]), _ptr(k_cache[1]), _ptr(v_cache[0]),
                                         _ptr(v_cache[1]), _ptr(out), _stream()),
            "mxq_attn_decode_static")
+    return out
+
+
+# --------------------------------------------------------------------------
+# Rotary positions, the paged KV cache, and attention over it
+
+def _current(dev, what: str):
+    """The calls run on the current device's current stream."""
+    if dev.index != torch.cuda.current_device():
+        raise MxqError("%s is on %s, which is not the current device" % (what, dev))
+    return dev
+
+
+def _heads(t, what: str, dev=None, heads=None, D=None):
+    """bf16 rows [tokens, heads, D] with unit stride along D."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16
+            and t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1)):
+        raise MxqError("%s must be a 3-D bf16 device tensor [tokens, heads, D] with unit "
+                       "stride along D" % what)
+    if dev is not None and t.device != dev:
+        raise MxqError("%s is on %s, not %s" % (what, t.device, dev))
+    if (heads is not None and t.shape[1] != heads) or (D is not None and t.shape[2] != D):
+        raise MxqError("%s is %s, not [tokens, %s, %s]" % (what, tuple(t.shape), heads, D))
+    return t
+
+
+def _index(t, n: int, dtype, what: str, dev):
+    """A contiguous 1-D integer device tensor of n elements."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 1
+            and t.is_contiguous()):
+        raise MxqError("%s must be a contiguous 1-D %s device tensor" % (what, dtype))
+    if t.shape[0] != n:
+        raise MxqError("%s holds %d elements, not %d" % (what, t.shape[0], n))
+    if t.device != dev:
+        raise MxqError("%s is on %s, not %s" % (what, t.device, dev))
+    return t
+
+
+def rope_inv_freq(rot: int, base: float = 10000.0, scaling: str | None = None,
+                  factor: float = 1.0, orig_positions: int = 0, low: float = 1.0,
+                  high: float = 32.0):
+    """The rotary frequencies of a head whose first `rot` values turn, for a
+    context `factor` times as long as the `orig_positions` a model was trained
+    on: (float64 array [rot / 2], factor for the cosines and sines).
+
+    None     f_i = base^(-2 i / rot).
+    "linear" f_i / factor: all positions squeezed into the trained range.
+    "base"   base * factor^(rot / (rot - 2)): the lowest frequency is divided by
+             the factor, the highest stays.
+    "ramp"   by the turns r_i = orig_positions f_i / 2 pi that a frequency makes
+             in the trained range: f_i for r_i >= high, f_i / factor for r_i <=
+             low, between the two their mix, linear in i from the index that
+             makes `high` turns (rounded down) to the one that makes `low` (up);
+             cosines and sines are scaled by 1 + 0.1 ln(factor).
+    "bands"  the mix linear in r_i instead, and cosines and sines as they are.
+    """
+    if rot < 2 or rot % 2:
+        raise MxqError("rot must be even and at least 2")
+    if not (np.isfinite(base) and base > 0 and np.isfinite(factor) and factor >= 1):
+        raise MxqError("base must be positive and factor at least 1")
+    i = np.arange(rot // 2, dtype=np.float64)
+    f = float(base) ** (-2.0 * i / rot)
+    if scaling is None:
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "base":
+        if rot == 2:                       # one frequency, which is 1
+            return f, 1.0
+        return (base * factor ** (rot / (rot - 2.0))) ** (-2.0 * i / rot), 1.0
+    if scaling not in ("ramp", "bands"):
+        raise MxqError("scaling must be None, 'linear', 'base', 'ramp' or 'bands'")
+    if orig_positions < 1 or not 0 < low < high:
+        raise MxqError("%r needs orig_positions and 0 < low < high" % scaling)
+    turns = orig_positions * f / (2 * np.pi)
+    if scaling == "bands":
+        keep = np.clip((turns - low) / (high - low), 0.0, 1.0)
+        return keep * f + (1 - keep) * f / factor, 1.0
+    if base == 1.0:
+        raise MxqError("'ramp' needs a base above 1")
+
+    def index(t):
+        return rot * np.log(orig_positions / (t * 2 * np.pi)) / (2 * np.log(base))
+
+    first, last = max(np.floor(index(high)), 0.0), min(np.ceil(index(low)), rot / 2 - 1.0)
+    keep = 1.0 - np.clip((i - first) / max(last - first, 0.001), 0.0, 1.0)
+    return keep * f + (1 - keep) * f / factor, 1.0 + 0.1 * float(np.log(factor))
+
+
+def rope_table(inv_freq, positions: int, mscale: float = 1.0, device="cuda", out=None):
+    """Cosines and sines of every position below `positions` (float32
+    [positions, rot / 2, 2], angles in float64, times mscale), made once."""
+    f = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64))
+    if f.ndim != 1 or not 1 <= f.size <= 256:
+        raise MxqError("inv_freq must hold 1 to 256 frequencies")
+    if positions < 1:
+        raise MxqError("positions must be at least 1")
+    if out is None:
+        out = torch.empty((positions, f.size, 2), dtype=torch.float32, device=device)
+    _dev_array(out, positions * f.size * 2, torch.float32, "table", out.device)
+    _current(out.device, "table")
+    _check(lib().mxq_rope_table(f.ctypes.data_as(ctypes.c_void_p), 2 * f.size, positions,
+                                float(mscale), _ptr(out), _stream()), "mxq_rope_table")
+    return out
+
+
+def _rotary(table, dev, interleaved: bool):
+    if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype is torch.float32
+            and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous()):
+        raise MxqError("the rotary table must be a contiguous float32 device tensor "
+                       "[positions, rot / 2, 2]")
+    if table.device != dev:
+        raise MxqError("the rotary table is on %s, not %s" % (table.device, dev))
+    return _Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1], 1 if interleaved else 0)
+
+
+def rope(x, pos, table, interleaved: bool = False, out=None):
+    """Rotary positions on bf16 rows x [T, H, D] (strided) at positions pos (int32
+    [T]): the first rot values of every head turn, as halves (i, i + rot / 2) or
+    interleaved pairs (2 i, 2 i + 1).  `out` may be x (in place), else a tensor
+    that does not overlap it."""
+    dev = _current(_heads(x, "x").device, "x")
+    T, H, D = x.shape
+    _index(pos, T, torch.int32, "pos", dev)
+    r = _rotary(table, dev, interleaved)
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=dev)
+    elif out is not x:
+        _heads(out, "out", dev, H, D)
+        if out.shape[0] != T:
+            raise MxqError("out is %s, not %s" % (tuple(out.shape), tuple(x.shape)))
+    _check(lib().mxq_rope(ctypes.byref(r), _ptr(x), T, H, D, x.stride(0), x.stride(1), _ptr(pos),
+                          _ptr(out), out.stride(0), out.stride(1), _stream()), "mxq_rope")
+    return out
+
+
+class PagedCache:
+    """A paged MXINT KV cache of one layer (include/mxq.h mxq_paged_kv): `pages`
+    pages of `page_tokens` tokens (a power of two, 16 to 1024) of Hkv heads of
+    128 values.  k and v are (mant, exp) pairs of uint8 device tensors of
+    pages * page_bytes and pages * page_exp_bytes bytes: the caller's, or new
+    ones, zeroed."""
+
+    def __init__(self, fmt: Format, Hkv: int, pages: int, page_tokens: int, device="cuda",
+                 k=None, v=None):
+        self.fmt, self.Hkv = fmt, int(Hkv)
+        self.pages, self.page_tokens = int(pages), int(page_tokens)
+        L = lib()
+        if not 16 <= self.page_tokens <= 1024:
+            _check(2, "PagedCache")
+        self.page_bytes = _size(L.mxq_kv_page_bytes(fmt.ref, self.Hkv, self.page_tokens),
+                                "mxq_kv_page_bytes")
+        self.page_exp_bytes = _size(L.mxq_kv_page_exp_bytes(fmt.ref, self.Hkv, self.page_tokens),
+                                    "mxq_kv_page_exp_bytes")
+        if self.pages < 1 or self.pages * self.page_tokens > 2 ** 31 - 1:
+            _check(2, "PagedCache")
+
+        def buffers(t, what):
+            nm, ne = self.pages * self.page_bytes, self.pages * self.page_exp_bytes
+            if t is None:
+                return (torch.zeros(nm, dtype=torch.uint8, device=device),
+                        torch.zeros(ne, dtype=torch.uint8, device=device))
+            mant, exp = t
+            _dev_bytes(mant, nm, what + " mantissa buffer")
+            return mant, _dev_bytes(exp, ne, what + " exponent buffer", mant.device)
+
+        self.k, self.v = buffers(k, "K"), buffers(v, "V")
+        self.device = self.k[0].device
+        if self.v[0].device != self.device:
+            raise MxqError("K and V must be on one device")
+        self._c = _PagedKv(self.pages, self.Hkv, self.page_tokens, 0, *[
+            t.data_ptr() for t in self.k + self.v])
+        self._ref = ctypes.byref(self._c)
+
+
+def kv_append(cache: PagedCache, k, v, slots, pos=None, rope=None, interleaved: bool = False,
+              q=None, q_out=None):
+    """New tokens into the cache: keys k (rotated at positions pos int32 [T] with
+    the table `rope`, where it is given) and values v, bf16 [T, Hkv, 128]
+    (strided), quantized into slots (int64 [T], distinct; one outside the cache
+    is padding).  With q (bf16 [T, Hq, 128], strided) the queries are rotated by
+    the same launch, and returned (contiguous; q_out may be q if that is
+    contiguous)."""
+    dev = _current(cache.device, "the cache")
+    _heads(k, "k", dev, cache.Hkv, 128)
+    _heads(v, "v", dev, cache.Hkv, 128)
+    T = k.shape[0]
+    if v.shape[0] != T:
+        raise MxqError("k and v have %d and %d tokens" % (T, v.shape[0]))
+    _index(slots, T, torch.int64, "slots", dev)
+    r = None
+    if rope is not None:
+        r = ctypes.byref(_rotary(rope, dev, interleaved))
+        _index(pos, T, torch.int32, "pos", dev)
+    Hq, qs = 0, (0, 0)
+    if q is not None:
+        _heads(q, "q", dev, None, 128)
+        Hq, qs = q.shape[1], (q.stride(0), q.stride(1))
+        if q.shape[0] != T or Hq < 1:
+            raise MxqError("q is %s: %d tokens and a head are needed" % (tuple(q.shape), T))
+        if q_out is None:
+            q_out = torch.empty((T, Hq, 128), dtype=torch.bfloat16, device=dev)
+        elif not _heads(q_out, "q_out", dev, Hq, 128).is_contiguous() or q_out.shape[0] != T:
+            raise MxqError("q_out must be contiguous, [%d, %d, 128]" % (T, Hq))
+    elif q_out is not None:
+        raise MxqError("q_out needs q")
+    _check(lib().mxq_kv_append(cache.fmt.ref, cache._ref, _ptr(k), k.stride(0), k.stride(1),
+                               _ptr(v), v.stride(0), v.stride(1), T, _ptr(slots),
+                               None if r is None else _ptr(pos), r, _ptr(q), Hq, qs[0], qs[1],
+                               _ptr(q_out), _stream()), "mxq_kv_append")
+    return q_out
+
+
+def kv_read(cache: PagedCache, slots, out=None):
+    """The cached rows of the slots (int64 [n]) as the bf16 values that they stand
+    for: (k, v), each [n, Hkv, 128]; zeros for a slot outside the cache."""
+    dev = _current(cache.device, "the cache")
+    if not isinstance(slots, torch.Tensor):
+        raise MxqError("slots must be a contiguous 1-D torch.int64 device tensor")
+    n = slots.shape[0] if slots.dim() == 1 else 0
+    _index(slots, n, torch.int64, "slots", dev)
+    if out is None:
+        out = tuple(torch.empty((n, cache.Hkv, 128), dtype=torch.bfloat16, device=dev)
+                    for _ in range(2))
+    k, v = out
+    for t, what in ((k, "k"), (v, "v")):
+        if not _heads(t, what, dev, cache.Hkv, 128).is_contiguous() or t.shape[0] != n:
+            raise MxqError("%s must be contiguous, [%d, %d, 128]" % (what, n, cache.Hkv))
+    _check(lib().mxq_kv_read(cache.fmt.ref, cache._ref, _ptr(slots), n, _ptr(k), _ptr(v),
+                             _stream()), "mxq_kv_read")
+    return k, v
+
+
+def attn_paged_work_bytes(cache: PagedCache, S: int, T: int, Hq: int, max_q: int,
+                          max_kv: int) -> int:
+    """Bytes of the scratch that attn_paged needs for these sizes."""
+    return _size(lib().mxq_attn_paged_work_bytes(cache.fmt.ref, cache._ref, S, T, Hq, max_q,
+                                                 max_kv), "mxq_attn_paged_work_bytes")
+
+
+def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: int, scale: float,
+               softcap: float = 0.0, window: int = 0, prefix=None, slopes=None, out=None,
+               dtype=torch.bfloat16, work=None):
+    """Attention of the new tokens of S sequences over their pages.  q: bf16 [T,
+    Hq, 128] (strided), sequence s owning the rows cu_q[s] .. cu_q[s + 1] (int32
+    [S + 1]), which are the last of its kv_len[s] (int32 [S]) cached tokens; its
+    pages are table[s] (int32 [S, n]).  max_q and max_kv bound the sequences'
+    rows and lengths.  A row sees the tokens up to its own, of those the last
+    `window` (0: all), and the first prefix[s] (int32 [S]); scores are capped by
+    softcap * tanh(x / softcap) and lowered by slopes[h] (float32 [Hq]) times the
+    distance.  Returns bf16 or float32 (`dtype`) [T, Hq, 128]."""
+    dev = _current(cache.device, "the cache")
+    T, Hq, _ = _heads(q, "q", dev, None, 128).shape
+    if not (isinstance(kv_len, torch.Tensor) and kv_len.dim() == 1):
+        raise MxqError("kv_len must be a contiguous 1-D torch.int32 device tensor")
+    S = kv_len.shape[0]
+    _index(kv_len, S, torch.int32, "kv_len", dev)
+    _index(cu_q, S + 1, torch.int32, "cu_q", dev)
+    if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype is torch.int32
+            and table.dim() == 2 and table.shape[0] == S and table.device == dev
+            and (table.stride(1) == 1 or table.shape[1] <= 1)):
+        raise MxqError("table must be an int32 device tensor [%d, pages] with unit stride" % S)
+    if prefix is not None:
+        _index(prefix, S, torch.int32, "prefix", dev)
+    if slopes is not None:
+        _index(slopes, Hq, torch.float32, "slopes", dev)
+    if out is None:
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise MxqError("dtype must be torch.bfloat16 or torch.float32")
+        out = torch.empty((T, Hq, 128), dtype=dtype, device=dev)
+    elif not (isinstance(out, torch.Tensor) and out.is_cuda and out.is_contiguous()
+              and out.dtype in (torch.bfloat16, torch.float32) and out.device == dev
+              and out.shape == q.shape):
+        raise MxqError("out must be a contiguous bf16 or float32 device tensor [%d, %d, 128]"
+                       % (T, Hq))
+    if work is None:
+        n = attn_paged_work_bytes(cache, S, T, Hq, max_q, max_kv)
+        work = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+    _dev_bytes(work, 0, "work", dev)
+    batch = _PagedBatch(S, T, max_q, max_kv, cu_q.data_ptr(), kv_len.data_ptr(),
+                        table.data_ptr(), table.stride(0), table.shape[1])
+    opts = _AttnOpts(scale, softcap, window, _ptr(prefix), _ptr(slopes))
+    _check(lib().mxq_attn_paged(cache.fmt.ref, cache._ref, ctypes.byref(batch),
+                                ctypes.byref(opts), _ptr(q), Hq, q.stride(0), q.stride(1),
+                                _ptr(out), 1 if out.dtype is torch.float32 else 0, _ptr(work),
+                                work.numel(), _stream()), "mxq_attn_paged")
     return out

@@ -1,0 +1,312 @@
+"""Attention over the paged MXINT cache (mxq_attn_paged) against the float64
+oracle; the bounds are derived in paged_util.  Every cache is noise outside the
+appended rows, E = 255 with mantissas among it, so that a place behind a
+sequence's last token, or another sequence's page, shows at once."""
+import numpy as np
+import pytest
+import torch
+
+from paged_util import D, Batch
+from paper_2607_17733_amd import mxq
+from parity_util import say
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16]
+MIXES = [(n4, n6, 4 - n4 - n6) for n4 in range(4, -1, -1) for n6 in range(4 - n4, -1, -1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300])
+def test_single_tokens(n, dtype):
+    say("decode", n, dtype)
+    Batch(n, [(1, n), (1, max(1, n // 2)), (1, n)], 8, 2).check(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 33, 64, 65, 130, 257])
+def test_whole_prompts(n, dtype):
+    say("prompt", n, dtype)
+    Batch(100 + n, [(n, n), (max(1, n // 3), max(1, n // 3))], 4, 2).check(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("q,n", [(2, 300), (5, 131), (7, 64), (20, 333), (40, 200), (130, 259)])
+def test_chunks_after_a_cached_part(q, n, dtype):
+    say("chunk", q, n, dtype)
+    Batch(200 + q, [(q, n), (q, q), (q, q + 1)], 8, 2, widths=(4, 4, 6, 8)).check(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_mixed_batch_with_empty_sequences(dtype):
+    # sequences without new tokens, without any token, with one, with a chunk
+    lens = [(0, 40), (1, 77), (33, 90), (0, 0), (1, 1), (70, 70), (3, 500), (0, 5)]
+    Batch(300, lens, 8, 2, widths=(3, 4, 6, 8), page=32).check(dtype)
+
+
+@pytest.mark.parametrize("mix", MIXES)
+@pytest.mark.parametrize("low", [3, 4])
+def test_every_width_mix(mix, low):
+    w = [low] * mix[0] + [6] * mix[1] + [8] * mix[2]
+    if mix[0] == 2 and low == 3:
+        w[1] = 4
+    say("widths", w)
+    Batch(400 + sum(w), [(1, 70), (21, 70)], 8, 2, widths=w).check(torch.float32)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (5, 5), (6, 2), (12, 4), (16, 1), (17, 1), (40, 2), (64, 1)])
+def test_head_groupings(Hq, Hkv, dtype):
+    say("heads", Hq, Hkv, dtype)
+    Batch(500 + Hq, [(1, 130), (9, 75)], Hq, Hkv).check(dtype)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256, 512, 1024])
+def test_page_sizes(page):
+    Batch(600 + page, [(1, 1030), (37, 500), (1, 15)], 4, 2, page=page, extra_pages=1).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("window", [1, 2, 16, 50, 64, 100, 1000])
+def test_windows(window, dtype):
+    Batch(700 + window, [(1, 300), (90, 200), (200, 200)], 4, 2, window=window).check(dtype)
+
+
+@pytest.mark.parametrize("window", [0, 1, 40])
+def test_prefixes(window):
+    # a prefix of nothing, of some tokens, past the rows' own positions, past the end
+    lens = [(1, 200), (60, 200), (100, 100), (100, 100), (30, 90), (5, 5)]
+    Batch(800 + window, lens, 4, 2, window=window, prefix=[3, 17, 0, 64, 90, 1000]).check()
+    Batch(801 + window, lens, 4, 2, window=window, prefix=[-5, 130, 99, 100, 0, 2]).check(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_capped_and_biased_scores(dtype):
+    lens = [(1, 333), (50, 210), (128, 128)]
+    slopes = [2.0 ** -(i + 1) for i in range(8)]
+    Batch(900, lens, 8, 2, softcap=5.0).check(dtype)
+    Batch(901, lens, 8, 2, slopes=slopes).check(dtype)
+    Batch(902, lens, 8, 2, softcap=20.0, slopes=slopes, window=70, prefix=[2, 0, 60]).check(dtype)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1.0, 4.0])
+def test_scales(scale):
+    Batch(950, [(1, 150), (40, 90)], 4, 2, scale=scale).check()
+
+
+def test_rows_that_see_nothing_are_zero():
+    # more new tokens than cached ones (positions below zero), no token at all
+    b = Batch(960, [(5, 5), (1, 40)], 4, 2)
+    b.kv_len.copy_(torch.tensor([2, 0]))
+    for dtype in TYPES:
+        o = b.run(dtype)
+        assert not o[:3].any() and not o[5].any() and bool(o[3:5].any(dim=2).all())
+    b = Batch(961, [(40, 40)], 4, 2, prefix=[3])
+    b.kv_len.copy_(torch.tensor([6]))                      # rows at -34 .. 5: the prefix is seen by all
+    o = b.run()
+    assert bool(o.any(dim=2).all())
+    assert torch.allclose(o[0].isnan(), torch.zeros_like(o[0], dtype=torch.bool))
+
+
+def test_rows_outside_every_sequence_stay_as_they_are():
+    for lens in ([(1, 60), (1, 9)], [(40, 60), (3, 9)]):
+        for dtype in TYPES:
+            b = Batch(970, lens, 8, 2, tail_rows=37)
+            out = torch.full((b.T, 8, D), 7.0, dtype=dtype, device="cuda")
+            b.q[-37:] = float("nan")
+            b.run(dtype, out=out)
+            assert bool((out[-37:] == 7.0).all()) and not out[:-37].isnan().any()
+
+
+def test_table_entries_outside_the_pool_read_as_zero_rows():
+    b = Batch(980, [(1, 100), (30, 64)], 4, 2, page=16)
+    kk, vv = mxq.kv_read(b.cache, b.slots)
+    zero = torch.zeros_like(kk[:16])
+    mxq.kv_append(b.cache, zero, zero, b.slots[16:32])     # the second page of the first sequence
+    mxq.kv_append(b.cache, zero[:16], zero[:16], b.slots[148:164])   # the last page of the second
+    want = [b.run(t) for t in TYPES]
+    for hole in (-1, 2 ** 31 - 1, -2 ** 31, b.cache.pages):
+        b.table[0, 1] = hole
+        b.table[1, 3] = hole
+        for t, w in zip(TYPES, want):
+            assert torch.equal(b.run(t), w)
+
+
+def test_strided_queries_and_table():
+    b = Batch(990, [(1, 100), (30, 64)], 6, 2)
+    want = b.run()
+    fused = torch.randn((b.T, 10, D), device="cuda").to(torch.bfloat16)
+    fused[:, 2:8] = b.q
+    assert torch.equal(b.run(q=fused[:, 2:8]), want)
+    heads = b.q.transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(b.run(q=heads), want)
+    wide = torch.full((2, b.table.shape[1] + 9), -7, dtype=torch.int32, device="cuda")
+    wide[:, 4:4 + b.table.shape[1]] = b.table
+    b.table = wide[:, 4:4 + b.table.shape[1]]
+    assert torch.equal(b.run(), want)
+
+
+def test_lengths_end_at_the_table_and_at_max_kv():
+    b = Batch(995, [(1, 100)], 4, 2, page=16)
+    b.kv_len.fill_(48)
+    want = b.run()
+    b.kv_len.fill_(2 ** 31 - 1)
+    full = b.table
+    b.table = full[:, :3].contiguous()
+    assert torch.equal(b.run(), want)
+    b.table, b.max_kv = full, 48
+    assert torch.equal(b.run(), want)
+
+
+@pytest.mark.parametrize("spread", [12, 40])
+def test_blocks_of_unlike_size(spread):
+    # block scales far apart: K's and V's from 2^-spread to 2^spread
+    Batch(1000 + spread, [(1, 90), (20, 60)], 4, 2, widths=(4, 4, 6, 8), spread=spread,
+          scale=2.0 ** -(spread + 3)).check()
+
+
+@pytest.mark.parametrize("widths", [(3, 4, 6, 8), (4, 4, 4, 4), (8, 8, 8, 8), (6, 6, 6, 6)])
+def test_values_at_the_ends_of_the_range(widths):
+    # V blocks near 2^110 (sums of them stay in range) and below 2^-126, K zero (uniform weights)
+    b = Batch(1100, [(1, 40), (20, 40)], 4, 2, widths=widths)
+    g = torch.Generator().manual_seed(5)
+    n = b.slots.numel()
+    v = torch.rand((n, 2, D), generator=g) * 0.75 + 0.25
+    v[:, 0] *= 2.0 ** 110
+    v[:, 1] *= 2.0 ** -126
+    k = torch.zeros((n, 2, D), dtype=torch.bfloat16)
+    mxq.kv_append(b.cache, k.cuda(), v.to(torch.bfloat16).cuda(), b.slots)
+    _, vv = mxq.kv_read(b.cache, b.slots)
+    for dtype in TYPES:
+        o = b.run(dtype).double().cpu()
+        assert bool(torch.isfinite(o).all())
+        for s, (rows, at) in enumerate(((range(0, 1), 0), (range(1, 21), 40))):
+            for r in rows:
+                L = 40 if s == 0 else 21 + (r - 1)
+                mean = vv[at:at + L].double().cpu().mean(dim=0).repeat_interleave(2, dim=0)
+                tol = (2.0 ** -7 if dtype is torch.bfloat16 else 2.0 ** -18)
+                # (values near 2^-126 may lose up to 2^-133 to bf16's subnormal steps)
+                assert bool(((o[r] - mean).abs() <= tol * mean.abs() + 2.0 ** -132).all())
+
+
+def test_infinite_and_nan_queries_stay_in_their_rows():
+    b = Batch(1200, [(1, 60), (40, 100)], 4, 2)
+    want = {t: b.run(t) for t in TYPES}
+    b.q[0, 1, 3] = float("nan")
+    b.q[7, 2, 9] = float("inf")
+    keep = torch.ones((b.T, 4), dtype=torch.bool, device="cuda")
+    keep[0, 1] = keep[7, 2] = False
+    for t in TYPES:
+        o = b.run(t)
+        assert bool(o[0, 1].isnan().all()) and torch.equal(o[keep], want[t][keep])
+
+
+def test_keys_that_held_infinities_count_as_zero():
+    b = Batch(1210, [(1, 50), (17, 50)], 4, 2)
+    x = torch.randn((100, 2, D), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16)
+    y = x.clone()
+    y[::7, :, 40] = float("inf")
+    y[3::7, :, 100] = float("nan")
+    z = x.clone()
+    z[::7, :, 32:64] = 0
+    z[3::7, :, 96:] = 0
+    out = []
+    for rows in (y, z):
+        mxq.kv_append(b.cache, rows.cuda(), rows.cuda(), b.slots)
+        out.append([b.run(t) for t in TYPES])
+    for a, c in zip(*out):
+        assert torch.equal(a, c) and bool(torch.isfinite(a).all())
+
+
+def test_repeats_and_work_contents_do_not_matter():
+    for lens in ([(1, 3000), (1, 700)], [(300, 900), (1, 40)]):
+        b = Batch(1300, lens, 8, 2)
+        n = mxq.attn_paged_work_bytes(b.cache, b.S, b.T, 8, b.max_q, b.max_kv)
+        work = torch.full((max(n, 16),), 255, dtype=torch.uint8, device="cuda")
+        for t in TYPES:
+            first = b.run(t, work=work)
+            assert torch.equal(first, b.run(t, work=work)) and torch.equal(first, b.run(t))
+
+
+def test_long_caches():
+    Batch(1400, [(1, 20000), (1, 1)], 8, 1).check(seqs=[0])
+    Batch(1401, [(5, 9001)], 8, 1, page=256, widths=(4, 4, 4, 8)).check(torch.bfloat16)
+
+
+def test_serving_batch_sampled():
+    # 24 sequences of unlike length, one of them far longer
+    lens = [(1, 50 + 61 * i) for i in range(23)] + [(1, 12000)]
+    Batch(1402, lens, 32, 8, page=64).check(seqs=[0, 7, 22, 23])
+
+
+def test_prompt_chunk_sampled():
+    Batch(1403, [(150, 2100), (1, 700), (400, 400)], 16, 2, page=64, widths=(4, 4, 4, 6)).check(
+        torch.bfloat16, seqs=[0, 1])
+
+
+def test_graph_replays_with_other_lengths():
+    # a decode step captured once, replayed as the sequences grow; and a chunk
+    for q, lens in ((1, [(1, 700), (1, 64)]), (20, [(20, 300), (20, 64)])):
+        b = Batch(1500 + q, lens, 8, 2)
+        work = torch.empty(max(16, mxq.attn_paged_work_bytes(b.cache, 2, b.T, 8, b.max_q, 1024)),
+                           dtype=torch.uint8, device="cuda")
+        b.max_kv = 1024
+        out = torch.empty((b.T, 8, D), dtype=torch.float32, device="cuda")
+        b.run(out=out, work=work)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.run(out=out, work=work)
+        first = b.kv_len.clone()
+        for step in (0, 5, 41, 20):
+            b.kv_len.copy_(first - step)
+            want = b.run()
+            out.fill_(float("nan"))
+            work.fill_(0xA5)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+
+
+def test_another_stream():
+    b = Batch(1600, [(1, 500), (40, 80)], 8, 2)
+    want = b.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = b.run()
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_layers_steps_together():
+    # a prompt in two chunks, then tokens one by one, appended and attended through one cache,
+    # against the whole prompt at once: the same rows, whatever the chunks
+    Hq, Hkv, page, N = 8, 2, 16, 75
+    g = torch.Generator().manual_seed(8)
+    rows = torch.randn((N, Hq + 2 * Hkv, D), generator=g).to(torch.bfloat16).cuda()
+    q, k, v = rows.split([Hq, Hkv, Hkv], dim=1)
+    table = mxq.rope_table(mxq.rope_inv_freq(128)[0], 128)
+    pages = torch.randperm(6, generator=g).int().cuda()[None]
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    slots = pages[0].long()[pos.long() // page] * page + pos.long() % page
+
+    def step(cache, a, b):
+        cu = torch.tensor([0, b - a], dtype=torch.int32, device="cuda")
+        n = torch.tensor([b], dtype=torch.int32, device="cuda")
+        qr = mxq.kv_append(cache, k[a:b], v[a:b], slots[a:b], pos=pos[a:b], rope=table, q=q[a:b])
+        assert torch.equal(qr, mxq.rope(q[a:b], pos[a:b], table))
+        return mxq.attn_paged(qr, cache, cu, n, pages, b - a, b, D ** -0.5, dtype=torch.float32)
+
+    fmt = mxq.Format(D, [4, 4, 6, 8])
+    whole = step(mxq.PagedCache(fmt, Hkv, 6, page), 0, N)
+    cache = mxq.PagedCache(fmt, Hkv, 6, page)
+    cuts = [0, 33, 70] + list(range(71, N + 1))
+    parts = torch.cat([step(cache, a, b) for a, b in zip(cuts, cuts[1:])])
+    # two float32 evaluations of the same mean, each within 2^-24 (131 + 4 + 64) of the values'
+    # largest (scores are of the order of 1 here; see paged_util)
+    bound = 2 * 2 * 2.0 ** -24 * (131 * 16 + 4 + 64 * 4) * float(v.float().abs().max()) * 1.1
+    assert float((whole - parts).abs().max()) <= bound
+    # the rotated, quantized first token attends to itself alone
+    _, vv = mxq.kv_read(cache, slots[:1])
+    assert torch.equal(whole[0], vv[0].float().repeat_interleave(Hq // Hkv, dim=0))

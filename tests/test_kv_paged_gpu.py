@@ -1,0 +1,221 @@
+"""The paged MXINT cache (mxq_kv_append, mxq_kv_read): bytes against the oracle.
+
+Rotation, quantization and layout are defined exactly, so every comparison is
+bit for bit: the pool's bytes after appending, the bytes that must not change,
+and the values read back.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import paged as opaged
+from paper_2607_17733_amd import mxq
+from parity_util import say
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+MIXES = [[3, 3, 3, 3], [4, 4, 4, 4], [6, 6, 6, 6], [8, 8, 8, 8], [4, 4, 6, 8], [3, 3, 6, 8],
+         [3, 4, 6, 8], [3, 4, 4, 4], [6, 6, 8, 8], [4, 6, 6, 6]]
+
+
+def bits_of(t):
+    return t.cpu().contiguous().view(torch.int16).numpy().view(np.uint16)
+
+
+def _pool(n, seed):
+    return torch.randint(0, 256, (n,), dtype=torch.uint8,
+                         generator=torch.Generator().manual_seed(seed))
+
+
+def _cache(widths, Hkv, pages, page, seed=1, round_="rne", clamp="sym"):
+    """A cache whose bytes are noise before anything is stored."""
+    fmt = mxq.Format(D, widths, round=round_, clamp=clamp)
+    c = mxq.PagedCache(fmt, Hkv, pages, page)
+    for i, t in enumerate(c.k + c.v):
+        t.copy_(_pool(t.numel(), seed + i))
+    return c
+
+
+def _rows(T, H, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((T, H, D), generator=g) * torch.exp2(torch.randint(-6, 7, (T, H, D // 32), generator=g)
+                                                         .float()).repeat_interleave(32, dim=2)
+    return x.to(torch.bfloat16)
+
+
+def _check(widths, T, Hkv, Hq, page, rot, interleaved, seed=0, round_="rne", clamp="sym", pages=None,
+           slots=None, strided=False):
+    say("append", widths, T, Hkv, Hq, page, rot, interleaved, round_, clamp)
+    pages = pages or -(-T // page) + 2
+    c = _cache(widths, Hkv, pages, page, seed + 1, round_, clamp)
+    want = [t.cpu().numpy().copy() for t in c.k + c.v]
+    fused = _rows(T, Hq + 2 * Hkv, seed + 2)
+    q, k, v = fused.split([Hq, Hkv, Hkv], dim=1)
+    g = torch.Generator().manual_seed(seed + 3)
+    if slots is None:
+        slots = torch.randperm(pages * page, generator=g)[:T]
+    pos = torch.randint(0, 300, (T,), generator=g).int()
+    table = mxq.rope_table(mxq.rope_inv_freq(rot)[0], 300) if rot else None
+    tn = table.cpu().numpy() if rot else None
+    dev = fused.cuda()
+    qd, kd, vd = dev.split([Hq, Hkv, Hkv], dim=1)
+    if not strided:
+        qd, kd, vd = qd.contiguous(), kd.contiguous(), vd.contiguous()
+    got_q = mxq.kv_append(c, kd, vd, slots.cuda(), pos=pos.cuda() if rot else None, rope=table,
+                          interleaved=interleaved, q=qd if Hq else None)
+    rk, rv = mxq.kv_read(c, slots.cuda())
+    torch.cuda.synchronize()
+    rm, cm = int(round_ == "rna"), int(clamp == "full")
+    kb, qb = bits_of(k), bits_of(q)
+    if rot:
+        kb = opaged.rope(kb, pos.numpy(), tn, interleaved)
+        qb = opaged.rope(qb, pos.numpy(), tn, interleaved)
+    s = slots.numpy()
+    opaged.append(want[0], want[1], kb, s, widths, Hkv, page, pages, rm, cm)
+    opaged.append(want[2], want[3], bits_of(v), s, widths, Hkv, page, pages, rm, cm)
+    for t, w, what in zip(c.k + c.v, want, ("K", "K exp", "V", "V exp")):
+        assert np.array_equal(t.cpu().numpy(), w), what
+    if Hq:
+        assert np.array_equal(bits_of(got_q), qb)
+    ok = (s >= 0) & (s < pages * page)
+    for t, b in ((rk, kb), (rv, bits_of(v))):
+        ref = opaged.values(b, widths, rm, cm)
+        ref[~ok] = 0
+        assert np.array_equal(t.cpu().double().numpy(), ref)
+
+
+@pytest.mark.parametrize("widths", MIXES)
+@pytest.mark.parametrize("clamp", ["sym", "full"])
+def test_every_width(widths, clamp):
+    _check(widths, 37, 2, 4, 16, 128, False, seed=sum(widths), clamp=clamp,
+           round_="rna" if sum(widths) % 2 else "rne")
+
+
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 33, 100])
+@pytest.mark.parametrize("page", [16, 64, 1024])
+def test_lengths_and_pages(T, page):
+    _check([4, 4, 6, 8], T, 3, 5, page, 64, True, seed=T, strided=True)
+
+
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (16, False), (16, True), (96, False), (96, True),
+                                             (128, True)])
+def test_rotations(rot, interleaved):
+    _check([3, 4, 6, 8], 21, 2, 3, 32, rot, interleaved, seed=rot, strided=True)
+
+
+@pytest.mark.parametrize("Hkv,Hq", [(1, 0), (1, 1), (1, 40), (16, 16), (8, 64)])
+def test_heads(Hkv, Hq):
+    _check([4, 4, 4, 4], 18, Hkv, Hq, 16, 128, False, seed=Hq)
+
+
+def test_padding_slots_are_not_stored():
+    T, page = 20, 16
+    slots = torch.randperm(48, generator=torch.Generator().manual_seed(2))[:T]
+    slots[3], slots[7], slots[11], slots[19] = -1, 48, -2 ** 63, 2 ** 62
+    _check([4, 4, 4, 8], T, 2, 2, page, 32, False, pages=3, slots=slots)
+
+
+def test_composition_with_rope_and_quantize_rows():
+    # the append's rows are those of rope followed by quantize_rows
+    T, Hkv, page, widths = 50, 2, 16, [4, 4, 6, 6]
+    c = _cache(widths, Hkv, 4, page)
+    k, v = _rows(T, Hkv, 5).cuda(), _rows(T, Hkv, 6).cuda()
+    pos = torch.arange(100, 100 + T, dtype=torch.int32, device="cuda")
+    table = mxq.rope_table(mxq.rope_inv_freq(128)[0], 200)
+    slots = torch.arange(T, device="cuda")
+    mxq.kv_append(c, k, v, slots, pos=pos, rope=table)
+    rk, rv = mxq.kv_read(c, slots)
+    for x, got in ((mxq.rope(k, pos, table), rk), (v, rv)):
+        rows, exps = mxq.quantize_rows(x.reshape(T * Hkv, D), c.fmt)
+        q, e = mxq.unpack_act(rows, exps, c.fmt, T * Hkv)
+        ref = oracle.dequantize(q.cpu().numpy(), e.cpu().numpy(), widths)
+        torch.cuda.synchronize()
+        assert np.array_equal(got.cpu().double().numpy().reshape(T * Hkv, D), ref)
+
+
+def test_special_values():
+    # zero, subnormal, huge, infinite and NaN blocks; a NaN from a position
+    # without an angle: E = 255 and zero mantissas
+    T, Hkv = 8, 1
+    k = torch.zeros((T, Hkv, D), dtype=torch.bfloat16)
+    k[1] = 1e-39
+    k[2] = 3.3e38
+    k[3, 0, 5] = float("inf")
+    k[4, 0, 40] = float("nan")
+    k[5] = -2.0 ** -126
+    k[6] = -0.0
+    k[7] = 1.0
+    for widths in ([3, 4, 6, 8], [8, 8, 8, 8], [4, 4, 4, 4]):
+        c = _cache(widths, Hkv, 1, 16)
+        want = [t.cpu().numpy().copy() for t in c.k]
+        slots = torch.arange(T)
+        mxq.kv_append(c, k.cuda(), k.cuda(), slots.cuda())
+        rk, rv = mxq.kv_read(c, slots.cuda())
+        torch.cuda.synchronize()
+        opaged.append(want[0], want[1], bits_of(k), slots.numpy(), widths, Hkv, 16, 1)
+        assert np.array_equal(c.k[0].cpu().numpy(), want[0])
+        assert np.array_equal(c.k[1].cpu().numpy(), want[1])
+        # (an E = 255 block stands for zeros here)
+        assert torch.equal(rk, rv) and bool(torch.isfinite(rk).all())
+        ref = opaged.values(bits_of(k), widths)
+        assert np.array_equal(rk.cpu().double().numpy(), ref)
+    table = mxq.rope_table(mxq.rope_inv_freq(128)[0], 4)
+    pos = torch.tensor([0, 1, 2, 3, 4, -1, 3, 7], dtype=torch.int32, device="cuda")
+    c = _cache([4, 4, 4, 4], 1, 1, 16)
+    mxq.kv_append(c, torch.ones_like(k).cuda(), k.cuda(), slots.cuda(), pos=pos, rope=table)
+    torch.cuda.synchronize()
+    e = c.k[1].cpu().view(16, 4)[:T]
+    assert [bool((r == 255).all()) for r in e] == [False] * 4 + [True, True, False, True]
+
+
+def test_queries_in_place_and_far_slots():
+    # q rotated in place (all halves and pairs), and a pool past 2^32 bytes, whose
+    # last slots need 64-bit offsets
+    T, Hkv, page = 33, 16, 1024
+    widths = [8, 8, 8, 8]
+    pages = 2200                                               # 4.6 GB of K mantissas
+    assert pages * page * Hkv * 128 > 2 ** 32
+    fmt = mxq.Format(D, widths)
+    n = pages * page
+    mk = lambda m: (torch.empty(m * Hkv * 128, dtype=torch.uint8, device="cuda"),  # noqa: E731
+                    torch.empty(m * Hkv * 4, dtype=torch.uint8, device="cuda"))
+    c = mxq.PagedCache(fmt, Hkv, pages, page, k=mk(n), v=mk(n))
+    k, v, q = _rows(T, Hkv, 1), _rows(T, Hkv, 2), _rows(T, 4, 3)
+    slots = torch.cat([torch.arange(n - 20, n), torch.arange(13)])
+    pos = torch.arange(T, dtype=torch.int32)
+    table = mxq.rope_table(mxq.rope_inv_freq(128)[0], 64)
+    for interleaved in (False, True):
+        qd = q.cuda()
+        got = mxq.kv_append(c, k.cuda(), v.cuda(), slots.cuda(), pos=pos.cuda(), rope=table,
+                            interleaved=interleaved, q=qd, q_out=qd)
+        rk, rv = mxq.kv_read(c, slots.cuda())
+        torch.cuda.synchronize()
+        tn = table.cpu().numpy()
+        assert got is qd and np.array_equal(bits_of(qd), opaged.rope(bits_of(q), pos.numpy(), tn, interleaved))
+        kb = opaged.rope(bits_of(k), pos.numpy(), tn, interleaved)
+        assert np.array_equal(rk.cpu().double().numpy(), opaged.values(kb, widths))
+        assert np.array_equal(rv.cpu().double().numpy(), opaged.values(bits_of(v), widths))
+
+
+def test_read_outside_the_cache_is_zero():
+    c = _cache([4, 4, 6, 8], 2, 2, 16)
+    x = _rows(32, 2, 8).cuda()
+    mxq.kv_append(c, x, x, torch.arange(32, device="cuda"))
+    slots = torch.tensor([-1, 0, 31, 32, 2 ** 40, -2 ** 63, 5, 5], device="cuda")
+    k, v = mxq.kv_read(c, slots)
+    torch.cuda.synchronize()
+    assert not k[[0, 3, 4, 5]].any() and not v[[0, 3, 4, 5]].any()
+    assert torch.equal(k[6], k[7]) and k[1].any() and k[2].any()
+
+
+def test_no_tokens():
+    c = _cache([4, 4, 4, 4], 2, 1, 16)
+    before = c.k[0].clone()
+    e = torch.empty((0, 2, D), dtype=torch.bfloat16, device="cuda")
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    mxq.kv_append(c, e, e, none)
+    k, v = mxq.kv_read(c, none)
+    torch.cuda.synchronize()
+    assert k.shape == (0, 2, D) and torch.equal(before, c.k[0])

@@ -14,6 +14,13 @@
 // the registers.  K and V are dequantized once per workgroup into LDS as bf16,
 // which is exact (at most 8 significant bits): a wave per 32-value block of the
 // row, a lane per token, so that widths are uniform over a wave.
+//
+// Sequences with at most 16 query rows per KV head (decoding, drafted tokens) have
+// a kernel of their own: bytes and dequantization bound them, not products.  There
+// each wave takes chunks of 32 tokens by itself, without a barrier, dequantizes K
+// straight into the operand of 16x16x32 products and V into its own LDS rows, and
+// the waves are merged at the end.  The tokens of a sequence are split over
+// workgroups where there are few rows; the splits' results are merged in order.
 #include <algorithm>
 
 #include "mxq_device.h"
@@ -39,6 +46,7 @@ constexpr int kD = 128;
 constexpr int kTok = 64;                 // tokens per step
 constexpr int kWaves = 4;
 constexpr int kRows = 32 * kWaves;       // query rows of a tile
+constexpr int kFewRows = 16;             // query rows of the kernel for few
 constexpr int kMaxSplits = 256;
 constexpr float kLog2e = 1.44269504f;
 
@@ -74,7 +82,7 @@ struct RawBlock {
 };
 
 template <int M>
-__device__ inline void load_block(const uint8_t *p, RawBlock &r) {
+__device__ __forceinline__ void load_block(const uint8_t *p, RawBlock &r) {
   if constexpr (M == 4 || M == 8) {
 #pragma unroll
     for (int i = 0; i < M / 4; ++i) {
@@ -94,7 +102,7 @@ __device__ inline void load_block(const uint8_t *p, RawBlock &r) {
     for (int i = 0; i < 3; ++i) r.w[i] = *(const uint32_t *)(p + 4 * i);
   }
 }
-__device__ inline void load_block(const uint8_t *p, int m, RawBlock &r) {
+__device__ __forceinline__ void load_block(const uint8_t *p, int m, RawBlock &r) {
   if (m == 4) load_block<4>(p, r);
   else if (m == 8) load_block<8>(p, r);
   else if (m == 6) load_block<6>(p, r);
@@ -119,7 +127,7 @@ constexpr int max_exp(int m) { return m == 3 ? 255 : m == 4 ? 247 : 253; }
 
 // Group j (eight values) of a block, in slot order: q * 2^(E - 127 - (m - 2)).
 template <int M>
-__device__ inline bf8 dequant8(const RawBlock &r, int j, int E) {
+__device__ __forceinline__ bf8 dequant8(const RawBlock &r, int j, int E) {
   if constexpr (M == 4) {
     // two's complement nibbles -> bytes of sign and magnitude 0..8, whose FP8
     // (e4m3) value is linear, k 2^-9; the conversion applies the block's scale
@@ -179,7 +187,7 @@ __device__ inline int swizzle(int t) { return 4 * (t & 3) + ((t >> 2) & 3); }
 
 // A token's block b to its LDS row.
 template <int M>
-__device__ inline void store_block(const RawBlock &r, int E, uint8_t *tile, int t, int b) {
+__device__ __forceinline__ void store_block(const RawBlock &r, int E, uint8_t *tile, int t, int b) {
   const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
   const bool big = __any(E > max_exp(M));
 #pragma unroll
@@ -192,7 +200,7 @@ __device__ inline void store_block(const RawBlock &r, int E, uint8_t *tile, int 
     *(bf8 *)(tile + t * kRowBytes + 16 * ((4 * b + j) ^ swizzle(t))) = v;
   }
 }
-__device__ inline void store_block(const RawBlock &r, int m, int E, uint8_t *tile, int t, int b) {
+__device__ __forceinline__ void store_block(const RawBlock &r, int m, int E, uint8_t *tile, int t, int b) {
   if (m == 4) store_block<4>(r, E, tile, t, b);
   else if (m == 8) store_block<8>(r, E, tile, t, b);
   else if (m == 6) store_block<6>(r, E, tile, t, b);
@@ -251,16 +259,17 @@ __device__ inline int find_seq(const AttnPagedArgs &a, int64_t number, int rows,
   return lo;
 }
 
-// The steps (of 64 tokens) that rows at positions p_lo .. p_hi need: those of the
+// The steps (of TOK tokens) that rows at positions p_lo .. p_hi need: those of the
 // prefix, then those from the first window on.
 struct Steps {
   int pre, shift, count;                 // step v < pre is v, another v + shift
 };
+template <int TOK>
 __device__ inline Steps steps_of(const AttnPagedArgs &a, const Seq &q, int64_t p_lo, int64_t p_hi) {
   Steps st;
-  const int hi = (int)((min((int64_t)q.len, max(p_hi + 1, (int64_t)0)) + kTok - 1) / kTok);
-  const int lo = a.window ? (int)(max(p_lo - a.window + 1, (int64_t)0) / kTok) : 0;
-  st.pre = (q.pre + kTok - 1) / kTok;
+  const int hi = (int)((min((int64_t)q.len, max(p_hi + 1, (int64_t)0)) + TOK - 1) / TOK);
+  const int lo = a.window ? (int)(max(p_lo - a.window + 1, (int64_t)0) / TOK) : 0;
+  st.pre = (q.pre + TOK - 1) / TOK;
   if (st.pre >= lo) {
     st.count = max(hi, st.pre);
     st.pre = st.shift = 0;
@@ -271,13 +280,14 @@ __device__ inline Steps steps_of(const AttnPagedArgs &a, const Seq &q, int64_t p
   return st;
 }
 
-// Partial results of the splits: (maximum, sum) [splits][T Hq], then the unscaled
-// outputs [splits][T Hq][128].
+// Partial results of the splits: (maximum, sum) [parts][T Hq], then the unscaled
+// outputs [parts][T Hq][128], `parts` being the larger number of splits of the two
+// kernels.
 __device__ inline float *part_ml(const AttnPagedArgs &a, int split, int64_t row) {
   return a.work + (split * a.T * a.Hq + row) * 2;
 }
-__device__ inline float *part_o(const AttnPagedArgs &a, int splits, int split, int64_t row) {
-  return a.work + splits * a.T * a.Hq * 2 + (split * a.T * a.Hq + row) * kD;
+__device__ inline float *part_o(const AttnPagedArgs &a, int split, int64_t row) {
+  return a.work + a.parts * a.T * a.Hq * 2 + (split * a.T * a.Hq + row) * kD;
 }
 
 template <bool F32>
@@ -290,7 +300,7 @@ __device__ inline float capped(float x, float cap) {
 
 template <bool F32>
 __global__ __launch_bounds__(64 * kWaves, 2)
-void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers) {
+void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];   // [buffer][K, V]
   const PageGeo &g = a.geo;
   const int t = threadIdx.x, lane = t & 63, h = lane >> 5, x = lane & 31;
@@ -307,9 +317,9 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers) {
   if (s < 0) return;
   const Seq q = seq_at(a, s);
   const int64_t rows = (int64_t)q.n * G, r0 = (int64_t)tile * kRows;
-  if (r0 >= rows) return;
+  if (r0 >= rows || (few && rows <= kFewRows)) return;
   const int64_t p0 = (int64_t)q.len - q.n;                 // the first row's position
-  const Steps st = steps_of(a, q, p0 + r0 / G, p0 + (min(r0 + kRows, rows) - 1) / G);
+  const Steps st = steps_of<kTok>(a, q, p0 + r0 / G, p0 + (min(r0 + kRows, rows) - 1) / G);
   const int v0 = (int)((int64_t)st.count * split / splits);
   const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
 
@@ -502,7 +512,7 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers) {
     if (h == 0) *(f2 *)part_ml(a, split, row) = f2{m, l};
     if (v0 >= v1) return;
   }
-  float *of = whole ? (float *)a.o + row * kD : part_o(a, splits, split, row);
+  float *of = whole ? (float *)a.o + row * kD : part_o(a, split, row);
   uint16_t *ob = (uint16_t *)a.o + row * kD;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -522,15 +532,324 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// Few rows.
+
+constexpr int kChunk = 32;               // tokens of a wave's step
+constexpr int kFewWaves = 4;
+// LDS rows of a wave's 32 dequantized V tokens: chunk c (16 bytes) of token t at c ^
+// swizzle: eight tokens' writes of one chunk, and a transposing read's eight tokens
+// of two adjacent chunks, lie in distinct banks.
+constexpr int kFewBytes = kChunk * kRowBytes;
+__device__ inline int few_swizzle(int t) { return 2 * (t & 7) + ((t >> 3) & 1); }
+
+// The words that hold group g of a packed block of width m.
+struct RawGroup {
+  uint32_t w[2];
+};
+template <int M>
+__device__ __forceinline__ void load_group(const uint8_t *p, int g, RawGroup &r) {
+  if constexpr (M == 4) {
+    r.w[0] = *(const uint32_t *)(p + 4 * g);
+  } else if constexpr (M == 6) {
+    r.w[0] = *(const uint32_t *)(p + 4 * g);
+    r.w[1] = *(const uint32_t *)(p + 16 + 4 * (g >> 1));
+  } else if constexpr (M == 8) {
+    const u2 a = *(const u2 *)(p + 8 * g);
+    r.w[0] = a[0];
+    r.w[1] = a[1];
+  } else {                               // bytes 3 g .. 3 g + 2 of twelve
+    const int at = (3 * g) & ~3;
+    r.w[0] = *(const uint32_t *)(p + at);
+    r.w[1] = *(const uint32_t *)(p + (at < 8 ? at + 4 : 8));
+  }
+}
+__device__ __forceinline__ void load_group(const uint8_t *p, int m, int g, RawGroup &r) {
+  if (m == 4) load_group<4>(p, g, r);
+  else if (m == 8) load_group<8>(p, g, r);
+  else if (m == 6) load_group<6>(p, g, r);
+  else load_group<3>(p, g, r);
+}
+
+template <int M>
+__device__ __forceinline__ bf8 dequant_group(const RawGroup &r, int g, int E, bool big) {
+  RawBlock b;                            // as group 0 of a block
+  if constexpr (M == 6) {
+    b.w[0] = r.w[0];
+    b.w[4] = r.w[1] << (4 * (g & 1));
+  } else if constexpr (M == 3) {
+    b.w[0] = __builtin_amdgcn_alignbit(r.w[1], r.w[0], 8 * ((3 * g) & 3));
+  } else {
+    b.w[0] = r.w[0];
+    if constexpr (M == 8) b.w[1] = r.w[1];
+  }
+  bf8 v = dequant8<M>(b, 0, E);
+  if (big) {
+    const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
+  }
+  return v;
+}
+__device__ __forceinline__ bf8 dequant_group(const RawGroup &r, int m, int g, int E, bool big) {
+  if (m == 4) return dequant_group<4>(r, g, E, big);
+  if (m == 8) return dequant_group<8>(r, g, E, big);
+  if (m == 6) return dequant_group<6>(r, g, E, big);
+  return dequant_group<3>(r, g, E, big);
+}
+
+// Whether one of four exponents may pass max_exp.
+__device__ inline bool has_big(uint32_t ex) {
+  return (ex & (ex << 1) & (ex << 2) & 0x80808080u) != 0;
+}
+
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// ALL4: every block has 4 bits.
+template <bool F32, bool ALL4>
+__global__ __launch_bounds__(64 * kFewWaves, 3)
+void attn_few_kernel(AttnPagedArgs a, int splits) {
+  __shared__ __attribute__((aligned(16))) uint8_t pool[kFewWaves][kFewBytes];
+  __shared__ float mm[kFewWaves][kFewRows], ml[kFewWaves][kFewRows];
+  const PageGeo &g = a.geo;
+  const int t = threadIdx.x, lane = t & 63, gr = lane >> 4, n = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const uint32_t Hkv = (uint32_t)g.Hkv;
+  const int G = a.G;
+  const uint32_t rest = blockIdx.x / Hkv;
+  const int kvh = (int)(blockIdx.x - rest * Hkv);
+  const int s = (int)(rest / (uint32_t)splits), split = (int)(rest - (uint32_t)s * (uint32_t)splits);
+  const Seq q = seq_at(a, s);
+  const int64_t rows = (int64_t)q.n * G;
+  if (rows == 0 || rows > kFewRows) return;
+  const int p0 = q.len - q.n;                              // the first row's position
+  const Steps st = steps_of<kChunk>(a, q, p0, (int64_t)q.len - 1);
+  const int v0 = (int)((int64_t)st.count * split / splits);
+  const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
+
+  // this lane's query row (columns past the last repeat it)
+  const int r = min(n, (int)rows - 1), tok = r / G, hd = kvh * G + r - tok * G, p = p0 + tok;
+  const int window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
+  auto width = [&](int j) { return ALL4 ? 4 : g.m[j]; };
+  // product j of a score: block j, lane group gr its values 8 gr .., in slot order
+  bf8 qop[4];
+  {
+    const uint16_t *src = a.q + (int64_t)(q.row0 + tok) * a.q_ts + hd * a.q_hs;
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u4 w = *(const u4 *)(src + 32 * j + 8 * gr);
+      w = a.scale == 0.f ? u4{0u, 0u, 0u, 0u} : w ^ u4{sign, sign, sign, sign};
+      if (split_slots(width(j)))
+        w = u4{__builtin_amdgcn_perm(w[1], w[0], 0x05040100), __builtin_amdgcn_perm(w[3], w[2], 0x05040100),
+               __builtin_amdgcn_perm(w[1], w[0], 0x07060302), __builtin_amdgcn_perm(w[3], w[2], 0x07060302)};
+      qop[j] = __builtin_bit_cast(bf8, w);
+    }
+  }
+  const float sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
+  const float slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;
+  const float ninf = -__builtin_inff();
+  float m = ninf, ref = 0.f, l = 0.f;
+  f4 o[8];                                                 // row n, slots 16 dt + 4 gr ..
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) o[dt] = f4{0.f, 0.f, 0.f, 0.f};
+
+  // A chunk's halves of 16 tokens lie in one page each.  Tokens past the last are
+  // the last one (weight 0), a half past the last the chunk's first.
+  const int32_t *pages = a.table + (int64_t)s * a.ld_table;
+  const int page_mask = (1 << g.lg_page) - 1, last = q.len - 1;
+  RawGroup rk[2][4], rv[2][4];
+  uint32_t ek[2], ev[2];
+  auto first_of = [&](int v) { return (v < st.pre ? v : v + st.shift) * kChunk; };
+  auto fetch = [&](int v) __attribute__((always_inline)) {
+    const int t0 = first_of(v);
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      const int th = t0 + 16 * mt <= last ? t0 + 16 * mt : t0;
+      const int page = pages[th >> g.lg_page];
+      const bool hole = page < 0 || page >= g.pages;
+      const int64_t run = ((int64_t)(hole ? 0 : page) * Hkv + kvh) << g.lg_page;
+      const int i = min(th + n, last) & page_mask;
+      const uint8_t *kp = a.k_mant + run * g.row, *vp = a.v_mant + run * g.row;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int w = width(j);
+        const uint32_t at = (uint32_t)((g.off[j] << g.lg_page) + i * 4 * w);
+        load_group(kp + at, w, gr, rk[mt][j]);
+        load_group(vp + at, w, gr, rv[mt][j]);
+      }
+      ek[mt] = *(const uint32_t *)(a.k_exp + (run + i) * 4);
+      ev[mt] = *(const uint32_t *)(a.v_exp + (run + i) * 4);
+      if (hole) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rk[mt][j].w[0] = rk[mt][j].w[1] = rv[mt][j].w[0] = rv[mt][j].w[1] = 0u;
+        ek[mt] = ev[mt] = 0u;
+      }
+    }
+  };
+  uint8_t *vs = pool[wave];
+  if (v0 + wave < v1) fetch(v0 + wave);
+  for (int v = v0 + wave; v < v1; v += kFewWaves) {
+    const int t0 = first_of(v);
+    const bool big = __any(has_big(ek[0]) || has_big(ek[1]) || has_big(ev[0]) || has_big(ev[1]));
+    // scores: tokens 16 mt + 4 gr + i of row n
+    f4 sa[2];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      sa[mt] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf8 k = dequant_group(rk[mt][j], width(j), gr, (int)((ek[mt] >> (8 * j)) & 255u), big);
+        sa[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[j], sa[mt], 0, 0, 0);
+      }
+    }
+    wave_sync();                                           // the last chunk's V rows are consumed
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(bf8 *)(vs + (16 * mt + n) * kRowBytes + 16 * ((4 * j + gr) ^ few_swizzle(n))) =
+            dequant_group(rv[mt][j], width(j), gr, (int)((ev[mt] >> (8 * j)) & 255u), big);
+    if (v + kFewWaves < v1) fetch(v + kFewWaves);
+    wave_sync();
+    float scale = sc;
+    if (a.softcap > 0.f || a.slopes) {
+      const float rel = (float)(p - t0 - 4 * gr);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float y = sa[mt][i] * sc;
+          if (a.softcap > 0.f) y = capped<F32>(y, a.softcap) * kUnit<F32>;
+          sa[mt][i] = fmaf(-slope, fabsf(rel - (float)(16 * mt + i)), y);
+        }
+      scale = 1.f;
+    }
+    if (t0 + kChunk - 1 > p0 || (q.len - 1) - t0 >= window || t0 + kChunk > q.len) {
+      const int rel = p - t0 - 4 * gr, pre = q.pre - t0 - 4 * gr, end = q.len - t0 - 4 * gr;
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = 16 * mt + i;
+          const bool see = ((k <= rel && rel - k < window) || k < pre) && k < end;
+          if (!see) sa[mt][i] = ninf;
+        }
+    }
+    float top = fmaxf(fmaxf(fmaxf(sa[0][0], sa[0][1]), fmaxf(sa[0][2], sa[0][3])),
+                      fmaxf(fmaxf(sa[1][0], sa[1][1]), fmaxf(sa[1][2], sa[1][3])));
+    top = top == ninf ? ninf : top * scale;
+    if (__any(top > m + kSlack<F32> || (m == ninf && top != ninf))) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float nm = fmaxf(m, top);
+      const float alpha = m == ninf ? 0.f : weight<F32>(m - nm);
+      m = nm;
+      ref = nm == ninf ? 0.f : nm;                         // scores of -inf weigh 0
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
+    }
+    float e[8];                                            // the product's slots: tokens 4 gr + i, 16 + 4 gr + i
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e[i] = weight<F32>(fmaf(sa[i >> 2][i & 3], scale, -ref));
+      l += e[i];
+    }
+    constexpr int kTerms = F32 ? 3 : 1;
+    bf8 pt[kTerms];
+#pragma unroll
+    for (int k = 0; k < kTerms; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        pt[k][i] = (__bf16)e[i];
+        if constexpr (F32) e[i] -= (float)pt[k][i];
+      }
+    const uint8_t *vp = vs + (4 * gr + (n >> 2)) * kRowBytes + 8 * (n & 1);
+    const int sw = few_swizzle(4 * gr + (n >> 2)), col = (n & 3) >> 1;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      const uint8_t *at = vp + 16 * ((2 * dt + col) ^ sw);
+      const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at);
+      const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(at + 16 * kRowBytes));
+      const bf8 vv = __builtin_bit_cast(bf8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int k = 0; k < kTerms; ++k)
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pt[k], o[dt], 0, 0, 0);
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  // Merge the waves in order: each writes its outputs, weighted against the row's
+  // largest reference, over its V rows.
+  if (gr == 0) {
+    mm[wave][n] = m;
+    ml[wave][n] = l;
+  }
+  __syncthreads();
+  float M = ninf;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, mm[w][n]);
+  const float f = m == ninf ? 0.f : weight<F32>(m - M);
+  float *mo = (float *)vs;                                 // [row][d]
+#pragma unroll
+  for (int dt = 0; dt < 8; ++dt) {
+    const int d8 = 16 * dt + 8 * (gr >> 1);
+    const bool sp = split_slots(width(dt >> 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)                            // (0 without a finite score; a NaN stays)
+      mo[n * kD + d8 + (sp ? 2 * i + (gr & 1) : 4 * (gr & 1) + i)] = o[dt][i] * f;
+  }
+  __syncthreads();
+  for (int i = t; i < (int)rows * (kD / 4); i += 64 * kFewWaves) {
+    const int row = i / (kD / 4), d = 4 * (i % (kD / 4));
+    float M2 = ninf, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) M2 = fmaxf(M2, mm[w][row]);
+    f4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      L += mm[w][row] == ninf ? ml[w][row] : ml[w][row] * weight<F32>(mm[w][row] - M2);
+      O += *(const f4 *)((float *)pool[w] + row * kD + d);
+    }
+    const int tk = row / G;
+    const int64_t at = (int64_t)(q.row0 + tk) * a.Hq + kvh * G + row - tk * G;
+    if (splits > 1) {
+      if (d == 0) *(f2 *)part_ml(a, split, at) = f2{M2, L};
+      *(f4 *)(part_o(a, split, at) + d) = O;
+    } else {
+      O *= L == 0.f ? 0.f : 1.f / L;
+      if (F32) *(f4 *)((float *)a.o + at * kD + d) = O;
+      else *(bf4 *)((uint16_t *)a.o + at * kD + d) =
+          bf4{(__bf16)O[0], (__bf16)O[1], (__bf16)O[2], (__bf16)O[3]};
+    }
+  }
+}
+
 // o[row] = the splits' partial results merged, in the order of the splits: half a
 // wave per row.
 template <bool F32>
-__global__ __launch_bounds__(256) void attn_merge_kernel(AttnPagedArgs a, int splits) {
+__global__ __launch_bounds__(256) void attn_merge_kernel(AttnPagedArgs a, int tile, int few) {
   const int t = threadIdx.x, c = t & 31;
   const int64_t row = (int64_t)blockIdx.x * 8 + (t >> 5);
   if (row >= a.T * a.Hq) return;
   const int tok = (int)(row / a.Hq);
   if (tok < a.cu_q[0] || tok >= a.cu_q[a.S]) return;       // no sequence's row
+  int splits = tile;
+  if (tile != few) {                                       // which kernel had the row
+    int lo = 0, hi = (int)a.S - 1;                         // the last sequence that begins at tok or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (a.cu_q[mid] <= tok) lo = mid;
+      else hi = mid - 1;
+    }
+    if ((int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G <= kFewRows) splits = few;
+    if (splits == 1) return;                               // written already
+  }
   const float ninf = -__builtin_inff();
   float M = ninf;
   for (int s = c; s < splits; s += 32) M = fmaxf(M, part_ml(a, s, row)[0]);
@@ -546,7 +865,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnPagedArgs a, int sp
     if (ml[0] == ninf && ml[1] == 0.f) continue;
     const float f = weight<F32>(ml[0] - ref);
     L += ml[1] * f;
-    O += *(const f4 *)(part_o(a, splits, s, row) + 4 * c) * f;
+    O += *(const f4 *)(part_o(a, s, row) + 4 * c) * f;
   }
   O *= L == 0.f ? 0.f : 1.f / L;
   if (F32) *(f4 *)((float *)a.o + row * kD + 4 * c) = O;
@@ -556,31 +875,58 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnPagedArgs a, int sp
 
 int64_t tile_numbers(const AttnPagedArgs &a) { return a.T * a.G / kRows + a.S; }
 
-// About four workgroups per CU, none with fewer than four steps of its longest tile.
-int tile_splits(const AttnPagedArgs &a) {
-  const int64_t wgs = std::max<int64_t>(tile_numbers(a) * a.geo.Hkv, 1);
-  const int64_t steps = (a.max_kv + kTok - 1) / kTok;
-  int64_t n = std::min<int64_t>(1024 / wgs, steps / 4);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
+// Splits of each kernel, 0 where it is not launched.
+struct Plan {
+  int tile, few;
+};
+Plan plan_of(const AttnPagedArgs &a) {
+  Plan p = {0, 0};
+  const int64_t Hkv = a.geo.Hkv;
+  auto split = [](int64_t wgs, int64_t want, int64_t steps, int64_t least) {
+    const int64_t n = std::min(want / std::max<int64_t>(wgs, 1), steps / least);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
+  };
+  // every sequence has max_q rows where their sum says so
+  if (a.max_q * a.G > kFewRows)
+    p.tile = split(tile_numbers(a) * Hkv, 1024, (a.max_kv + kTok - 1) / kTok, 4);
+  if (a.max_q * a.G <= kFewRows || (a.G <= kFewRows && a.T < a.S * a.max_q))
+    p.few = split(a.S * Hkv, 1024, (a.max_kv + kChunk - 1) / kChunk, kFewWaves);
+  return p;
 }
 
 }  // namespace
 
 int64_t attn_paged_work(const AttnPagedArgs &a) {
-  const int splits = tile_splits(a);
-  return splits == 1 ? 0 : splits * a.T * a.Hq * (kD + 2) * (int64_t)sizeof(float);
+  const Plan p = plan_of(a);
+  const int n = std::max(p.tile, p.few);
+  return n <= 1 ? 0 : n * a.T * a.Hq * (kD + 2) * (int64_t)sizeof(float);
 }
 
-hipError_t launch_attn_paged(const AttnPagedArgs &a, hipStream_t s) {
-  const int splits = tile_splits(a);
-  const int64_t numbers = tile_numbers(a), wgs = numbers * a.geo.Hkv * splits;
-  if (wgs >= ((int64_t)1 << 32) / (64 * kWaves)) return hipErrorInvalidValue;
-  const auto tile = a.o_f32 ? attn_tile_kernel<true> : attn_tile_kernel<false>;
-  hipLaunchKernelGGL(tile, dim3((unsigned)wgs), dim3(64 * kWaves), 0, s, a, splits, numbers);
+hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
+  AttnPagedArgs a = args;
+  const Plan p = plan_of(a);
+  a.parts = std::max(p.tile, p.few);
+  const int64_t numbers = tile_numbers(a);
+  const int64_t wgs = numbers * a.geo.Hkv * p.tile, few_wgs = a.S * a.geo.Hkv * p.few;
+  // (a dispatch holds fewer than 2^32 threads)
+  if (std::max(wgs, few_wgs) >= ((int64_t)1 << 32) / 256) return hipErrorInvalidValue;
+  if (p.few) {
+    const PageGeo &g = a.geo;
+    const bool all4 = g.m[0] == 4 && g.m[3] == 4;          // (widths do not decrease)
+    const auto fn = a.o_f32 ? (all4 ? attn_few_kernel<true, true> : attn_few_kernel<true, false>)
+                            : (all4 ? attn_few_kernel<false, true> : attn_few_kernel<false, false>);
+    hipLaunchKernelGGL(fn, dim3((unsigned)few_wgs), dim3(64 * kFewWaves), 0, s, a, p.few);
+  }
+  if (p.tile) {
+    const auto fn = a.o_f32 ? attn_tile_kernel<true> : attn_tile_kernel<false>;
+    hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(64 * kWaves), 0, s, a, p.tile, numbers,
+                       p.few ? 1 : 0);
+  }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
+  if (e != hipSuccess || a.parts <= 1) return e;
   const auto merge = a.o_f32 ? attn_merge_kernel<true> : attn_merge_kernel<false>;
-  hipLaunchKernelGGL(merge, dim3((unsigned)((a.T * a.Hq + 7) / 8)), dim3(256), 0, s, a, splits);
+  hipLaunchKernelGGL(merge, dim3((unsigned)((a.T * a.Hq + 7) / 8)), dim3(256), 0, s, a,
+                     p.tile ? p.tile : p.few, p.few ? p.few : p.tile);
   return hipGetLastError();
 }
 

@@ -198,6 +198,7 @@ struct AttnPagedArgs {
   int64_t S, T, Hq, max_q, max_kv, window;
   int G;
   float scale, softcap;
+  int parts;               // of the partial results (set by launch_attn_paged)
 };
 int64_t attn_paged_work(const AttnPagedArgs &args);
 hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s);

@@ -111,7 +111,7 @@ __device__ __forceinline__ void load_block(const uint8_t *p, int m, RawBlock &r)
 
 // Slot i of eight values holds element slot_elem(m, i): 4- and 6-bit blocks yield
 // the even elements, then the odd ones.
-__device__ inline bool split_slots(int m) { return m == 4 || m == 6; }
+__device__ constexpr bool split_slots(int m) { return m == 4 || m == 6; }
 
 // (a & m) | (b & ~m) for m = 0x0F0F0F0F; the mask is opaque to the compiler, which
 // would split a constant one into two instructions.
@@ -185,20 +185,29 @@ constexpr int kRowBytes = 2 * kD;
 constexpr int kTileBytes = kTok * kRowBytes;
 __device__ inline int swizzle(int t) { return 4 * (t & 3) + ((t >> 2) & 3); }
 
+// The rest of the scale of blocks beyond max_exp.  (E = 255 is no exception: the
+// quantizer writes zero mantissas with it.)
+template <int M>
+__device__ __forceinline__ void big_scale(bf8 &v, int E) {
+  if constexpr (M == 3) return;
+  const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
+}
+
 // A token's block b to its LDS row.
 template <int M>
 __device__ __forceinline__ void store_block(const RawBlock &r, int E, uint8_t *tile, int t, int b) {
-  const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
-  const bool big = __any(E > max_exp(M));
+  bf8 v[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    bf8 v = dequant8<M>(r, j, E);
-    if (big) {
+  for (int j = 0; j < 4; ++j) v[j] = dequant8<M>(r, j, E);
+  if (__any(E > max_exp(M))) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
-    }
-    *(bf8 *)(tile + t * kRowBytes + 16 * ((4 * b + j) ^ swizzle(t))) = v;
+    for (int j = 0; j < 4; ++j) big_scale<M>(v[j], E);
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *(bf8 *)(tile + t * kRowBytes + 16 * ((4 * b + j) ^ swizzle(t))) = v[j];
 }
 __device__ __forceinline__ void store_block(const RawBlock &r, int m, int E, uint8_t *tile, int t, int b) {
   if (m == 4) store_block<4>(r, E, tile, t, b);
@@ -543,59 +552,110 @@ constexpr int kFewWaves = 4;
 constexpr int kFewBytes = kChunk * kRowBytes;
 __device__ inline int few_swizzle(int t) { return 2 * (t & 7) + ((t >> 3) & 1); }
 
-// The words that hold group g of a packed block of width m.
-struct RawGroup {
-  uint32_t w[2];
+// The widths of a row's blocks: N3 3-bit, N4 4-bit, N6 6-bit and N8 8-bit blocks, in
+// that order.  Rows of one width are read a block per lane (lane group g: block g,
+// product j: its group j), others a group of each block (product j: block j, lane
+// group g: its group g), so that all lanes run one width's code.
+template <int N3, int N4, int N6, int N8>
+struct Mix {
+  static constexpr bool kUniform = N3 == 4 || N4 == 4 || N6 == 4 || N8 == 4;
+  static constexpr int width(int b) {
+    return b < N3 ? 3 : b < N3 + N4 ? 4 : b < N3 + N4 + N6 ? 6 : 8;
+  }
+  static constexpr int off(int b) { return b == 0 ? 0 : off(b - 1) + 4 * width(b - 1); }
+  // words of product j that a lane loads, and where they begin
+  static constexpr int words(int j) {
+    return kUniform ? (j == 0 ? width(0) : 0) : width(j) == 4 ? 1 : 2;
+  }
+  static constexpr int start(int j) { return j == 0 ? 0 : start(j - 1) + words(j - 1); }
+  static constexpr int kWords = start(4);
+  // first value of the eight of (lane group g, product j)
+  static constexpr __device__ int value(int g, int j) { return kUniform ? 32 * g + 8 * j : 32 * j + 8 * g; }
 };
-template <int M>
-__device__ __forceinline__ void load_group(const uint8_t *p, int g, RawGroup &r) {
+
+// A lane's share of a token's row: its packed words and the four exponents.
+template <class Mx>
+struct RawRow {
+  uint32_t w[Mx::kWords];
+  uint32_t ex;
+};
+
+// `plane` points at the page's first token, `i` is the token.
+template <class Mx, int J>
+__device__ __forceinline__ void load_group(const uint8_t *page, int lg_page, uint32_t i, int g,
+                                           RawRow<Mx> &r) {
+  constexpr int M = Mx::width(J), S = Mx::start(J);
+  const uint8_t *p = page + (((uint32_t)Mx::off(J) << lg_page) + i * (4 * M));
   if constexpr (M == 4) {
-    r.w[0] = *(const uint32_t *)(p + 4 * g);
+    r.w[S] = *(const uint32_t *)(p + 4 * g);
   } else if constexpr (M == 6) {
-    r.w[0] = *(const uint32_t *)(p + 4 * g);
-    r.w[1] = *(const uint32_t *)(p + 16 + 4 * (g >> 1));
+    r.w[S] = *(const uint32_t *)(p + 4 * g);
+    r.w[S + 1] = *(const uint32_t *)(p + 16 + 4 * (g >> 1));
   } else if constexpr (M == 8) {
     const u2 a = *(const u2 *)(p + 8 * g);
-    r.w[0] = a[0];
-    r.w[1] = a[1];
+    r.w[S] = a[0];
+    r.w[S + 1] = a[1];
   } else {                               // bytes 3 g .. 3 g + 2 of twelve
     const int at = (3 * g) & ~3;
-    r.w[0] = *(const uint32_t *)(p + at);
-    r.w[1] = *(const uint32_t *)(p + (at < 8 ? at + 4 : 8));
+    r.w[S] = *(const uint32_t *)(p + at);
+    r.w[S + 1] = *(const uint32_t *)(p + (at < 8 ? at + 4 : 8));
   }
 }
-__device__ __forceinline__ void load_group(const uint8_t *p, int m, int g, RawGroup &r) {
-  if (m == 4) load_group<4>(p, g, r);
-  else if (m == 8) load_group<8>(p, g, r);
-  else if (m == 6) load_group<6>(p, g, r);
-  else load_group<3>(p, g, r);
+template <class Mx>
+__device__ __forceinline__ void load_row(const uint8_t *page, int lg_page, uint32_t i, int g,
+                                         RawRow<Mx> &r) {
+  if constexpr (Mx::kUniform) {
+    constexpr int M = Mx::width(0);
+    RawBlock b;
+    load_block<M>(page + ((((uint32_t)(4 * M * g)) << lg_page) + i * (4 * M)), b);
+#pragma unroll
+    for (int k = 0; k < M; ++k) r.w[k] = b.w[k];
+  } else {
+    load_group<Mx, 0>(page, lg_page, i, g, r);
+    load_group<Mx, 1>(page, lg_page, i, g, r);
+    load_group<Mx, 2>(page, lg_page, i, g, r);
+    load_group<Mx, 3>(page, lg_page, i, g, r);
+  }
 }
 
-template <int M>
-__device__ __forceinline__ bf8 dequant_group(const RawGroup &r, int g, int E, bool big) {
-  RawBlock b;                            // as group 0 of a block
-  if constexpr (M == 6) {
-    b.w[0] = r.w[0];
-    b.w[4] = r.w[1] << (4 * (g & 1));
-  } else if constexpr (M == 3) {
-    b.w[0] = __builtin_amdgcn_alignbit(r.w[1], r.w[0], 8 * ((3 * g) & 3));
-  } else {
-    b.w[0] = r.w[0];
-    if constexpr (M == 8) b.w[1] = r.w[1];
-  }
-  bf8 v = dequant8<M>(b, 0, E);
-  if (big) {
-    const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
+// Product J's eight values, in slot order.
+template <class Mx, int J>
+__device__ __forceinline__ bf8 dequant_group(const RawRow<Mx> &r, int g) {
+  constexpr int M = Mx::width(J), S = Mx::start(J);
+  const int E = (int)__builtin_amdgcn_ubfe(r.ex, Mx::kUniform ? 8 * g : 8 * J, 8);
+  RawBlock b;
+  bf8 v;
+  if constexpr (Mx::kUniform) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
+    for (int k = 0; k < M; ++k) b.w[k] = r.w[k];
+    v = dequant8<M>(b, J, E);
+  } else {                               // as group 0 of a block
+    if constexpr (M == 6) {
+      b.w[0] = r.w[S];
+      b.w[4] = r.w[S + 1] << (4 * (g & 1));
+    } else if constexpr (M == 3) {
+      b.w[0] = __builtin_amdgcn_alignbit(r.w[S + 1], r.w[S], 8 * ((3 * g) & 3));
+    } else {
+      b.w[0] = r.w[S];
+      if constexpr (M == 8) b.w[1] = r.w[S + 1];
+    }
+    v = dequant8<M>(b, 0, E);
   }
   return v;
 }
-__device__ __forceinline__ bf8 dequant_group(const RawGroup &r, int m, int g, int E, bool big) {
-  if (m == 4) return dequant_group<4>(r, g, E, big);
-  if (m == 8) return dequant_group<8>(r, g, E, big);
-  if (m == 6) return dequant_group<6>(r, g, E, big);
-  return dequant_group<3>(r, g, E, big);
+template <class Mx>
+__device__ __forceinline__ void dequant_row(const RawRow<Mx> &r, int g, bool big, bf8 (&v)[4]) {
+  v[0] = dequant_group<Mx, 0>(r, g);
+  v[1] = dequant_group<Mx, 1>(r, g);
+  v[2] = dequant_group<Mx, 2>(r, g);
+  v[3] = dequant_group<Mx, 3>(r, g);
+  if (big) {
+    auto E = [&](int j) { return (int)__builtin_amdgcn_ubfe(r.ex, Mx::kUniform ? 8 * g : 8 * j, 8); };
+    big_scale<Mx::width(0)>(v[0], E(0));
+    big_scale<Mx::width(1)>(v[1], E(1));
+    big_scale<Mx::width(2)>(v[2], E(2));
+    big_scale<Mx::width(3)>(v[3], E(3));
+  }
 }
 
 // Whether one of four exponents may pass max_exp.
@@ -609,8 +669,7 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// ALL4: every block has 4 bits.
-template <bool F32, bool ALL4>
+template <bool F32, class Mx>
 __global__ __launch_bounds__(64 * kFewWaves, 3)
 void attn_few_kernel(AttnPagedArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) uint8_t pool[kFewWaves][kFewBytes];
@@ -634,17 +693,16 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   // this lane's query row (columns past the last repeat it)
   const int r = min(n, (int)rows - 1), tok = r / G, hd = kvh * G + r - tok * G, p = p0 + tok;
   const int window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
-  auto width = [&](int j) { return ALL4 ? 4 : g.m[j]; };
-  // product j of a score: block j, lane group gr its values 8 gr .., in slot order
+  // product j of a score: the values of lane group gr, in slot order
   bf8 qop[4];
   {
     const uint16_t *src = a.q + (int64_t)(q.row0 + tok) * a.q_ts + hd * a.q_hs;
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u4 w = *(const u4 *)(src + 32 * j + 8 * gr);
+      u4 w = *(const u4 *)(src + Mx::value(gr, j));
       w = a.scale == 0.f ? u4{0u, 0u, 0u, 0u} : w ^ u4{sign, sign, sign, sign};
-      if (split_slots(width(j)))
+      if (split_slots(Mx::width(j)))
         w = u4{__builtin_amdgcn_perm(w[1], w[0], 0x05040100), __builtin_amdgcn_perm(w[3], w[2], 0x05040100),
                __builtin_amdgcn_perm(w[1], w[0], 0x07060302), __builtin_amdgcn_perm(w[3], w[2], 0x07060302)};
       qop[j] = __builtin_bit_cast(bf8, w);
@@ -662,8 +720,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   // the last one (weight 0), a half past the last the chunk's first.
   const int32_t *pages = a.table + (int64_t)s * a.ld_table;
   const int page_mask = (1 << g.lg_page) - 1, last = q.len - 1;
-  RawGroup rk[2][4], rv[2][4];
-  uint32_t ek[2], ev[2];
+  RawRow<Mx> rk[2], rv[2];
   auto first_of = [&](int v) { return (v < st.pre ? v : v + st.shift) * kChunk; };
   auto fetch = [&](int v) __attribute__((always_inline)) {
     const int t0 = first_of(v);
@@ -675,19 +732,14 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
       const int64_t run = ((int64_t)(hole ? 0 : page) * Hkv + kvh) << g.lg_page;
       const int i = min(th + n, last) & page_mask;
       const uint8_t *kp = a.k_mant + run * g.row, *vp = a.v_mant + run * g.row;
+      load_row<Mx>(kp, g.lg_page, (uint32_t)i, gr, rk[mt]);
+      load_row<Mx>(vp, g.lg_page, (uint32_t)i, gr, rv[mt]);
+      rk[mt].ex = *(const uint32_t *)(a.k_exp + (run + i) * 4);
+      rv[mt].ex = *(const uint32_t *)(a.v_exp + (run + i) * 4);
+      if (hole) {                                          // zero rows
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int w = width(j);
-        const uint32_t at = (uint32_t)((g.off[j] << g.lg_page) + i * 4 * w);
-        load_group(kp + at, w, gr, rk[mt][j]);
-        load_group(vp + at, w, gr, rv[mt][j]);
-      }
-      ek[mt] = *(const uint32_t *)(a.k_exp + (run + i) * 4);
-      ev[mt] = *(const uint32_t *)(a.v_exp + (run + i) * 4);
-      if (hole) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) rk[mt][j].w[0] = rk[mt][j].w[1] = rv[mt][j].w[0] = rv[mt][j].w[1] = 0u;
-        ek[mt] = ev[mt] = 0u;
+        for (int k = 0; k < Mx::kWords; ++k) rk[mt].w[k] = rv[mt].w[k] = 0u;
+        rk[mt].ex = rv[mt].ex = 0u;
       }
     }
   };
@@ -695,25 +747,27 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   if (v0 + wave < v1) fetch(v0 + wave);
   for (int v = v0 + wave; v < v1; v += kFewWaves) {
     const int t0 = first_of(v);
-    const bool big = __any(has_big(ek[0]) || has_big(ek[1]) || has_big(ev[0]) || has_big(ev[1]));
+    const bool big = __any(has_big(rk[0].ex) || has_big(rk[1].ex) || has_big(rv[0].ex) || has_big(rv[1].ex));
     // scores: tokens 16 mt + 4 gr + i of row n
     f4 sa[2];
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
+      bf8 k[4];
+      dequant_row(rk[mt], gr, big, k);
       sa[mt] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf8 k = dequant_group(rk[mt][j], width(j), gr, (int)((ek[mt] >> (8 * j)) & 255u), big);
-        sa[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[j], sa[mt], 0, 0, 0);
-      }
+      for (int j = 0; j < 4; ++j)
+        sa[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], qop[j], sa[mt], 0, 0, 0);
     }
     wave_sync();                                           // the last chunk's V rows are consumed
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < 2; ++mt) {
+      bf8 w[4];
+      dequant_row(rv[mt], gr, big, w);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *(bf8 *)(vs + (16 * mt + n) * kRowBytes + 16 * ((4 * j + gr) ^ few_swizzle(n))) =
-            dequant_group(rv[mt][j], width(j), gr, (int)((ev[mt] >> (8 * j)) & 255u), big);
+        *(bf8 *)(vs + (16 * mt + n) * kRowBytes + 16 * ((Mx::value(gr, j) >> 3) ^ few_swizzle(n))) = w[j];
+    }
     if (v + kFewWaves < v1) fetch(v + kFewWaves);
     wave_sync();
     float scale = sc;
@@ -799,7 +853,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
 #pragma unroll
   for (int dt = 0; dt < 8; ++dt) {
     const int d8 = 16 * dt + 8 * (gr >> 1);
-    const bool sp = split_slots(width(dt >> 1));
+    const bool sp = split_slots(Mx::width(dt >> 1));
 #pragma unroll
     for (int i = 0; i < 4; ++i)                            // (0 without a finite score; a NaN stays)
       mo[n * kD + d8 + (sp ? 2 * i + (gr & 1) : 4 * (gr & 1) + i)] = o[dt][i] * f;
@@ -873,6 +927,26 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnPagedArgs a, int ti
       bf4{(__bf16)O[0], (__bf16)O[1], (__bf16)O[2], (__bf16)O[3]};
 }
 
+// The kernel for a row's widths, code = 125 n3 + 25 n4 + 5 n6 + n8 (the 35 mixes of
+// four blocks).
+template <int C>
+bool dispatch_few(int code, const AttnPagedArgs &a, int splits, unsigned wgs, hipStream_t s) {
+  constexpr int n3 = C / 125, n4 = C / 25 % 5, n6 = C / 5 % 5, n8 = C % 5;
+  if constexpr (n3 + n4 + n6 + n8 == 4) {
+    if (code == C) {
+      using Mx = Mix<n3, n4, n6, n8>;
+      const auto fn = a.o_f32 ? attn_few_kernel<true, Mx> : attn_few_kernel<false, Mx>;
+      hipLaunchKernelGGL(fn, dim3(wgs), dim3(64 * kFewWaves), 0, s, a, splits);
+      return true;
+    }
+  }
+  if constexpr (C > 0) {
+    return dispatch_few<C - 1>(code, a, splits, wgs, s);
+  } else {
+    return false;
+  }
+}
+
 int64_t tile_numbers(const AttnPagedArgs &a) { return a.T * a.G / kRows + a.S; }
 
 // Splits of each kernel, 0 where it is not launched.
@@ -911,11 +985,10 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   // (a dispatch holds fewer than 2^32 threads)
   if (std::max(wgs, few_wgs) >= ((int64_t)1 << 32) / 256) return hipErrorInvalidValue;
   if (p.few) {
-    const PageGeo &g = a.geo;
-    const bool all4 = g.m[0] == 4 && g.m[3] == 4;          // (widths do not decrease)
-    const auto fn = a.o_f32 ? (all4 ? attn_few_kernel<true, true> : attn_few_kernel<true, false>)
-                            : (all4 ? attn_few_kernel<false, true> : attn_few_kernel<false, false>);
-    hipLaunchKernelGGL(fn, dim3((unsigned)few_wgs), dim3(64 * kFewWaves), 0, s, a, p.few);
+    int n[9] = {};
+    for (int b = 0; b < 4; ++b) ++n[a.geo.m[b]];
+    if (!dispatch_few<500>(125 * n[3] + 25 * n[4] + 5 * n[6] + n[8], a, p.few, (unsigned)few_wgs, s))
+      return hipErrorInvalidValue;
   }
   if (p.tile) {
     const auto fn = a.o_f32 ? attn_tile_kernel<true> : attn_tile_kernel<false>;

@@ -202,5 +202,8 @@ struct AttnPagedArgs {
 };
 int64_t attn_paged_work(const AttnPagedArgs &args);
 hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s);
+// The kernel for few rows (attn_few_*.hip), `groups` of 16 query rows.
+hipError_t launch_attn_few_bf16(const AttnPagedArgs &args, int splits, int groups, hipStream_t s);
+hipError_t launch_attn_few_f32(const AttnPagedArgs &args, int splits, int groups, hipStream_t s);
 
 }  // namespace mxq

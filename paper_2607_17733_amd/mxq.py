@@ -628,35 +628,37 @@ def attn_decode_static(q, k_cache, v_cache, fmt: Format, B: int, Hq: int, Hkv: i
 # Rotary positions, the paged KV cache, and attention over it
 
 def _current(dev, what: str):
-    """The calls run on the current device's current stream."""
-    if dev.index != torch.cuda.current_device():
+    """The calls run on the current device's current stream: its handle."""
+    i = torch._C._cuda_getDevice()
+    if dev.index != i:
         raise MxqError("%s is on %s, which is not the current device" % (what, dev))
-    return dev
+    return torch._C._cuda_getCurrentRawStream(i)
 
 
 def _heads(t, what: str, dev=None, heads=None, D=None):
-    """bf16 rows [tokens, heads, D] with unit stride along D."""
+    """bf16 rows [tokens, heads, D] with unit stride along D: their shape."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16
             and t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1)):
         raise MxqError("%s must be a 3-D bf16 device tensor [tokens, heads, D] with unit "
                        "stride along D" % what)
     if dev is not None and t.device != dev:
         raise MxqError("%s is on %s, not %s" % (what, t.device, dev))
-    if (heads is not None and t.shape[1] != heads) or (D is not None and t.shape[2] != D):
-        raise MxqError("%s is %s, not [tokens, %s, %s]" % (what, tuple(t.shape), heads, D))
-    return t
+    s = t.shape
+    if (heads is not None and s[1] != heads) or (D is not None and s[2] != D):
+        raise MxqError("%s is %s, not [tokens, %s, %s]" % (what, tuple(s), heads, D))
+    return s
 
 
 def _index(t, n: int, dtype, what: str, dev):
-    """A contiguous 1-D integer device tensor of n elements."""
+    """A contiguous 1-D integer device tensor of n elements: its address."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 1
             and t.is_contiguous()):
         raise MxqError("%s must be a contiguous 1-D %s device tensor" % (what, dtype))
-    if t.shape[0] != n:
-        raise MxqError("%s holds %d elements, not %d" % (what, t.shape[0], n))
+    if t.numel() != n:
+        raise MxqError("%s holds %d elements, not %d" % (what, t.numel(), n))
     if t.device != dev:
         raise MxqError("%s is on %s, not %s" % (what, t.device, dev))
-    return t
+    return t.data_ptr()
 
 
 def rope_inv_freq(rot: int, base: float = 10000.0, scaling: str | None = None,
@@ -721,20 +723,23 @@ def rope_table(inv_freq, positions: int, mscale: float = 1.0, device="cuda", out
     if out is None:
         out = torch.empty((positions, f.size, 2), dtype=torch.float32, device=device)
     _dev_array(out, positions * f.size * 2, torch.float32, "table", out.device)
-    _current(out.device, "table")
     _check(lib().mxq_rope_table(f.ctypes.data_as(ctypes.c_void_p), 2 * f.size, positions,
-                                float(mscale), _ptr(out), _stream()), "mxq_rope_table")
+                                float(mscale), _ptr(out), _current(out.device, "table")),
+           "mxq_rope_table")
     return out
 
 
 def _rotary(table, dev, interleaved: bool):
     if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype is torch.float32
-            and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous()):
+            and table.dim() == 3 and table.is_contiguous()):
         raise MxqError("the rotary table must be a contiguous float32 device tensor "
                        "[positions, rot / 2, 2]")
+    n, half, two = table.shape
+    if two != 2:
+        raise MxqError("the rotary table is %s, not [positions, rot / 2, 2]" % (tuple(table.shape),))
     if table.device != dev:
         raise MxqError("the rotary table is on %s, not %s" % (table.device, dev))
-    return _Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1], 1 if interleaved else 0)
+    return ctypes.byref(_Rotary(table.data_ptr(), n, 2 * half, 1 if interleaved else 0))
 
 
 def rope(x, pos, table, interleaved: bool = False, out=None):
@@ -742,18 +747,19 @@ def rope(x, pos, table, interleaved: bool = False, out=None):
     [T]): the first rot values of every head turn, as halves (i, i + rot / 2) or
     interleaved pairs (2 i, 2 i + 1).  `out` may be x (in place), else a tensor
     that does not overlap it."""
-    dev = _current(_heads(x, "x").device, "x")
-    T, H, D = x.shape
-    _index(pos, T, torch.int32, "pos", dev)
-    r = _rotary(table, dev, interleaved)
+    T, H, D = _heads(x, "x")
+    dev = x.device
+    stream = _current(dev, "x")
     if out is None:
-        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=dev)
-    elif out is not x:
-        _heads(out, "out", dev, H, D)
-        if out.shape[0] != T:
-            raise MxqError("out is %s, not %s" % (tuple(out.shape), tuple(x.shape)))
-    _check(lib().mxq_rope(ctypes.byref(r), _ptr(x), T, H, D, x.stride(0), x.stride(1), _ptr(pos),
-                          _ptr(out), out.stride(0), out.stride(1), _stream()), "mxq_rope")
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    elif out is not x and _heads(out, "out", dev, H, D)[0] != T:
+        raise MxqError("out is %s, not %s" % (tuple(out.shape), tuple(x.shape)))
+    st, so = x.stride(), out.stride()
+    status = lib().mxq_rope(_rotary(table, dev, interleaved), x.data_ptr(), T, H, D, st[0], st[1],
+                            _index(pos, T, torch.int32, "pos", dev), out.data_ptr(), so[0], so[1],
+                            stream)
+    if status:
+        _check(status, "mxq_rope")
     return out
 
 
@@ -804,53 +810,55 @@ def kv_append(cache: PagedCache, k, v, slots, pos=None, rope=None, interleaved: 
     is padding).  With q (bf16 [T, Hq, 128], strided) the queries are rotated by
     the same launch, and returned (contiguous; q_out may be q if that is
     contiguous)."""
-    dev = _current(cache.device, "the cache")
-    _heads(k, "k", dev, cache.Hkv, 128)
-    _heads(v, "v", dev, cache.Hkv, 128)
-    T = k.shape[0]
-    if v.shape[0] != T:
+    dev = cache.device
+    stream = _current(dev, "the cache")
+    T = _heads(k, "k", dev, cache.Hkv, 128)[0]
+    if _heads(v, "v", dev, cache.Hkv, 128)[0] != T:
         raise MxqError("k and v have %d and %d tokens" % (T, v.shape[0]))
-    _index(slots, T, torch.int64, "slots", dev)
-    r = None
+    r = at = None
     if rope is not None:
-        r = ctypes.byref(_rotary(rope, dev, interleaved))
-        _index(pos, T, torch.int32, "pos", dev)
-    Hq, qs = 0, (0, 0)
+        r = _rotary(rope, dev, interleaved)
+        at = _index(pos, T, torch.int32, "pos", dev)
+    Hq, qs, qp, op = 0, (0, 0), None, None
     if q is not None:
-        _heads(q, "q", dev, None, 128)
-        Hq, qs = q.shape[1], (q.stride(0), q.stride(1))
-        if q.shape[0] != T or Hq < 1:
+        Tq, Hq, _ = _heads(q, "q", dev, None, 128)
+        if Tq != T or Hq < 1:
             raise MxqError("q is %s: %d tokens and a head are needed" % (tuple(q.shape), T))
         if q_out is None:
-            q_out = torch.empty((T, Hq, 128), dtype=torch.bfloat16, device=dev)
-        elif not _heads(q_out, "q_out", dev, Hq, 128).is_contiguous() or q_out.shape[0] != T:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        elif _heads(q_out, "q_out", dev, Hq, 128)[0] != T or not q_out.is_contiguous():
             raise MxqError("q_out must be contiguous, [%d, %d, 128]" % (T, Hq))
+        qs, qp, op = q.stride(), q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise MxqError("q_out needs q")
-    _check(lib().mxq_kv_append(cache.fmt.ref, cache._ref, _ptr(k), k.stride(0), k.stride(1),
-                               _ptr(v), v.stride(0), v.stride(1), T, _ptr(slots),
-                               None if r is None else _ptr(pos), r, _ptr(q), Hq, qs[0], qs[1],
-                               _ptr(q_out), _stream()), "mxq_kv_append")
+    ks, vs = k.stride(), v.stride()
+    status = lib().mxq_kv_append(cache.fmt._ref, cache._ref, k.data_ptr(), ks[0], ks[1],
+                                 v.data_ptr(), vs[0], vs[1], T,
+                                 _index(slots, T, torch.int64, "slots", dev), at, r, qp, Hq, qs[0],
+                                 qs[1], op, stream)
+    if status:
+        _check(status, "mxq_kv_append")
     return q_out
 
 
 def kv_read(cache: PagedCache, slots, out=None):
     """The cached rows of the slots (int64 [n]) as the bf16 values that they stand
     for: (k, v), each [n, Hkv, 128]; zeros for a slot outside the cache."""
-    dev = _current(cache.device, "the cache")
-    if not isinstance(slots, torch.Tensor):
-        raise MxqError("slots must be a contiguous 1-D torch.int64 device tensor")
-    n = slots.shape[0] if slots.dim() == 1 else 0
-    _index(slots, n, torch.int64, "slots", dev)
+    dev = cache.device
+    stream = _current(dev, "the cache")
+    n = slots.numel() if isinstance(slots, torch.Tensor) else 0
+    at = _index(slots, n, torch.int64, "slots", dev)
     if out is None:
-        out = tuple(torch.empty((n, cache.Hkv, 128), dtype=torch.bfloat16, device=dev)
-                    for _ in range(2))
-    k, v = out
-    for t, what in ((k, "k"), (v, "v")):
-        if not _heads(t, what, dev, cache.Hkv, 128).is_contiguous() or t.shape[0] != n:
-            raise MxqError("%s must be contiguous, [%d, %d, 128]" % (what, n, cache.Hkv))
-    _check(lib().mxq_kv_read(cache.fmt.ref, cache._ref, _ptr(slots), n, _ptr(k), _ptr(v),
-                             _stream()), "mxq_kv_read")
+        # (one allocation for both)
+        k, v = torch.empty((2, n, cache.Hkv, 128), dtype=torch.bfloat16, device=dev).unbind()
+    else:
+        k, v = out
+        for t, what in ((k, "k"), (v, "v")):
+            if _heads(t, what, dev, cache.Hkv, 128)[0] != n or not t.is_contiguous():
+                raise MxqError("%s must be contiguous, [%d, %d, 128]" % (what, n, cache.Hkv))
+    status = lib().mxq_kv_read(cache.fmt._ref, cache._ref, at, n, k.data_ptr(), v.data_ptr(), stream)
+    if status:
+        _check(status, "mxq_kv_read")
     return k, v
 
 
@@ -872,25 +880,23 @@ def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: in
     `window` (0: all), and the first prefix[s] (int32 [S]); scores are capped by
     softcap * tanh(x / softcap) and lowered by slopes[h] (float32 [Hq]) times the
     distance.  Returns bf16 or float32 (`dtype`) [T, Hq, 128]."""
-    dev = _current(cache.device, "the cache")
-    T, Hq, _ = _heads(q, "q", dev, None, 128).shape
-    if not (isinstance(kv_len, torch.Tensor) and kv_len.dim() == 1):
-        raise MxqError("kv_len must be a contiguous 1-D torch.int32 device tensor")
-    S = kv_len.shape[0]
-    _index(kv_len, S, torch.int32, "kv_len", dev)
-    _index(cu_q, S + 1, torch.int32, "cu_q", dev)
+    dev = cache.device
+    stream = _current(dev, "the cache")
+    T, Hq, _ = _heads(q, "q", dev, None, 128)
+    S = kv_len.numel() if isinstance(kv_len, torch.Tensor) else 0
+    at = (_index(cu_q, S + 1, torch.int32, "cu_q", dev), _index(kv_len, S, torch.int32, "kv_len", dev))
     if not (isinstance(table, torch.Tensor) and table.is_cuda and table.dtype is torch.int32
             and table.dim() == 2 and table.shape[0] == S and table.device == dev
             and (table.stride(1) == 1 or table.shape[1] <= 1)):
         raise MxqError("table must be an int32 device tensor [%d, pages] with unit stride" % S)
     if prefix is not None:
-        _index(prefix, S, torch.int32, "prefix", dev)
+        prefix = _index(prefix, S, torch.int32, "prefix", dev)
     if slopes is not None:
-        _index(slopes, Hq, torch.float32, "slopes", dev)
+        slopes = _index(slopes, Hq, torch.float32, "slopes", dev)
     if out is None:
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise MxqError("dtype must be torch.bfloat16 or torch.float32")
-        out = torch.empty((T, Hq, 128), dtype=dtype, device=dev)
+        out = torch.empty_like(q, dtype=dtype, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.is_cuda and out.is_contiguous()
               and out.dtype in (torch.bfloat16, torch.float32) and out.device == dev
               and out.shape == q.shape):
@@ -899,12 +905,16 @@ def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: in
     if work is None:
         n = attn_paged_work_bytes(cache, S, T, Hq, max_q, max_kv)
         work = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
-    _dev_bytes(work, 0, "work", dev)
-    batch = _PagedBatch(S, T, max_q, max_kv, cu_q.data_ptr(), kv_len.data_ptr(),
-                        table.data_ptr(), table.stride(0), table.shape[1])
-    opts = _AttnOpts(scale, softcap, window, _ptr(prefix), _ptr(slopes))
-    _check(lib().mxq_attn_paged(cache.fmt.ref, cache._ref, ctypes.byref(batch),
-                                ctypes.byref(opts), _ptr(q), Hq, q.stride(0), q.stride(1),
-                                _ptr(out), 1 if out.dtype is torch.float32 else 0, _ptr(work),
-                                work.numel(), _stream()), "mxq_attn_paged")
+    else:
+        _dev_bytes(work, 0, "work", dev)
+    batch = _PagedBatch(S, T, max_q, max_kv, at[0], at[1], table.data_ptr(), table.stride(0),
+                        table.shape[1])
+    opts = _AttnOpts(scale, softcap, window, prefix, slopes)
+    qs = q.stride()
+    status = lib().mxq_attn_paged(cache.fmt._ref, cache._ref, ctypes.byref(batch),
+                                  ctypes.byref(opts), q.data_ptr(), Hq, qs[0], qs[1],
+                                  out.data_ptr(), 1 if out.dtype is torch.float32 else 0,
+                                  work.data_ptr(), work.numel(), stream)
+    if status:
+        _check(status, "mxq_attn_paged")
     return out

@@ -204,7 +204,7 @@ def host():
     """Host tensors presented as device tensors; a launch fails the test."""
     real = mxq.lib()
     with mock.patch.object(torch.Tensor, "is_cuda", new_callable=mock.PropertyMock, return_value=True), \
-            mock.patch.object(mxq, "_current", lambda dev, what: dev), \
+            mock.patch.object(mxq, "_current", lambda dev, what: None), \
             mock.patch.object(mxq, "lib", lambda path=mxq.LIB_PATH: _NoLaunch(real)):
         yield
 
@@ -282,8 +282,9 @@ def test_binding_refuses_attention(host):
 
 
 def test_calls_on_another_device_are_refused():
-    with mock.patch.object(torch.cuda, "current_device", lambda: 0):
-        assert mxq._current(torch.device("cuda:0"), "x") == torch.device("cuda:0")
+    with mock.patch.object(torch._C, "_cuda_getDevice", lambda: 0, create=True), \
+            mock.patch.object(torch._C, "_cuda_getCurrentRawStream", lambda i: 77 + i, create=True):
+        assert mxq._current(torch.device("cuda:0"), "x") == 77
         with pytest.raises(mxq.MxqError, match="current device"):
             mxq._current(torch.device("cuda:1"), "x")
 

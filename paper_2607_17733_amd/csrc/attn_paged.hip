@@ -35,31 +35,44 @@ constexpr int kRows = 32 * kWaves;       // query rows of a tile
 constexpr int kFewMost = 32;             // query rows of the kernel for few
 constexpr int kMaxSplits = 256;
 
-// LDS rows of a token's 128 bf16 values: sixteen chunks of 16 bytes, chunk c of
-// token t at c ^ swizzle(t).  Sixteen tokens' writes or operand reads of one chunk
-// and a transposing read (four tokens, four adjacent chunks) lie in distinct banks.
-constexpr int kTileBytes = kTok * kRowBytes;
-__device__ inline int swizzle(int t) { return 4 * (t & 3) + ((t >> 2) & 3); }
+// LDS rows of a token's 128 bf16 values.  The strides put sixteen tokens' operand
+// reads of K, and a transposing read of V (four tokens, 64 bytes), into distinct banks;
+// every access is a base plus a constant (an exclusive-or swizzle costs twenty
+// address registers, which the loop does not have).
+constexpr int kKRow = kRowBytes + 16, kVRow = kRowBytes + 64;
+constexpr int kKBytes = kTok * kKRow, kVBytes = kTok * kVRow, kStage = kKBytes + kVBytes;
 
-// A token's block b to its LDS row.
+// Keeps the packed words packed until here: the conversions that the ways to dequantize
+// a block have in common would else be done when it is loaded, and held in 32 registers.
 template <int M>
-__device__ __forceinline__ void store_block(const RawBlock &r, int E, uint8_t *tile, int t, int b) {
-  bf8 v[4];
+__device__ __forceinline__ RawBlock packed(const RawBlock &r) {
+  RawBlock b;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = dequant8<M>(r, j, E);
-  if (__any(E > max_exp(M))) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) big_scale<M>(v[j], E);
+  for (int i = 0; i < M; ++i) {
+    b.w[i] = r.w[i];
+    asm volatile("" : "+v"(b.w[i]));
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    *(bf8 *)(tile + t * kRowBytes + 16 * ((4 * b + j) ^ swizzle(t))) = v[j];
+  return b;
 }
-__device__ __forceinline__ void store_block(const RawBlock &r, int m, int E, uint8_t *tile, int t, int b) {
-  if (m == 4) store_block<4>(r, E, tile, t, b);
-  else if (m == 8) store_block<8>(r, E, tile, t, b);
-  else if (m == 6) store_block<6>(r, E, tile, t, b);
-  else store_block<3>(r, E, tile, t, b);
+
+// A token's block to its place in LDS, without the rest of the scale that blocks beyond
+// max_exp have ...
+template <int M>
+__device__ __forceinline__ void store_block(const RawBlock &r, int E, uint8_t *to) {
+  const RawBlock b = packed<M>(r);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) *(bf8 *)(to + 16 * j) = dequant8<M>(b, j, E);
+}
+// ... and again with it.
+template <int M>
+__device__ __forceinline__ void store_big(const RawBlock &r, int E, uint8_t *to) {
+  const RawBlock b = packed<M>(r);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    bf8 v = dequant8<M>(b, j, E);
+    big_scale<M>(v, E);
+    *(bf8 *)(to + 16 * j) = v;
+  }
 }
 
 // The tiles of `rows` query rows of all sequences are numbered with gaps: those of
@@ -86,10 +99,254 @@ __device__ inline int find_seq(const AttnPagedArgs &a, int64_t number, int rows,
   return lo;
 }
 
+// A wave's share of a tile: 32 query rows, a row per lane and its partner.
+struct TileRow {
+  int p;                                 // the row's position
+  int pw0, pw1;                          // the wave's first and last
+  int window, len, pre;
+  float sc, slope, softcap;
+  bool biased;
+};
+
+// S^T of half a step: 32 tokens (`rows`: row x, 16 h bytes on), this lane's query row;
+// value i is token 4 h + 8 (i / 4) + i % 4.
+__device__ __forceinline__ bf8 k_operand(const uint8_t *rows, int ks) {
+  return *(const bf8 *)(rows + 32 * ks);
+}
+__device__ __forceinline__ void scores(const uint8_t *rows, const bf8 (&qop)[8], f16v &s) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks)
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(rows, ks), qop[ks], s, 0, 0, 0);
+}
+// V^T operand of product i of half a step: tokens 16 (i / 4) .., values 32 (i % 4) ..;
+// lane half h holds its tokens 4 h .. 4 h + 3 and 8 + 4 h ..
+__device__ __forceinline__ bf8 v_operand(const uint8_t *vt, int i) {
+  const uint8_t *at = vt + 16 * (i >> 2) * kVRow + 64 * (i & 3);
+  const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at);
+  const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(at + 8 * kVRow));
+  return __builtin_bit_cast(bf8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Caps, biases and masks of half a step from token t0 on; returns the factor that is
+// left to apply.
+template <bool F32>
+__device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s) {
+  auto c = [](int i) { return 8 * (i >> 2) + (i & 3); };
+  float scale = w.sc;
+  if (w.softcap > 0.f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = capped<F32>(s[i] * scale, w.softcap) * kUnit<F32>;
+    scale = 1.f;
+  }
+  if (w.biased) {
+    const float rel = (float)(w.p - t0 - 4 * h);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(-w.slope, fabsf(rel - (float)c(i)), s[i] * scale);
+    scale = 1.f;
+  }
+  // masks, where not every row of the wave sees all
+  if (t0 + 31 > w.pw0 || w.pw1 - t0 >= w.window || t0 + 32 > w.len) {
+    const int rel = w.p - t0 - 4 * h, pre = w.pre - t0 - 4 * h, end = w.len - t0 - 4 * h;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = c(i);
+      const bool see = ((k <= rel && rel - k < w.window) || k < pre) && k < end;
+      s[i] = see ? s[i] : -__builtin_inff();
+    }
+  }
+  return scale;
+}
+
+// Dequantization: a wave's block of a step's K or V rows, a lane per token.  V's
+// unit v are the tokens of step v; K's are the second half of step v and the first
+// half of step v + 1.
+struct Loader {
+  const int32_t *pages;                  // of the sequence
+  int64_t plane;                         // of the block, in a page of one head
+  uint32_t page_rows, head_rows;         // rows of a page; those of the heads before
+  int blk, lane, last, lg_page, row, n_pages;
+  Steps st;
+  int v1;
+  // (past the last step: the last step's)
+  __device__ __forceinline__ int token(int v, bool k) const {
+    const int at = lane + (k ? kTok / 2 : 0);
+    const int u = min(max(v + (at >> 6), 0), v1 - 1);
+    return min((u < st.pre ? u : u + st.shift) * kTok + (at & (kTok - 1)), last);
+  }
+  __device__ __forceinline__ int page(int v, bool k) const { return pages[token(v, k) >> lg_page]; }
+  // The packed block and its exponent; false for a page outside the pool.
+  template <int M>
+  __device__ __forceinline__ bool load(const uint8_t *mant, const uint8_t *exp, int v, bool k, int page,
+                                       RawBlock &r, uint32_t &E) const {
+    const bool hole = (uint32_t)page >= (uint32_t)n_pages;
+    const uint32_t i = (uint32_t)token(v, k) & ((1u << lg_page) - 1);
+    const int64_t run = (int64_t)((uint64_t)(hole ? 0u : (uint32_t)page) * page_rows + head_rows);
+    load_block<M>(mant + run * row + plane + i * (4 * M), r);
+    E = exp[(run + i) * 4 + blk];
+    return !hole;
+  }
+};
+
+// A unit's block to LDS, where it needs more than store_block: pages outside the pool
+// (zero rows), exponents beyond max_exp.
+template <int M>
+__device__ __forceinline__ void store_rest(RawBlock &r, uint32_t E, bool good, uint8_t *to) {
+  if (__any(!good || (int)E > max_exp(M))) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r.w[k] = good ? r.w[k] : 0u;
+    store_big<M>(r, (int)E, to);
+  }
+}
+
+// Half a step: the probabilities of its 32 tokens while the next half's scores are
+// computed, then its share of the values while a unit of packed rows is dequantized.
+// A product holds the matrix core for 32 cycles, in which the wave issues eight vector
+// instructions: the work is cut into eight pieces each and one put behind each product,
+// in this order (left to itself the compiler puts the products in a row: every
+// sched_barrier keeps it from that), operands read two products ahead.
+template <bool F32, int M>
+__device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const bf8 (&qop)[8],
+                                          const uint8_t *next_rows, const uint8_t *vt, f16v &s, f16v &nx,
+                                          f16v (&o)[4], float &m, float &ref, float &l, RawBlock &r,
+                                          uint32_t E, uint8_t *to) {
+  const float ninf = -__builtin_inff();
+  bf8 kop[2] = {k_operand(next_rows, 0), k_operand(next_rows, 1)}, vop[2];
+  const float scale = adjust<F32>(w, t0, h, s);
+  float top = s[0];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+  top = fmaxf(top, other_half(top));
+  top = top == ninf ? ninf : top * scale;
+  if (__any(top > m + kSlack<F32> || (m == ninf && top != ninf))) {
+    const float nm = fmaxf(m, top);
+    const float alpha = m == ninf ? 0.f : weight<F32>(m - nm);
+    m = nm;
+    ref = nm == ninf ? 0.f : nm;                           // scores of -inf weigh 0
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) nx[i] = 0.f;
+  constexpr int kTerms = F32 ? 3 : 1;
+  bf8 pt[2][kTerms];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    nx = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[i & 1], qop[i], nx, 0, 0, 0);
+    if (i < 6) kop[i & 1] = k_operand(next_rows, i + 2);
+    else vop[i & 1] = v_operand(vt, i - 6);
+    float e0 = weight<F32>(fmaf(s[2 * i], scale, -ref)), e1 = weight<F32>(fmaf(s[2 * i + 1], scale, -ref));
+    l += e0;
+    l += e1;
+#pragma unroll
+    for (int k = 0; k < kTerms; ++k) {
+      const bf2 y = {(__bf16)e0, (__bf16)e1};
+      pt[i >> 2][k][2 * (i & 3)] = y[0];
+      pt[i >> 2][k][2 * (i & 3) + 1] = y[1];
+      if constexpr (F32) {
+        e0 -= (float)y[0];
+        e1 -= (float)y[1];
+      }
+    }
+  }
+  const RawBlock b = packed<M>(r);
+  const float sc = factor<M>((int)E);
+  Ints u = {0, 0};
+  bf4 first = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < kTerms; ++k)
+      o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[i & 1], pt[i >> 2][k], o[i & 3], 0, 0, 0);
+    if (i < 6) vop[i & 1] = v_operand(vt, i + 2);
+    // (4-bit integers take twice as long as their conversion)
+    if ((i & 1) == 0) {
+      u = ints8<M>(b, i >> 1);
+      if constexpr (M != 4) first = four<M>(u.b0, sc);
+    } else {
+      if constexpr (M == 4) first = four<M>(u.b0, sc);
+      *(bf8 *)(to + 16 * (i >> 1)) = both(first, four<M>(u.b1, sc));
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The steps v0 .. v1 - 1 of a tile, for a wave whose block has M bits.  One barrier
+// per step: behind it K's unit v and V's unit v are in LDS, and nobody reads the
+// other buffers any more, which take the units v + 1 meanwhile.  `live`: the wave
+// has query rows (one that has none only dequantizes).
+template <bool F32, int M>
+__device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader &ld, int v0, int v1,
+                                           bool live, const TileRow &w, const bf8 (&qop)[8],
+                                           uint8_t *lds, f16v (&o)[4], float &m, float &l) {
+  const int lane = ld.lane, h = lane >> 5, n = lane & 15;
+  // where this lane reads K's and V's operands and writes its blocks
+  const int kr = (lane & 31) * kKRow + 16 * h;
+  const int vr = kKBytes + (4 * h + (n >> 2)) * kVRow + 32 * (lane >> 4 & 1) + 8 * (n & 3);
+  const int kw = lane * kKRow + 64 * ld.blk, vw = kKBytes + lane * kVRow + 64 * ld.blk;
+  RawBlock rk, rv;
+  uint32_t ek, ev;
+  bool gk, gv;                                             // (false: the page is outside the pool)
+  auto load_k = [&](int v, int page) { gk = ld.template load<M>(a.k_mant, a.k_exp, v, true, page, rk, ek); };
+  auto load_v = [&](int v, int page) { gv = ld.template load<M>(a.v_mant, a.v_exp, v, false, page, rv, ev); };
+  auto put = [&](RawBlock &r, uint32_t E, bool good, uint8_t *to) {
+    store_block<M>(r, (int)E, to);
+    store_rest<M>(r, E, good, to);
+  };
+  // K's units v0 - 1 (its second half is the first step's first) and v0, V's unit v0,
+  // all their loads in flight together, then those of the units v0 + 1
+  uint8_t *cur = lds, *nxt = lds + kStage;
+  int pk = ld.page(v0, true), pv = ld.page(v0, false);
+  const int p1 = ld.page(v0 - 1, true), p2 = ld.page(v0 + 1, true), p3 = ld.page(v0 + 1, false);
+  RawBlock r1;
+  uint32_t e1;
+  const bool g1 = ld.template load<M>(a.k_mant, a.k_exp, v0 - 1, true, p1, r1, e1);
+  load_k(v0, pk);
+  load_v(v0, pv);
+  pk = ld.page(v0 + 2, true);
+  pv = ld.page(v0 + 2, false);
+  put(r1, e1, g1, nxt + kw);
+  put(rk, ek, gk, cur + kw);
+  load_k(v0 + 1, p2);
+  put(rv, ev, gv, cur + vw);
+  load_v(v0 + 1, p3);
+  __syncthreads();
+  f16v s, nx;
+  float ref = 0.f;
+  if (live) scores(nxt + kr + 32 * kKRow, qop, s);
+  for (int v = v0; v < v1; ++v) {
+    const int t0 = (v < ld.st.pre ? v : v + ld.st.shift) * kTok;
+    __syncthreads();
+    if (live) {
+      half_step<F32, M>(w, t0, h, qop, cur + kr, cur + vr, s, nx, o, m, ref, l, rk, ek, nxt + kw);
+      half_step<F32, M>(w, t0 + 32, h, qop, cur + kr + 32 * kKRow, cur + vr + 32 * kVRow, nx, s, o, m, ref, l,
+                        rv, ev, nxt + vw);
+    } else {
+      store_block<M>(rk, (int)ek, nxt + kw);
+      store_block<M>(rv, (int)ev, nxt + vw);
+    }
+    store_rest<M>(rk, ek, gk, nxt + kw);
+    store_rest<M>(rv, ev, gv, nxt + vw);
+    load_k(v + 2, pk);
+    load_v(v + 2, pv);
+    pk = ld.page(v + 3, true);
+    pv = ld.page(v + 3, false);
+    uint8_t *const swap = cur;
+    cur = nxt;
+    nxt = swap;
+  }
+}
+
 template <bool F32>
 __global__ __launch_bounds__(64 * kWaves, 2)
 void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];   // [buffer][K, V]
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage];         // K and V of two steps
   const PageGeo &g = a.geo;
   const int t = threadIdx.x, lane = t & 63, h = lane >> 5, x = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -111,14 +368,22 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   const int v0 = (int)((int64_t)st.count * split / splits);
   const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
 
-  // this lane's query row, and the wave's first and last position
+  // this lane's query row
   const int64_t wr = r0 + 32 * wave;
   const bool live = wr < rows;                             // of the wave
   const int64_t r = min(wr + x, rows - 1);
   const int tok = (int)(r / G), hd = kvh * G + (int)(r - (int64_t)tok * G);
-  const int p = (int)(p0 + tok);
-  const int pw0 = (int)(p0 + min(wr, rows - 1) / G), pw1 = (int)(p0 + (min(wr + 32, rows) - 1) / G);
-  const int window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
+  TileRow w;
+  w.p = (int)(p0 + tok);
+  w.pw0 = (int)(p0 + min(wr, rows - 1) / G);
+  w.pw1 = (int)(p0 + (min(wr + 32, rows) - 1) / G);
+  w.window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
+  w.len = q.len;
+  w.pre = q.pre;
+  w.sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
+  w.softcap = a.softcap;
+  w.biased = a.slopes != nullptr;
+  w.slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;
 
   // The score product's Q operand: 16 values of the reduction per product, lane
   // half h taking eight, in the slot order of their block.  A negative scale goes
@@ -129,167 +394,40 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
     const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
-      u4 w = *(const u4 *)(src + 16 * ks + 8 * h);
-      w = a.scale == 0.f ? u4{0u, 0u, 0u, 0u} : w ^ u4{sign, sign, sign, sign};
+      u4 y = *(const u4 *)(src + 16 * ks + 8 * h);
+      y = a.scale == 0.f ? u4{0u, 0u, 0u, 0u} : y ^ u4{sign, sign, sign, sign};
       if (split_slots(g.m[ks >> 1]))
-        w = u4{__builtin_amdgcn_perm(w[1], w[0], 0x05040100), __builtin_amdgcn_perm(w[3], w[2], 0x05040100),
-               __builtin_amdgcn_perm(w[1], w[0], 0x07060302), __builtin_amdgcn_perm(w[3], w[2], 0x07060302)};
-      qop[ks] = __builtin_bit_cast(bf8, w);
+        y = u4{__builtin_amdgcn_perm(y[1], y[0], 0x05040100), __builtin_amdgcn_perm(y[3], y[2], 0x05040100),
+               __builtin_amdgcn_perm(y[1], y[0], 0x07060302), __builtin_amdgcn_perm(y[3], y[2], 0x07060302)};
+      qop[ks] = __builtin_bit_cast(bf8, y);
     }
   }
-  const float sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
-  const float slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;
 
-  const float ninf = -__builtin_inff();
-  float m = ninf, ref = 0.f, l = 0.f;                      // l: this lane's tokens
+  float m = -__builtin_inff(), l = 0.f;                    // l: this lane's tokens
   f16v o[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-
-  // Dequantization: this wave's block, this lane's token of a step.  Tokens past
-  // the last are the last one (weight 0).
-  const int blk = wave, bm = pick(g.m, blk);
-  const int64_t plane = (int64_t)pick(g.off, blk) << g.lg_page;
-  const int page_mask = (1 << g.lg_page) - 1;
-  const int32_t *pages = a.table + (int64_t)s * a.ld_table;
-  RawBlock rk, rv;
-  uint32_t ek, ev;
-  auto token_of = [&](int v) { return min((v < st.pre ? v : v + st.shift) * kTok + lane, q.len - 1); };
-  auto page_of = [&](int v) { return pages[token_of(min(v, v1 - 1)) >> g.lg_page]; };
-  auto fetch = [&](int v, int page) __attribute__((always_inline)) {
-    const bool hole = page < 0 || page >= g.pages;
-    const int i = token_of(v) & page_mask;
-    const int64_t run = ((int64_t)(hole ? 0 : page) * Hkv + kvh) << g.lg_page;
-    const int64_t at = run * g.row + plane + i * 4 * bm;
-    load_block(a.k_mant + at, bm, rk);
-    load_block(a.v_mant + at, bm, rv);
-    ek = a.k_exp[(run + i) * 4 + blk];
-    ev = a.v_exp[(run + i) * 4 + blk];
-    if (hole) {                                            // zero rows
-#pragma unroll
-      for (int k = 0; k < 8; ++k) rk.w[k] = rv.w[k] = 0u;
-    }
-  };
-  auto put = [&](int buf) __attribute__((always_inline)) {
-    store_block(rk, bm, (int)ek, lds[buf][0], lane, blk);
-    store_block(rv, bm, (int)ev, lds[buf][1], lane, blk);
-  };
-
   if (v0 < v1) {
-    const int page = page_of(v0);
-    int next = page_of(v0 + 1);
-    fetch(v0, page);
-    put(0);
-    for (int v = v0; v < v1; ++v) {
-      const int buf = (v - v0) & 1;
-      __syncthreads();                                     // this step's rows are there, the last one's read
-      if (v + 1 < v1) {
-        fetch(v + 1, next);
-        next = page_of(v + 2);
-      }
-      const int t0 = (v < st.pre ? v : v + st.shift) * kTok;
-      if (live && ((t0 <= pw1 && pw0 - t0 - kTok + 1 < window) || t0 < q.pre)) {
-        // scores
-        f16v sa[2];
-        const uint8_t *kt = lds[buf][0] + x * kRowBytes;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sa[u][i] = 0.f;
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) {
-            const bf8 k = *(const bf8 *)(kt + u * 32 * kRowBytes + 16 * ((2 * ks + h) ^ swizzle(x)));
-            sa[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qop[ks], sa[u], 0, 0, 0);
-          }
-        }
-        // value i of half u is token t0 + 4 h + c(u, i)
-        auto c = [](int u, int i) { return 32 * u + 8 * (i >> 2) + (i & 3); };
-        float scale = sc;
-        if (a.softcap > 0.f || a.slopes) {
-          const float rel = (float)(p - t0 - 4 * h);
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float y = sa[u][i] * sc;
-              if (a.softcap > 0.f) y = capped<F32>(y, a.softcap) * kUnit<F32>;
-              sa[u][i] = fmaf(-slope, fabsf(rel - (float)c(u, i)), y);
-            }
-          scale = 1.f;
-        }
-        // masks, for steps that not every row of the wave sees whole
-        if (t0 + kTok - 1 > pw0 || pw1 - t0 >= window || t0 + kTok > q.len) {
-          const int rel = p - t0 - 4 * h, pre = q.pre - t0 - 4 * h, end = q.len - t0 - 4 * h;
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int k = c(u, i);
-              const bool see = ((k <= rel && rel - k < window) || k < pre) && k < end;
-              if (!see) sa[u][i] = ninf;
-            }
-        }
-        float top = sa[0][0];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) top = fmaxf(top, sa[u][i]);
-        top = fmaxf(top, other_half(top));
-        top = top == ninf ? ninf : top * scale;
-        if (__any(top > m + kSlack<F32> || (m == ninf && top != ninf))) {
-          const float nm = fmaxf(m, top);
-          const float alpha = m == ninf ? 0.f : weight<F32>(m - nm);
-          m = nm;
-          ref = nm == ninf ? 0.f : nm;                     // scores of -inf weigh 0
-          l *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            sa[u][i] = weight<F32>(fmaf(sa[u][i], scale, -ref));
-            l += sa[u][i];
-          }
-        // values: product z takes tokens 16 z ..; lane half h holds its tokens
-        // 4 h .. 4 h + 3 and 8 + 4 h ..
-        const int n = lane & 15, w4 = lane >> 4 & 1;
-        const uint8_t *vt = lds[buf][1] + (4 * h + (n >> 2)) * kRowBytes + 8 * (n & 1);
-        const int col = 2 * w4 + ((n & 3) >> 1);
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          float e[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) e[i] = sa[z >> 1][8 * (z & 1) + i];
-          constexpr int kTerms = F32 ? 3 : 1;
-          bf8 pt[kTerms];
-#pragma unroll
-          for (int k = 0; k < kTerms; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              pt[k][i] = (__bf16)e[i];
-              if constexpr (F32) e[i] -= (float)pt[k][i];
-            }
-#pragma unroll
-          for (int dt = 0; dt < 4; ++dt) {
-            const uint8_t *v0p = vt + 16 * z * kRowBytes + 16 * ((4 * dt + col) ^ (4 * (n >> 2) + h));
-            const uint8_t *v1p = vt + (16 * z + 8) * kRowBytes + 16 * ((4 * dt + col) ^ (4 * (n >> 2) + h + 2));
-            const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)v0p);
-            const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)v1p);
-            const bf8 vv = __builtin_bit_cast(bf8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int k = 0; k < kTerms; ++k)
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pt[k], o[dt], 0, 0, 0);
-          }
-        }
-      }
-      if (v + 1 < v1) put(buf ^ 1);
-    }
+    Loader ld;
+    ld.pages = a.table + (int64_t)s * a.ld_table;
+    ld.blk = wave;
+    ld.plane = (int64_t)pick(g.off, wave) << g.lg_page;
+    ld.page_rows = (uint32_t)Hkv << g.lg_page;
+    ld.head_rows = (uint32_t)kvh << g.lg_page;
+    ld.lane = lane;
+    ld.last = q.len - 1;
+    ld.lg_page = g.lg_page;
+    ld.row = g.row;
+    ld.n_pages = (int)g.pages;
+    ld.st = st;
+    ld.v1 = v1;
+    const int bm = pick(g.m, wave);
+    if (bm == 4) tile_steps<F32, 4>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
+    else if (bm == 8) tile_steps<F32, 8>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
+    else if (bm == 6) tile_steps<F32, 6>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
+    else tile_steps<F32, 3>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
   }
   if (wr + x >= rows) return;
   l += other_half(l);

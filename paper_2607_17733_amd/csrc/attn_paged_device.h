@@ -101,57 +101,75 @@ __device__ inline uint32_t low_nibbles_else(uint32_t a, uint32_t b) {
 // range; a block beyond it is dequantized there and scaled again.
 constexpr int max_exp(int m) { return m == 3 ? 255 : m == 4 ? 247 : 253; }
 
-// Group j (eight values) of a block, in slot order: q * 2^(E - 127 - (m - 2)).
+// Group j (eight values) of a block, in slot order: q * 2^(E - 127 - (m - 2)), in two
+// parts (so that a caller can put other work between them): integers, four values each.
+struct Ints {
+  uint32_t b0, b1;
+};
 template <int M>
-__device__ __forceinline__ bf8 dequant8(const RawBlock &r, int j, int E) {
+__device__ __forceinline__ Ints ints8(const RawBlock &r, int j) {
+  Ints y;
   if constexpr (M == 4) {
     // two's complement nibbles -> bytes of sign and magnitude 0..8, whose FP8
-    // (e4m3) value is linear, k 2^-9; the conversion applies the block's scale
+    // (e4m3) value is linear, k 2^-9
     const uint32_t w = r.w[j];
     const uint32_t sg = w & 0x88888888u, one = sg >> 3;
     const uint32_t mag = (w ^ ((one << 4) - one)) + one;
-    const uint32_t ev = low_nibbles_else(mag, sg << 4), od = low_nibbles_else(mag >> 4, sg);
-    const float sc = __uint_as_float((uint32_t)(min(E, max_exp(4)) + 7) << 23);
-    bf2 v[4];
-    v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(ev, sc, false);
-    v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(ev, sc, true);
-    v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(od, sc, false);
-    v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(od, sc, true);
-    return bf8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
+    y.b0 = low_nibbles_else(mag, sg << 4);
+    y.b1 = low_nibbles_else(mag >> 4, sg);
+  } else if constexpr (M == 8) {
+    y.b0 = r.w[2 * j] ^ 0x80808080u;                       // bytes u = q + 128
+    y.b1 = r.w[2 * j + 1] ^ 0x80808080u;
+  } else if constexpr (M == 6) {
+    // bytes u = q + 32; byte i of the top word: bits 7:6 and 5:4 (3:2 and 1:0 in
+    // the odd groups) are the top bits of elements 2i and 2i + 1
+    const uint32_t w = r.w[j], tw = r.w[4 + (j >> 1)] << (4 * (j & 1));
+    y.b0 = low_nibbles_else(w, (tw >> 2) & 0x30303030u) ^ 0x20202020u;
+    y.b1 = low_nibbles_else(w >> 4, tw & 0x30303030u) ^ 0x20202020u;
   } else {
-    const float sc = __builtin_amdgcn_ldexpf(1.f, min(E, max_exp(M)) - 127 - (M - 2));
-    float x[8];
+    const int b = 24 * j, lo = b >> 5, sh = b & 31;
+    uint32_t w = r.w[lo] >> sh;
+    if (sh > 8) w |= r.w[lo + 1] << (32 - sh);
+    y.b0 = w;                                              // eight 3-bit fields
+    y.b1 = w >> 12;
+  }
+  return y;
+}
+// The factor that four() takes, of a block with exponent E.
+template <int M>
+__device__ __forceinline__ float factor(int E) {
+  if constexpr (M == 4) return __uint_as_float((uint32_t)(min(E, max_exp(4)) + 7) << 23);
+  return __builtin_amdgcn_ldexpf(1.f, min(E, max_exp(M)) - 127 - (M - 2));
+}
+// Four values from one of the two integers.
+template <int M>
+__device__ __forceinline__ bf4 four(uint32_t u, float sc) {
+  if constexpr (M == 4) {                                  // the conversion applies the scale
+    const bf2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, sc, false);
+    const bf2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, sc, true);
+    return bf4{x[0], x[1], y[0], y[1]};
+  } else {
+    float x[4];
     if constexpr (M == 3) {
-      const int b = 24 * j, lo = b >> 5, sh = b & 31;
-      uint32_t w = r.w[lo] >> sh;
-      if (sh > 8) w |= r.w[lo + 1] << (32 - sh);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (float)(int)__builtin_amdgcn_sbfe((int)w, 3 * i, 3) * sc;
+      for (int i = 0; i < 4; ++i) x[i] = (float)(int)__builtin_amdgcn_sbfe((int)u, 3 * i, 3) * sc;
     } else {
-      // bytes u = q + 2^(M - 1); u sc - 2^(M - 1) sc is exact, in one rounding
-      uint32_t b0, b1;
-      if constexpr (M == 8) {
-        b0 = r.w[2 * j] ^ 0x80808080u;
-        b1 = r.w[2 * j + 1] ^ 0x80808080u;
-      } else {
-        // byte i of the top word: bits 7:6 and 5:4 (3:2 and 1:0 in the odd groups)
-        // are the top bits of elements 2i and 2i + 1
-        const uint32_t w = r.w[j], tw = r.w[4 + (j >> 1)] << (4 * (j & 1));
-        b0 = low_nibbles_else(w, (tw >> 2) & 0x30303030u) ^ 0x20202020u;
-        b1 = low_nibbles_else(w >> 4, tw & 0x30303030u) ^ 0x20202020u;
-      }
+      // u sc - 2^(M - 1) sc is exact, in one rounding
       const float off = sc * -(float)(1 << (M - 1));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[i] = fmaf((float)((b0 >> (8 * i)) & 255u), sc, off);
-        x[4 + i] = fmaf((float)((b1 >> (8 * i)) & 255u), sc, off);
-      }
+      for (int i = 0; i < 4; ++i) x[i] = fmaf((float)((u >> (8 * i)) & 255u), sc, off);
     }
-    bf8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (__bf16)x[i];
-    return y;
+    return bf4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
   }
+}
+__device__ __forceinline__ bf8 both(bf4 x, bf4 y) {
+  return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <int M>
+__device__ __forceinline__ bf8 dequant8(const RawBlock &r, int j, int E) {
+  const Ints u = ints8<M>(r, j);
+  const float sc = factor<M>(E);
+  return both(four<M>(u.b0, sc), four<M>(u.b1, sc));
 }
 
 // The rest of the scale of blocks beyond max_exp.  (E = 255 is no exception: the

@@ -79,24 +79,28 @@ __device__ __forceinline__ void store_big(const RawBlock &r, int E, uint8_t *to)
 // sequence s begin at floor(cu_q[s] G / rows) + s.  No two sequences meet (a
 // sequence of n rows has at most floor(end / rows) - floor(begin / rows) + 1
 // tiles), and floor(T G / rows) + S numbers are enough, so that the launch needs
-// no look at the device's lengths.  The sequence of a number, by 64-way search
-// (-1: a gap).
-__device__ inline int find_seq(const AttnPagedArgs &a, int64_t number, int rows, int &tile) {
-  const int lane = threadIdx.x & 63;
-  auto start = [&](int s) { return (int64_t)max(a.cu_q[s], 0) * a.G / rows + s; };
-  int lo = 0, cnt = (int)a.S;
-  for (;;) {
+// no look at the device's lengths.  The sequence of a number, by 64-way search; up
+// to 64 sequences cost one load latency, their lengths included.  False: a gap.
+__device__ inline bool find_seq(const AttnPagedArgs &a, int64_t number, int rows, Seq &q, int &tile) {
+  const int lane = threadIdx.x & 63, S = (int)a.S;
+  auto start = [&](int s, int cu) { return (int64_t)max(cu, 0) * a.G / rows + s; };
+  int lo = 0, cnt = S;
+  while (cnt > 64) {
     const int step = (cnt + 63) / 64, s = lo + lane * step;
-    const bool le = s < lo + cnt && start(s) <= number;
+    const bool le = s < lo + cnt && start(s, a.cu_q[min(s, S)]) <= number;
     const int k = __popcll(__ballot(le));
-    if (k == 0) return -1;
+    if (k == 0) return false;
     lo += (k - 1) * step;
-    if (step == 1) break;
-    cnt = min(step, (int)a.S - lo);
+    cnt = min(step, S - lo);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  tile = (int)(number - start(lo));
-  return lo;
+  const int s = min(lo + lane, S - 1);
+  const int c0 = a.cu_q[s], c1 = a.cu_q[s + 1], len = a.kv_len[s], pre = a.prefix ? a.prefix[s] : 0;
+  const int k = __popcll(__ballot(lane < cnt && start(s, c0) <= number)) - 1;
+  if (k < 0) return false;
+  auto of = [&](int x) { return __builtin_amdgcn_readlane(x, k); };
+  q = seq_of(a, of(s), of(c0), of(c1), of(len), of(pre));
+  tile = (int)(number - start(q.s, of(c0)));
+  return true;
 }
 
 // A wave's share of a tile: 32 query rows, a row per lane and its partner.
@@ -358,9 +362,8 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   const int64_t number = numbers - 1 - rest / (uint32_t)splits;
   const int split = (int)(rest % (uint32_t)splits);
   int tile;
-  const int s = find_seq(a, number, kRows, tile);
-  if (s < 0) return;
-  const Seq q = seq_at(a, s);
+  Seq q;
+  if (!find_seq(a, number, kRows, q, tile)) return;
   const int64_t rows = (int64_t)q.n * G, r0 = (int64_t)tile * kRows;
   if (r0 >= rows || rows <= few_rows) return;
   const int64_t p0 = (int64_t)q.len - q.n;                 // the first row's position
@@ -385,9 +388,9 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   w.biased = a.slopes != nullptr;
   w.slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;
 
-  // The score product's Q operand: 16 values of the reduction per product, lane
-  // half h taking eight, in the slot order of their block.  A negative scale goes
-  // into its sign; for a scale of zero Q is zero (a masked score, -inf, is scaled).
+  // The score product's Q operand: 16 values of the reduction per product, lane half h
+  // taking eight, in the slot order of their block.  A negative scale goes into its
+  // sign; for a scale of zero Q is zero (a masked score, -inf, is scaled).
   bf8 qop[8];
   {
     const uint16_t *src = a.q + (int64_t)(q.row0 + tok) * a.q_ts + hd * a.q_hs;
@@ -411,7 +414,7 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   if (v0 < v1) {
     Loader ld;
-    ld.pages = a.table + (int64_t)s * a.ld_table;
+    ld.pages = a.table + (int64_t)q.s * a.ld_table;
     ld.blk = wave;
     ld.plane = (int64_t)pick(g.off, wave) << g.lg_page;
     ld.page_rows = (uint32_t)Hkv << g.lg_page;
@@ -465,25 +468,32 @@ constexpr int kMergeThreads = 256;
 constexpr int kBatch = 8;
 template <bool F32, int GROUPS>
 __global__ __launch_bounds__(kMergeThreads)
-void attn_merge_kernel(AttnPagedArgs a, int tile, int few, int few_rows) {
+void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int64_t count) {
   constexpr int kRowsHere = kMergeThreads / 32 / GROUPS;
   __shared__ __attribute__((aligned(16))) float po[GROUPS > 1 ? GROUPS : 1][kD];
   __shared__ float pm[GROUPS], pl[GROUPS];
   const int t = threadIdx.x, c = t & 31, grp = (t >> 5) % GROUPS;
-  const int64_t row = (int64_t)blockIdx.x * kRowsHere + (t >> 5) / GROUPS;
-  if (row >= a.T * a.Hq) return;                           // (uniform where the groups meet)
-  const int tok = (int)(row / a.Hq);
-  if (tok < a.cu_q[0] || tok >= a.cu_q[a.S]) return;       // no sequence's row
-  int splits = tile;
-  if (tile != few) {                                       // which kernel had the row
-    int lo = 0, hi = (int)a.S - 1;                         // the last sequence that begins at tok or before
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (a.cu_q[mid] <= tok) lo = mid;
-      else hi = mid - 1;
+  const int64_t id = (int64_t)blockIdx.x * kRowsHere + (t >> 5) / GROUPS;
+  if (id >= count) return;                                 // (uniform where the groups meet)
+  int64_t row = id;
+  if (most > 0) {                                          // row id % (most Hq) of a short sequence
+    const int64_t per = most * a.Hq;
+    const int s = (int)(id / per), c0 = a.cu_q[s], n = a.cu_q[s + 1] - c0;
+    const int64_t r = id - s * per;
+    if (r >= n * a.Hq || n * (int64_t)a.G > few_rows || c0 < 0 || c0 + (int64_t)n > a.T) return;
+    row = c0 * a.Hq + r;
+  } else {
+    const int tok = (int)(row / a.Hq);
+    if (tok < a.cu_q[0] || tok >= a.cu_q[a.S]) return;     // no sequence's row
+    if (few_rows > 0) {                                    // the other kernel's rows
+      int lo = 0, hi = (int)a.S - 1;                       // the last sequence that begins at tok or before
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (a.cu_q[mid] <= tok) lo = mid;
+        else hi = mid - 1;
+      }
+      if ((int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G <= few_rows) return;
     }
-    if ((int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G <= few_rows) splits = few;
-    if (splits == 1) return;                               // written already
   }
   const float ninf = -__builtin_inff();
   float M = ninf, L = 0.f;
@@ -554,15 +564,14 @@ void attn_merge_kernel(AttnPagedArgs a, int tile, int few, int few_rows) {
       bf4{(__bf16)O[0], (__bf16)O[1], (__bf16)O[2], (__bf16)O[3]};
 }
 
-template <bool F32>
-void launch_merge(const AttnPagedArgs &a, int tile, int few, int few_rows, hipStream_t s) {
-  const int64_t rows = a.T * a.Hq;
-  if (std::max(tile, few) <= kBatch)
-    hipLaunchKernelGGL((attn_merge_kernel<F32, 1>), dim3((unsigned)((rows + 7) / 8)),
-                       dim3(kMergeThreads), 0, s, a, tile, few, few_rows);
-  else
-    hipLaunchKernelGGL((attn_merge_kernel<F32, 8>), dim3((unsigned)rows), dim3(kMergeThreads), 0, s,
-                       a, tile, few, few_rows);
+// The rows of the tiles (most 0), or up to `most` rows of every short sequence.
+void launch_merge(const AttnPagedArgs &a, int splits, int few_rows, int most, hipStream_t s) {
+  const int64_t count = most > 0 ? a.S * most * a.Hq : a.T * a.Hq;
+  const bool few = splits <= kBatch;
+  const auto fn = few ? (a.o_f32 ? attn_merge_kernel<true, 1> : attn_merge_kernel<false, 1>)
+                      : (a.o_f32 ? attn_merge_kernel<true, 8> : attn_merge_kernel<false, 8>);
+  hipLaunchKernelGGL(fn, dim3((unsigned)(few ? (count + 7) / 8 : count)), dim3(kMergeThreads), 0, s, a,
+                     splits, few_rows, most, count);
 }
 
 int64_t tile_numbers(const AttnPagedArgs &a) { return a.T * a.G / kRows + a.S; }
@@ -603,23 +612,22 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   const int64_t numbers = tile_numbers(a);
   const int64_t wgs = numbers * a.geo.Hkv * p.tile;
   const int few_rows = p.few ? 16 * p.groups : 0;          // what the tiles leave to the other kernel
+  const int most = (int)std::min<int64_t>(a.max_q, few_rows / a.G);
   // (a dispatch holds fewer than 2^32 threads)
-  if (std::max({wgs, a.S * a.geo.Hkv * p.few, a.parts > 1 ? a.T * a.Hq : 0}) >= ((int64_t)1 << 32) / 256)
+  const int64_t merged = std::max(p.tile > 1 ? a.T * a.Hq : 0, p.few > 1 ? a.S * most * a.Hq : 0);
+  if (std::max({wgs, a.S * a.geo.Hkv * p.few, merged}) >= ((int64_t)1 << 32) / 256)
     return hipErrorInvalidValue;
-  hipError_t e = hipSuccess;
   if (p.few) {
-    e = a.o_f32 ? launch_attn_few_f32(a, p.few, p.groups, s) : launch_attn_few_bf16(a, p.few, p.groups, s);
+    const hipError_t e = a.o_f32 ? launch_attn_few_f32(a, p.few, p.groups, s)
+                                 : launch_attn_few_bf16(a, p.few, p.groups, s);
     if (e != hipSuccess) return e;
+    if (p.few > 1) launch_merge(a, p.few, few_rows, most, s);
   }
   if (p.tile) {
     const auto fn = a.o_f32 ? attn_tile_kernel<true> : attn_tile_kernel<false>;
     hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(64 * kWaves), 0, s, a, p.tile, numbers, few_rows);
-    e = hipGetLastError();
+    if (p.tile > 1) launch_merge(a, p.tile, few_rows, 0, s);
   }
-  if (e != hipSuccess || a.parts <= 1) return e;
-  const int tile = p.tile ? p.tile : p.few, few = p.few ? p.few : p.tile;
-  if (a.o_f32) launch_merge<true>(a, tile, few, few_rows, s);
-  else launch_merge<false>(a, tile, few, few_rows, s);
   return hipGetLastError();
 }
 

@@ -196,18 +196,21 @@ struct Seq {
   int len;                               // cached tokens
   int pre;                               // the tokens that every row sees
 };
-__device__ inline Seq seq_at(const AttnPagedArgs &a, int s) {
+__device__ inline Seq seq_of(const AttnPagedArgs &a, int s, int begin, int end, int kv_len, int prefix) {
   Seq q;
   q.s = s;
   const int T = (int)a.T;
-  const int c0 = min(max(a.cu_q[s], 0), T), c1 = min(max(a.cu_q[s + 1], c0), T);
+  const int c0 = min(max(begin, 0), T), c1 = min(max(end, c0), T);
   q.row0 = c0;
   q.n = c1 - c0;
-  int64_t len = min((int64_t)a.kv_len[s], a.max_kv);
+  int64_t len = min((int64_t)kv_len, a.max_kv);
   len = min(len, a.table_pages << a.geo.lg_page);
   q.len = (int)max(len, (int64_t)0);
-  q.pre = a.prefix ? min(max(a.prefix[s], 0), q.len) : 0;
+  q.pre = min(max(prefix, 0), q.len);
   return q;
+}
+__device__ inline Seq seq_at(const AttnPagedArgs &a, int s) {
+  return seq_of(a, s, a.cu_q[s], a.cu_q[s + 1], a.kv_len[s], a.prefix ? a.prefix[s] : 0);
 }
 
 // The steps (of TOK tokens) that rows at positions p_lo .. p_hi need: those of the

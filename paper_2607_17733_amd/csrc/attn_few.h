@@ -132,10 +132,8 @@ __device__ __forceinline__ void dequant_row(const RawRow<Mx> &r, int g, bool big
   }
 }
 
-// Whether one of four exponents may pass max_exp (E >= 224).
-__device__ inline bool has_big(uint32_t ex) {
-  return (ex & (ex << 1) & (ex << 2) & 0x80808080u) != 0;
-}
+// Nonzero if one of four exponents may pass max_exp (E >= 224).
+__device__ inline uint32_t big_bits(uint32_t ex) { return ex & (ex << 1) & (ex << 2) & 0x80808080u; }
 
 __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -177,11 +175,12 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   // the last one (weight 0), a half past the last token is the chunk's first.
   const int32_t *pages = a.table + (int64_t)s * a.ld_table;
   const int page_mask = (1 << g.lg_page) - 1, last = q.len - 1;
-  auto first_of = [&](int v) { return (v < st.pre ? v : v + st.shift) * kFewChunk; };
+  // (past the last chunk: the last one)
+  auto first_of = [&](int v) { return (min(v, v1 - 1) < st.pre ? min(v, v1 - 1) : min(v, v1 - 1) + st.shift) * kFewChunk; };
   auto half_of = [&](int t0, int mt) { return t0 + 16 * mt <= last ? t0 + 16 * mt : t0; };
   int pg[2];
   auto number = [&](int v) __attribute__((always_inline)) {
-    const int t0 = first_of(min(v, v1 - 1));
+    const int t0 = first_of(v);
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) pg[mt] = pages[half_of(t0, mt) >> g.lg_page];
   };
@@ -250,8 +249,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
         for (int k = 0; k < Mx::kWords; ++k) c.k[mt].w[k] = c.v[mt].w[k] = 0u;
         c.k[mt].ex = c.v[mt].ex = 0u;
       }
-    const bool big = __any(has_big(c.k[0].ex) || has_big(c.k[1].ex) || has_big(c.v[0].ex) ||
-                           has_big(c.v[1].ex));
+    const bool big = __any((big_bits(c.k[0].ex) | big_bits(c.k[1].ex) | big_bits(c.v[0].ex) |
+                            big_bits(c.v[1].ex)) != 0);
     // scores: tokens 16 mt + 4 gr + i of row n
     f4 sa[NC][2];
 #pragma unroll
@@ -302,7 +301,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int k = 16 * (i >> 2) + (i & 3);
-          const bool see = ((k <= rel && rel - k < window) || k < pre) && k < end;
+          const bool see = (((k <= rel) & (rel - k < window)) | (k < pre)) & (k < end);
           x[i] = see ? x[i] : ninf;
         }
       }
@@ -348,13 +347,12 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
           o[e][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pt[e][k], o[e][dt], 0, 0, 0);
     }
   };
-  // the next chunk's rows are asked for before one is computed, then the page
-  // numbers of the one after it
+  // The next chunk's rows are asked for before one is computed, then the page numbers
+  // of the one after it.  (Also behind the last chunk: a load under a condition would
+  // make the compiler wait for all of them where one set's rows are used.)
   auto step = [&](Chunk<Mx> &cur, Chunk<Mx> &next) __attribute__((always_inline)) {
-    if (v + kFewWaves < v1) {
-      fetch(v + kFewWaves, next);
-      number(v + 2 * kFewWaves);
-    }
+    fetch(v + kFewWaves, next);
+    number(v + 2 * kFewWaves);
     compute(v, cur);
     v += kFewWaves;
   };

@@ -156,7 +156,7 @@ __device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int k = c(i);
-      const bool see = ((k <= rel && rel - k < w.window) || k < pre) && k < end;
+      const bool see = (((k <= rel) & (rel - k < w.window)) | (k < pre)) & (k < end);
       s[i] = see ? s[i] : -__builtin_inff();
     }
   }

@@ -149,9 +149,9 @@ struct Chunk {
 };
 
 // NC: groups of 16 query rows.  Two sets of a chunk's registers leave room for three
-// waves per SIMD with one group and narrow rows, else for two.
+// waves per SIMD with one group and rows of at most seven words a lane, else for two.
 template <bool F32, class Mx, int NC>
-__global__ __launch_bounds__(64 * kFewWaves, NC == 1 && Mx::kWords <= 4 ? 3 : 2)
+__global__ __launch_bounds__(64 * kFewWaves, NC == 1 && Mx::kWords <= 7 ? 3 : 2)
 void attn_few_kernel(AttnPagedArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) uint8_t pool[kFewWaves][kFewBytes];
   __shared__ float mm[kFewWaves][16 * NC], ml[kFewWaves][16 * NC];

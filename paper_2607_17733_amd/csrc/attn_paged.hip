@@ -30,8 +30,6 @@ namespace mxq {
 namespace {
 
 constexpr int kTok = 64;                 // tokens per step
-constexpr int kWaves = 4;
-constexpr int kRows = 32 * kWaves;       // query rows of a tile
 constexpr int kFewMost = 32;             // query rows of the kernel for few
 constexpr int kMaxSplits = 256;
 
@@ -205,12 +203,13 @@ __device__ __forceinline__ void store_rest(RawBlock &r, uint32_t E, bool good, u
 }
 
 // Half a step: the probabilities of its 32 tokens while the next half's scores are
-// computed, then its share of the values while a unit of packed rows is dequantized.
+// computed, then its share of the values while GROUPS groups of a packed block, from G0
+// on, are dequantized.
 // A product holds the matrix core for 32 cycles, in which the wave issues eight vector
 // instructions: the work is cut into eight pieces each and one put behind each product,
 // in this order (left to itself the compiler puts the products in a row: every
 // sched_barrier keeps it from that), operands read two products ahead.
-template <bool F32, int M>
+template <bool F32, int M, int G0, int GROUPS>
 __device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const bf8 (&qop)[8],
                                           const uint8_t *next_rows, const uint8_t *vt, f16v &s, f16v &nx,
                                           f16v (&o)[4], float &m, float &ref, float &l, RawBlock &r,
@@ -270,12 +269,14 @@ __device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const
       o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[i & 1], pt[i >> 2][k], o[i & 3], 0, 0, 0);
     if (i < 6) vop[i & 1] = v_operand(vt, i + 2);
     // (4-bit integers take twice as long as their conversion)
-    if ((i & 1) == 0) {
-      u = ints8<M>(b, i >> 1);
+    constexpr int kPer = 8 / GROUPS;                       // products per group
+    const int j = G0 + i / kPer;
+    if (i % kPer == 0) {
+      u = ints8<M>(b, j);
       if constexpr (M != 4) first = four<M>(u.b0, sc);
-    } else {
+    } else if (i % kPer == kPer / 2) {
       if constexpr (M == 4) first = four<M>(u.b0, sc);
-      *(bf8 *)(to + 16 * (i >> 1)) = both(first, four<M>(u.b1, sc));
+      *(bf8 *)(to + 16 * j) = both(first, four<M>(u.b1, sc));
     }
   }
   __builtin_amdgcn_sched_barrier(0);
@@ -283,22 +284,26 @@ __device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const
 
 // The steps v0 .. v1 - 1 of a tile, for a wave whose block has M bits.  One barrier
 // per step: behind it K's unit v and V's unit v are in LDS, and nobody reads the
-// other buffers any more, which take the units v + 1 meanwhile.  `live`: the wave
-// has query rows (one that has none only dequantizes).
-template <bool F32, int M>
+// other buffers any more, which take the units v + 1 meanwhile.  Four waves dequantize
+// a block of K and one of V each, of eight the first four one of K, the others one of V
+// (job: which).  `live`: the wave has query rows (one that has none only dequantizes).
+template <bool F32, int NW, int M>
 __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader &ld, int v0, int v1,
-                                           bool live, const TileRow &w, const bf8 (&qop)[8],
+                                           bool job_k, bool live, const TileRow &w, const bf8 (&qop)[8],
                                            uint8_t *lds, f16v (&o)[4], float &m, float &l) {
   const int lane = ld.lane, h = lane >> 5, n = lane & 15;
   // where this lane reads K's and V's operands and writes its blocks
   const int kr = (lane & 31) * kKRow + 16 * h;
   const int vr = kKBytes + (4 * h + (n >> 2)) * kVRow + 32 * (lane >> 4 & 1) + 8 * (n & 3);
   const int kw = lane * kKRow + 64 * ld.blk, vw = kKBytes + lane * kVRow + 64 * ld.blk;
-  RawBlock rk, rv;
-  uint32_t ek, ev;
-  bool gk, gv;                                             // (false: the page is outside the pool)
-  auto load_k = [&](int v, int page) { gk = ld.template load<M>(a.k_mant, a.k_exp, v, true, page, rk, ek); };
-  auto load_v = [&](int v, int page) { gv = ld.template load<M>(a.v_mant, a.v_exp, v, false, page, rv, ev); };
+  const bool k1 = NW == 4 || job_k;                        // the first block's job
+  const int w1 = k1 ? kw : vw;
+  RawBlock r1, r2;
+  uint32_t e1, e2;
+  bool g1, g2;                                             // (false: the page is outside the pool)
+  const uint8_t *const m1 = k1 ? a.k_mant : a.v_mant, *const x1 = k1 ? a.k_exp : a.v_exp;
+  auto load_1 = [&](int v, int page) { g1 = ld.template load<M>(m1, x1, v, k1, page, r1, e1); };
+  auto load_2 = [&](int v, int page) { g2 = ld.template load<M>(a.v_mant, a.v_exp, v, false, page, r2, e2); };
   auto put = [&](RawBlock &r, uint32_t E, bool good, uint8_t *to) {
     store_block<M>(r, (int)E, to);
     store_rest<M>(r, E, good, to);
@@ -306,20 +311,23 @@ __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader 
   // K's units v0 - 1 (its second half is the first step's first) and v0, V's unit v0,
   // all their loads in flight together, then those of the units v0 + 1
   uint8_t *cur = lds, *nxt = lds + kStage;
-  int pk = ld.page(v0, true), pv = ld.page(v0, false);
-  const int p1 = ld.page(v0 - 1, true), p2 = ld.page(v0 + 1, true), p3 = ld.page(v0 + 1, false);
-  RawBlock r1;
-  uint32_t e1;
-  const bool g1 = ld.template load<M>(a.k_mant, a.k_exp, v0 - 1, true, p1, r1, e1);
-  load_k(v0, pk);
-  load_v(v0, pv);
-  pk = ld.page(v0 + 2, true);
-  pv = ld.page(v0 + 2, false);
-  put(r1, e1, g1, nxt + kw);
-  put(rk, ek, gk, cur + kw);
-  load_k(v0 + 1, p2);
-  put(rv, ev, gv, cur + vw);
-  load_v(v0 + 1, p3);
+  int n1 = ld.page(v0, k1), n2 = NW == 4 ? ld.page(v0, false) : 0;
+  const int p0 = ld.page(v0 - 1, true), p1 = ld.page(v0 + 1, k1), p2 = NW == 4 ? ld.page(v0 + 1, false) : 0;
+  RawBlock r0;
+  uint32_t e0 = 0;
+  bool g0 = true;
+  if (k1) g0 = ld.template load<M>(a.k_mant, a.k_exp, v0 - 1, true, p0, r0, e0);
+  load_1(v0, n1);
+  if constexpr (NW == 4) load_2(v0, n2);
+  n1 = ld.page(v0 + 2, k1);
+  if constexpr (NW == 4) n2 = ld.page(v0 + 2, false);
+  if (k1) put(r0, e0, g0, nxt + kw);
+  put(r1, e1, g1, cur + w1);
+  load_1(v0 + 1, p1);
+  if constexpr (NW == 4) {
+    put(r2, e2, g2, cur + vw);
+    load_2(v0 + 1, p2);
+  }
   __syncthreads();
   f16v s, nx;
   float ref = 0.f;
@@ -328,29 +336,37 @@ __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader 
     const int t0 = (v < ld.st.pre ? v : v + ld.st.shift) * kTok;
     __syncthreads();
     if (live) {
-      half_step<F32, M>(w, t0, h, qop, cur + kr, cur + vr, s, nx, o, m, ref, l, rk, ek, nxt + kw);
-      half_step<F32, M>(w, t0 + 32, h, qop, cur + kr + 32 * kKRow, cur + vr + 32 * kVRow, nx, s, o, m, ref, l,
-                        rv, ev, nxt + vw);
+      const uint8_t *const k2 = cur + kr + 32 * kKRow, *const v2 = cur + vr + 32 * kVRow;
+      if constexpr (NW == 4) {
+        half_step<F32, M, 0, 4>(w, t0, h, qop, cur + kr, cur + vr, s, nx, o, m, ref, l, r1, e1, nxt + kw);
+        half_step<F32, M, 0, 4>(w, t0 + 32, h, qop, k2, v2, nx, s, o, m, ref, l, r2, e2, nxt + vw);
+      } else {
+        half_step<F32, M, 0, 2>(w, t0, h, qop, cur + kr, cur + vr, s, nx, o, m, ref, l, r1, e1, nxt + w1);
+        half_step<F32, M, 2, 2>(w, t0 + 32, h, qop, k2, v2, nx, s, o, m, ref, l, r1, e1, nxt + w1);
+      }
     } else {
-      store_block<M>(rk, (int)ek, nxt + kw);
-      store_block<M>(rv, (int)ev, nxt + vw);
+      store_block<M>(r1, (int)e1, nxt + w1);
+      if constexpr (NW == 4) store_block<M>(r2, (int)e2, nxt + vw);
     }
-    store_rest<M>(rk, ek, gk, nxt + kw);
-    store_rest<M>(rv, ev, gv, nxt + vw);
-    load_k(v + 2, pk);
-    load_v(v + 2, pv);
-    pk = ld.page(v + 3, true);
-    pv = ld.page(v + 3, false);
+    store_rest<M>(r1, e1, g1, nxt + w1);
+    load_1(v + 2, n1);
+    n1 = ld.page(v + 3, k1);
+    if constexpr (NW == 4) {
+      store_rest<M>(r2, e2, g2, nxt + vw);
+      load_2(v + 2, n2);
+      n2 = ld.page(v + 3, false);
+    }
     uint8_t *const swap = cur;
     cur = nxt;
     nxt = swap;
   }
 }
 
-template <bool F32>
-__global__ __launch_bounds__(64 * kWaves, 2)
+template <bool F32, int NW>
+__global__ __launch_bounds__(64 * NW, 2)
 void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage];         // K and V of two steps
+  constexpr int kRows = 32 * NW;
   const PageGeo &g = a.geo;
   const int t = threadIdx.x, lane = t & 63, h = lane >> 5, x = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -413,10 +429,13 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   if (v0 < v1) {
+    // (of eight waves, two on a SIMD: a wide block of K goes with a narrow one of V)
+    const bool job_k = wave < 4;
+    const int blk = job_k ? wave : 7 - wave;
     Loader ld;
     ld.pages = a.table + (int64_t)q.s * a.ld_table;
-    ld.blk = wave;
-    ld.plane = (int64_t)pick(g.off, wave) << g.lg_page;
+    ld.blk = blk;
+    ld.plane = (int64_t)pick(g.off, blk) << g.lg_page;
     ld.page_rows = (uint32_t)Hkv << g.lg_page;
     ld.head_rows = (uint32_t)kvh << g.lg_page;
     ld.lane = lane;
@@ -426,11 +445,11 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
     ld.n_pages = (int)g.pages;
     ld.st = st;
     ld.v1 = v1;
-    const int bm = pick(g.m, wave);
-    if (bm == 4) tile_steps<F32, 4>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
-    else if (bm == 8) tile_steps<F32, 8>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
-    else if (bm == 6) tile_steps<F32, 6>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
-    else tile_steps<F32, 3>(a, ld, v0, v1, live, w, qop, lds, o, m, l);
+    const int bm = pick(g.m, blk);
+    if (bm == 4) tile_steps<F32, NW, 4>(a, ld, v0, v1, job_k, live, w, qop, lds, o, m, l);
+    else if (bm == 8) tile_steps<F32, NW, 8>(a, ld, v0, v1, job_k, live, w, qop, lds, o, m, l);
+    else if (bm == 6) tile_steps<F32, NW, 6>(a, ld, v0, v1, job_k, live, w, qop, lds, o, m, l);
+    else tile_steps<F32, NW, 3>(a, ld, v0, v1, job_k, live, w, qop, lds, o, m, l);
   }
   if (wr + x >= rows) return;
   l += other_half(l);
@@ -574,24 +593,43 @@ void launch_merge(const AttnPagedArgs &a, int splits, int few_rows, int most, hi
                      splits, few_rows, most, count);
 }
 
-int64_t tile_numbers(const AttnPagedArgs &a) { return a.T * a.G / kRows + a.S; }
+int64_t tile_numbers(const AttnPagedArgs &a, int waves) { return a.T * a.G / (32 * waves) + a.S; }
 
-// Splits of each kernel (0 where it is not launched), and the groups of 16 query
-// rows that the kernel for few rows takes.
+// Which kernels run, and their splits (0: not launched).  Times in us, 64 query and 8
+// KV heads, 4-bit cache, 256 CUs.
 struct Plan {
-  int tile, few, groups;
+  int tile, few;
+  int waves;                             // of a tile
+  int groups;                            // of 16 query rows, of the kernel for few
 };
 Plan plan_of(const AttnPagedArgs &a) {
-  Plan p = {0, 0, 1};
-  const int64_t Hkv = a.geo.Hkv, most = a.max_q * a.G;
+  Plan p = {0, 0, 4, 1};
+  const int64_t Hkv = a.geo.Hkv, most = a.max_q * a.G, cus = device_cu_count();
+  const bool even = a.T == a.S * a.max_q;                  // every sequence has max_q rows
   auto split = [](int64_t wgs, int64_t want, int64_t steps, int64_t least) {
     const int64_t n = std::min(want / std::max<int64_t>(wgs, 1), steps / least);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
+    return std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
   };
-  if (most > kFewMost) p.tile = split(tile_numbers(a) * Hkv, 1024, (a.max_kv + kTok - 1) / kTok, 4);
-  // (every sequence has max_q rows where their sum says so)
-  if (!p.tile || (a.G <= kFewMost && a.T < a.S * a.max_q)) {
-    p.few = split(a.S * Hkv, 512, (a.max_kv + kFewChunk - 1) / kFewChunk, 4);
+  if (most > kFewMost) {
+    // Eight waves share the dequantization of K and V among twice the rows, but are
+    // one workgroup per CU: they need a tile for each (2048 rows over 16384 tokens,
+    // 512 tiles, 1017 us against 1125 with four waves; 1024 rows, 256 tiles, 537
+    // against 595; 512 rows, 363 against 349; 40 rows of 4 sequences over 8192, 100
+    // against 91).
+    p.waves = a.T * a.G / 256 * Hkv >= cus ? 8 : 4;
+    const int64_t rows = 32 * p.waves;
+    const int64_t tiles = even ? a.S * ((most + rows - 1) / rows) : a.T * a.G / rows + 1;
+    // one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of at
+    // least four steps each
+    p.tile = (int)split(tiles * Hkv, p.waves == 8 ? cus : 2 * cus, (a.max_kv + kTok - 1) / kTok, 4);
+  }
+  // (in a mixed batch the two kernels share the sequences between them)
+  if (!p.tile || (a.G <= kFewMost && !even)) {
+    const int64_t chunks = (a.max_kv + kFewChunk - 1) / kFewChunk;
+    // One round of workgroups; two where each keeps 1024 tokens, since the lengths of a
+    // batch differ (32 sequences of 2048 to 8192 tokens: 61.6 and 52.9; 16 of 4096:
+    // 23.6 and 25.2 with 512 tokens each).
+    p.few = (int)std::max(split(a.S * Hkv, 2 * cus, chunks, 4), split(a.S * Hkv, 4 * cus, chunks, 32));
     p.groups = (p.tile ? a.G : most) <= 16 ? 1 : 2;
   }
   return p;
@@ -609,13 +647,13 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   AttnPagedArgs a = args;
   const Plan p = plan_of(a);
   a.parts = std::max(p.tile, p.few);
-  const int64_t numbers = tile_numbers(a);
+  const int64_t numbers = tile_numbers(a, p.waves);
   const int64_t wgs = numbers * a.geo.Hkv * p.tile;
   const int few_rows = p.few ? 16 * p.groups : 0;          // what the tiles leave to the other kernel
   const int most = (int)std::min<int64_t>(a.max_q, few_rows / a.G);
   // (a dispatch holds fewer than 2^32 threads)
   const int64_t merged = std::max(p.tile > 1 ? a.T * a.Hq : 0, p.few > 1 ? a.S * most * a.Hq : 0);
-  if (std::max({wgs, a.S * a.geo.Hkv * p.few, merged}) >= ((int64_t)1 << 32) / 256)
+  if (std::max({wgs, a.S * a.geo.Hkv * p.few, merged}) >= ((int64_t)1 << 32) / 512)
     return hipErrorInvalidValue;
   if (p.few) {
     const hipError_t e = a.o_f32 ? launch_attn_few_f32(a, p.few, p.groups, s)
@@ -624,8 +662,10 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
     if (p.few > 1) launch_merge(a, p.few, few_rows, most, s);
   }
   if (p.tile) {
-    const auto fn = a.o_f32 ? attn_tile_kernel<true> : attn_tile_kernel<false>;
-    hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(64 * kWaves), 0, s, a, p.tile, numbers, few_rows);
+    const auto fn = p.waves == 4 ? (a.o_f32 ? attn_tile_kernel<true, 4> : attn_tile_kernel<false, 4>)
+                                 : (a.o_f32 ? attn_tile_kernel<true, 8> : attn_tile_kernel<false, 8>);
+    hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3((unsigned)(64 * p.waves)), 0, s, a, p.tile, numbers,
+                       few_rows);
     if (p.tile > 1) launch_merge(a, p.tile, few_rows, 0, s);
   }
   return hipGetLastError();

@@ -322,7 +322,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] = weight<F32>(fmaf(x[i], scale, -ref[e]));
-        l[e] += x[i];
+        if constexpr (F32) l[e] += x[i];
       }
 #pragma unroll
       for (int k = 0; k < kTerms; ++k)
@@ -331,6 +331,12 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
           pt[e][k][i] = (__bf16)x[i];
           if constexpr (F32) x[i] -= (float)pt[e][k][i];
         }
+      if constexpr (!F32) {                                // the sum of what the values are weighted with
+#pragma unroll
+        for (int i = 0; i < 8; i += 2)
+          l[e] = __builtin_amdgcn_fdot2_f32_bf16(bf2{pt[e][0][i], pt[e][0][i + 1]},
+                                                 bf2{(__bf16)1.f, (__bf16)1.f}, l[e], false);
+      }
     }
     const uint8_t *vp = vs + (4 * gr + (n >> 2)) * kRowBytes + 8 * (n & 1);
     const int sw = few_swizzle(4 * gr + (n >> 2)), col = (n & 3) >> 1;

@@ -244,11 +244,11 @@ __device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const
     if (i < 6) kop[i & 1] = k_operand(next_rows, i + 2);
     else vop[i & 1] = v_operand(vt, i - 6);
     float e0 = weight<F32>(fmaf(s[2 * i], scale, -ref)), e1 = weight<F32>(fmaf(s[2 * i + 1], scale, -ref));
-    l += e0;
-    l += e1;
+    if constexpr (F32) l += e0 + e1;
 #pragma unroll
     for (int k = 0; k < kTerms; ++k) {
       const bf2 y = {(__bf16)e0, (__bf16)e1};
+      if constexpr (!F32) l = __builtin_amdgcn_fdot2_f32_bf16(y, bf2{(__bf16)1.f, (__bf16)1.f}, l, false);
       pt[i >> 2][k][2 * (i & 3)] = y[0];
       pt[i >> 2][k][2 * (i & 3) + 1] = y[1];
       if constexpr (F32) {
@@ -489,31 +489,33 @@ template <bool F32, int GROUPS>
 __global__ __launch_bounds__(kMergeThreads)
 void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int64_t count) {
   constexpr int kRowsHere = kMergeThreads / 32 / GROUPS;
-  __shared__ __attribute__((aligned(16))) float po[GROUPS > 1 ? GROUPS : 1][kD];
-  __shared__ float pm[GROUPS], pl[GROUPS];
-  const int t = threadIdx.x, c = t & 31, grp = (t >> 5) % GROUPS;
+  __shared__ __attribute__((aligned(16))) float pos[GROUPS > 1 ? kMergeThreads / 32 : 1][kD];
+  __shared__ float pms[kMergeThreads / 32], pls[kMergeThreads / 32];
+  const int t = threadIdx.x, c = t & 31, grp = (t >> 5) % GROUPS, first = (t >> 5) - grp;
   const int64_t id = (int64_t)blockIdx.x * kRowsHere + (t >> 5) / GROUPS;
-  if (id >= count) return;                                 // (uniform where the groups meet)
-  int64_t row = id;
-  if (most > 0) {                                          // row id % (most Hq) of a short sequence
+  bool here = id < count;                                  // (all meet at the barrier)
+  int64_t row = here ? id : 0;
+  if (!here) {
+  } else if (most > 0) {                                   // row id % (most Hq) of a short sequence
     const int64_t per = most * a.Hq;
     const int s = (int)(id / per), c0 = a.cu_q[s], n = a.cu_q[s + 1] - c0;
     const int64_t r = id - s * per;
-    if (r >= n * a.Hq || n * (int64_t)a.G > few_rows || c0 < 0 || c0 + (int64_t)n > a.T) return;
-    row = c0 * a.Hq + r;
+    here = r < n * a.Hq && n * (int64_t)a.G <= few_rows && c0 >= 0 && c0 + (int64_t)n <= a.T;
+    row = here ? c0 * a.Hq + r : 0;
   } else {
     const int tok = (int)(row / a.Hq);
-    if (tok < a.cu_q[0] || tok >= a.cu_q[a.S]) return;     // no sequence's row
-    if (few_rows > 0) {                                    // the other kernel's rows
+    here = tok >= a.cu_q[0] && tok < a.cu_q[a.S];          // else no sequence's row
+    if (here && few_rows > 0) {                            // not the other kernel's rows
       int lo = 0, hi = (int)a.S - 1;                       // the last sequence that begins at tok or before
       while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
         if (a.cu_q[mid] <= tok) lo = mid;
         else hi = mid - 1;
       }
-      if ((int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G <= few_rows) return;
+      here = (int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G > few_rows;
     }
   }
+  if (!here) splits = 0;
   const float ninf = -__builtin_inff();
   float M = ninf, L = 0.f;
   f4 O = {0.f, 0.f, 0.f, 0.f};
@@ -550,13 +552,15 @@ void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int6
     }
   }
   if constexpr (GROUPS > 1) {
-    *(f4 *)(po[grp] + 4 * c) = O;
+    *(f4 *)(pos[t >> 5] + 4 * c) = O;
     if (c == 0) {
-      pm[grp] = M;
-      pl[grp] = L;
+      pms[t >> 5] = M;
+      pls[t >> 5] = L;
     }
+  }
+  if constexpr (GROUPS > 1) {
     __syncthreads();
-    if (grp > 0) return;
+    const float(*po)[kD] = pos + first, *pm = pms + first, *pl = pls + first;
     float Mx = ninf, Ls[GROUPS];
     f4 Os[GROUPS];
 #pragma unroll
@@ -577,6 +581,7 @@ void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int6
     L = Ls[0];
     O = Os[0];
   }
+  if (!here || grp > 0) return;
   O *= L == 0.f ? 0.f : 1.f / L;
   if (F32) *(f4 *)((float *)a.o + row * kD + 4 * c) = O;
   else *(bf4 *)((uint16_t *)a.o + row * kD + 4 * c) =
@@ -586,11 +591,15 @@ void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int6
 // The rows of the tiles (most 0), or up to `most` rows of every short sequence.
 void launch_merge(const AttnPagedArgs &a, int splits, int few_rows, int most, hipStream_t s) {
   const int64_t count = most > 0 ? a.S * most * a.Hq : a.T * a.Hq;
-  const bool few = splits <= kBatch;
-  const auto fn = few ? (a.o_f32 ? attn_merge_kernel<true, 1> : attn_merge_kernel<false, 1>)
-                      : (a.o_f32 ? attn_merge_kernel<true, 8> : attn_merge_kernel<false, 8>);
-  hipLaunchKernelGGL(fn, dim3((unsigned)(few ? (count + 7) / 8 : count)), dim3(kMergeThreads), 0, s, a,
-                     splits, few_rows, most, count);
+  // as many groups as the splits fill with one batch each (6880 rows of 9 splits: eight
+  // groups 23.9 us, two 7)
+  auto go = [&](auto fn, int groups) {
+    hipLaunchKernelGGL(fn, dim3((unsigned)((count * groups + 7) / 8)), dim3(kMergeThreads), 0, s, a, splits,
+                       few_rows, most, count);
+  };
+  if (splits <= kBatch) go(a.o_f32 ? attn_merge_kernel<true, 1> : attn_merge_kernel<false, 1>, 1);
+  else if (splits <= 2 * kBatch) go(a.o_f32 ? attn_merge_kernel<true, 2> : attn_merge_kernel<false, 2>, 2);
+  else go(a.o_f32 ? attn_merge_kernel<true, 8> : attn_merge_kernel<false, 8>, 8);
 }
 
 int64_t tile_numbers(const AttnPagedArgs &a, int waves) { return a.T * a.G / (32 * waves) + a.S; }

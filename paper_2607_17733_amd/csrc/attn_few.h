@@ -20,11 +20,11 @@ namespace mxq {
 namespace {
 
 constexpr int kFewWaves = 4;
-// LDS rows of a wave's 32 dequantized V tokens: chunk c (16 bytes) of token t at c ^
-// swizzle: eight tokens' writes of one chunk, and a transposing read's eight tokens
-// of two adjacent chunks, lie in distinct banks.
-constexpr int kFewBytes = kFewChunk * kRowBytes;
-__device__ inline int few_swizzle(int t) { return 2 * (t & 7) + ((t >> 3) & 1); }
+// LDS rows of a wave's 32 dequantized V tokens: the stride puts the rows of eight lanes'
+// 16-byte writes, and of a transposing read, into distinct banks, and every access is
+// a base plus a constant.
+constexpr int kFewRow = kRowBytes + 32;
+constexpr int kFewBytes = kFewChunk * kFewRow;
 
 // The widths of a row's blocks: N3 3-bit, N4 4-bit, N6 6-bit and N8 8-bit blocks, in
 // that order.  Rows of one width are read a block per lane (lane group g: block g,
@@ -54,41 +54,54 @@ struct RawRow {
   uint32_t ex;
 };
 
-// `plane` points at the page's first token, `i` is the token.
+// A lane's place in the planes of a page, for the page's token i + n: at[j] + 4 m_j i
+// (rows of one width: at[0]).
+template <class Mx>
+struct Place {
+  uint32_t at[4];
+};
+template <class Mx>
+__device__ __forceinline__ Place<Mx> place_of(int lg_page, int g, int n) {
+  Place<Mx> p;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    constexpr int kM0 = Mx::width(0);
+    const int m = Mx::width(j);
+    p.at[j] = Mx::kUniform ? ((uint32_t)(4 * kM0 * g) << lg_page) + n * 4 * kM0
+                           : ((uint32_t)Mx::off(j) << lg_page) + n * 4 * m +
+                                 (m == 8 ? 8 * g : m == 3 ? ((3 * g) & ~3) : 4 * g);
+  }
+  return p;
+}
+// `page`: the page's first token of the head, with 16 tokens from token i on.
 template <class Mx, int J>
-__device__ __forceinline__ void load_group(const uint8_t *page, int lg_page, uint32_t i, int g,
+__device__ __forceinline__ void load_group(const uint8_t *page, uint32_t i, const Place<Mx> &pl, int g,
                                            RawRow<Mx> &r) {
   constexpr int M = Mx::width(J), S = Mx::start(J);
-  const uint8_t *p = page + (((uint32_t)Mx::off(J) << lg_page) + i * (4 * M));
-  if constexpr (M == 4) {
-    r.w[S] = *(const uint32_t *)(p + 4 * g);
-  } else if constexpr (M == 6) {
-    r.w[S] = *(const uint32_t *)(p + 4 * g);
-    r.w[S + 1] = *(const uint32_t *)(p + 16 + 4 * (g >> 1));
+  const uint8_t *p = page + i * (4 * M) + pl.at[J];
+  r.w[S] = *(const uint32_t *)p;
+  if constexpr (M == 6) {                // low nibbles, and the half block's top bits
+    r.w[S + 1] = *(const uint32_t *)(page + i * (4 * M) + pl.at[J] + 16 - 4 * g + 4 * (g >> 1));
   } else if constexpr (M == 8) {
-    const u2 a = *(const u2 *)(p + 8 * g);
-    r.w[S] = a[0];
-    r.w[S + 1] = a[1];
-  } else {                               // bytes 3 g .. 3 g + 2 of twelve
-    const int at = (3 * g) & ~3;
-    r.w[S] = *(const uint32_t *)(p + at);
-    r.w[S + 1] = *(const uint32_t *)(p + (at < 8 ? at + 4 : 8));
+    r.w[S + 1] = *(const uint32_t *)(p + 4);
+  } else if constexpr (M == 3) {         // bytes 3 g .. 3 g + 2 of twelve
+    r.w[S + 1] = *(const uint32_t *)(p + (g < 3 ? 4 : 0));
   }
 }
 template <class Mx>
-__device__ __forceinline__ void load_row(const uint8_t *page, int lg_page, uint32_t i, int g,
+__device__ __forceinline__ void load_row(const uint8_t *page, uint32_t i, const Place<Mx> &pl, int g,
                                          RawRow<Mx> &r) {
   if constexpr (Mx::kUniform) {
     constexpr int M = Mx::width(0);
     RawBlock b;
-    load_block<M>(page + ((((uint32_t)(4 * M * g)) << lg_page) + i * (4 * M)), b);
+    load_block<M>(page + i * (4 * M) + pl.at[0], b);
 #pragma unroll
     for (int k = 0; k < M; ++k) r.w[k] = b.w[k];
   } else {
-    load_group<Mx, 0>(page, lg_page, i, g, r);
-    load_group<Mx, 1>(page, lg_page, i, g, r);
-    load_group<Mx, 2>(page, lg_page, i, g, r);
-    load_group<Mx, 3>(page, lg_page, i, g, r);
+    load_group<Mx, 0>(page, i, pl, g, r);
+    load_group<Mx, 1>(page, i, pl, g, r);
+    load_group<Mx, 2>(page, i, pl, g, r);
+    load_group<Mx, 3>(page, i, pl, g, r);
   }
 }
 
@@ -148,10 +161,15 @@ struct Chunk {
   bool hole[2];
 };
 
-// NC: groups of 16 query rows.  Two sets of a chunk's registers leave room for three
-// waves per SIMD with one group and rows of at most seven words a lane, else for two.
+// Waves per SIMD that two sets of a chunk's registers leave room for, by the groups of
+// 16 query rows and a lane's words of a row.
+constexpr int few_waves(int groups, int words) {
+  return groups > 1 || words > 6 ? 2 : words > 4 ? 3 : 4;
+}
+
+// NC: groups of 16 query rows.
 template <bool F32, class Mx, int NC>
-__global__ __launch_bounds__(64 * kFewWaves, NC == 1 && Mx::kWords <= 7 ? 3 : 2)
+__global__ __launch_bounds__(64 * kFewWaves, few_waves(NC, Mx::kWords))
 void attn_few_kernel(AttnPagedArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) uint8_t pool[kFewWaves][kFewBytes];
   __shared__ float mm[kFewWaves][16 * NC], ml[kFewWaves][16 * NC];
@@ -171,12 +189,16 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   const int v0 = (int)((int64_t)st.count * split / splits);
   const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
 
-  // A chunk's halves of 16 tokens lie in one page each.  Tokens past the last are
-  // the last one (weight 0), a half past the last token is the chunk's first.
+  // A chunk's halves of 16 tokens lie in one page each (a half past the last token is
+  // the chunk's first).  Places past the last token are read too, they are the page's
+  // own, and are cleared where they are used.
   const int32_t *pages = a.table + (int64_t)s * a.ld_table;
   const int page_mask = (1 << g.lg_page) - 1, last = q.len - 1;
   // (past the last chunk: the last one)
-  auto first_of = [&](int v) { return (min(v, v1 - 1) < st.pre ? min(v, v1 - 1) : min(v, v1 - 1) + st.shift) * kFewChunk; };
+  auto first_of = [&](int v) {
+    const int u = min(v, v1 - 1);
+    return (u < st.pre ? u : u + st.shift) * kFewChunk;
+  };
   auto half_of = [&](int t0, int mt) { return t0 + 16 * mt <= last ? t0 + 16 * mt : t0; };
   int pg[2];
   auto number = [&](int v) __attribute__((always_inline)) {
@@ -185,6 +207,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
     for (int mt = 0; mt < 2; ++mt) pg[mt] = pages[half_of(t0, mt) >> g.lg_page];
   };
   const uint32_t page_rows = Hkv << g.lg_page;             // rows of a page, below 2^26
+  const Place<Mx> place = place_of<Mx>(g.lg_page, gr, n);
   auto fetch = [&](int v, Chunk<Mx> &c) __attribute__((always_inline)) {
     const int t0 = first_of(v);
 #pragma unroll
@@ -192,12 +215,12 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
       c.hole[mt] = (uint32_t)pg[mt] >= (uint32_t)g.pages;
       const uint32_t page = c.hole[mt] ? 0u : (uint32_t)pg[mt];
       const int64_t run = (int64_t)((uint64_t)page * page_rows + ((uint32_t)kvh << g.lg_page));
-      const uint32_t i = (uint32_t)(min(half_of(t0, mt) + n, last) & page_mask);
+      const uint32_t i = (uint32_t)(half_of(t0, mt) & page_mask);
       const int64_t at = run * g.row;
-      load_row<Mx>(a.k_mant + at, g.lg_page, i, gr, c.k[mt]);
-      load_row<Mx>(a.v_mant + at, g.lg_page, i, gr, c.v[mt]);
-      c.k[mt].ex = *(const uint32_t *)(a.k_exp + run * 4 + 4 * i);
-      c.v[mt].ex = *(const uint32_t *)(a.v_exp + run * 4 + 4 * i);
+      load_row<Mx>(a.k_mant + at, i, place, gr, c.k[mt]);
+      load_row<Mx>(a.v_mant + at, i, place, gr, c.v[mt]);
+      c.k[mt].ex = *(const uint32_t *)(a.k_exp + (run + i) * 4 + 4 * n);
+      c.v[mt].ex = *(const uint32_t *)(a.v_exp + (run + i) * 4 + 4 * n);
     }
   };
   Chunk<Mx> c0, c1;
@@ -239,6 +262,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
     for (int dt = 0; dt < 8; ++dt) o[c][dt] = f4{0.f, 0.f, 0.f, 0.f};
   }
   uint8_t *vs = pool[wave];
+  uint8_t *const vw = vs + n * kFewRow + 2 * Mx::value(gr, 0);
+  const uint8_t *const vr = vs + (4 * gr + (n >> 2)) * kFewRow + 8 * (n & 3);
 
   auto compute = [&](int v, Chunk<Mx> &c) __attribute__((always_inline)) {
     const int t0 = first_of(v);
@@ -249,6 +274,11 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
         for (int k = 0; k < Mx::kWords; ++k) c.k[mt].w[k] = c.v[mt].w[k] = 0u;
         c.k[mt].ex = c.v[mt].ex = 0u;
       }
+    if (t0 + kFewChunk > q.len) {                          // places past the last token: tiny values
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+        if (t0 + 16 * mt + n > last) c.k[mt].ex = c.v[mt].ex = 0u;
+    }
     const bool big = __any((big_bits(c.k[0].ex) | big_bits(c.k[1].ex) | big_bits(c.v[0].ex) |
                             big_bits(c.v[1].ex)) != 0);
     // scores: tokens 16 mt + 4 gr + i of row n
@@ -272,7 +302,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
       dequant_row(c.v[mt], gr, big, w);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *(bf8 *)(vs + (16 * mt + n) * kRowBytes + 16 * ((Mx::value(gr, j) >> 3) ^ few_swizzle(n))) = w[j];
+        *(bf8 *)(vw + 16 * mt * kFewRow + 2 * (Mx::value(0, j) - Mx::value(0, 0))) = w[j];
     }
     wave_sync();
     constexpr int kTerms = F32 ? 3 : 1;
@@ -338,13 +368,10 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
                                                  bf2{(__bf16)1.f, (__bf16)1.f}, l[e], false);
       }
     }
-    const uint8_t *vp = vs + (4 * gr + (n >> 2)) * kRowBytes + 8 * (n & 1);
-    const int sw = few_swizzle(4 * gr + (n >> 2)), col = (n & 3) >> 1;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
-      const uint8_t *at = vp + 16 * ((2 * dt + col) ^ sw);
-      const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)at);
-      const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(at + 16 * kRowBytes));
+      const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(vr + 32 * dt));
+      const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4 *)(vr + 32 * dt + 16 * kFewRow));
       const bf8 vv = __builtin_bit_cast(bf8, (s8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int e = 0; e < NC; ++e)

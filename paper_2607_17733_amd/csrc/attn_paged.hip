@@ -105,6 +105,7 @@ __device__ inline bool find_seq(const AttnPagedArgs &a, int64_t number, int rows
 struct TileRow {
   int p;                                 // the row's position
   int pw0, pw1;                          // the wave's first and last
+  int last;                              // the last token that one of the wave's rows may see
   int window, len, pre;
   float sc, slope, softcap;
   bool biased;
@@ -144,8 +145,14 @@ __device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s
   }
   if (w.biased) {
     const float rel = (float)(w.p - t0 - 4 * h);
+    if (t0 + 31 > w.pw0 && w.pre > 0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fmaf(-w.slope, fabsf(rel - (float)c(i)), s[i] * scale);
+      for (int i = 0; i < 16; ++i) s[i] = fmaf(-w.slope, fabsf(rel - (float)c(i)), s[i] * scale);
+    } else {                                               // (no token behind its row is visible)
+      const float near = -w.slope * rel;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale, fmaf(w.slope, (float)c(i), near));
+    }
     scale = 1.f;
   }
   // masks, where not every row of the wave sees all
@@ -286,7 +293,8 @@ __device__ __forceinline__ void half_step(const TileRow &w, int t0, int h, const
 // per step: behind it K's unit v and V's unit v are in LDS, and nobody reads the
 // other buffers any more, which take the units v + 1 meanwhile.  Four waves dequantize
 // a block of K and one of V each, of eight the first four one of K, the others one of V
-// (job: which).  `live`: the wave has query rows (one that has none only dequantizes).
+// (job_k: which).  `live`: the wave has query rows; where it has none, or none that see
+// the step, it only dequantizes.
 template <bool F32, int NW, int M>
 __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader &ld, int v0, int v1,
                                            bool job_k, bool live, const TileRow &w, const bf8 (&qop)[8],
@@ -335,7 +343,8 @@ __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader 
   for (int v = v0; v < v1; ++v) {
     const int t0 = (v < ld.st.pre ? v : v + ld.st.shift) * kTok;
     __syncthreads();
-    if (live) {
+    // (steps behind all of the wave's rows come last)
+    if (live && t0 <= w.last) {
       const uint8_t *const k2 = cur + kr + 32 * kKRow, *const v2 = cur + vr + 32 * kVRow;
       if constexpr (NW == 4) {
         half_step<F32, M, 0, 4>(w, t0, h, qop, cur + kr, cur + vr, s, nx, o, m, ref, l, r1, e1, nxt + kw);
@@ -396,6 +405,7 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   w.p = (int)(p0 + tok);
   w.pw0 = (int)(p0 + min(wr, rows - 1) / G);
   w.pw1 = (int)(p0 + (min(wr + 32, rows) - 1) / G);
+  w.last = max(w.pw1, q.pre - 1);
   w.window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
   w.len = q.len;
   w.pre = q.pre;
@@ -620,12 +630,12 @@ Plan plan_of(const AttnPagedArgs &a) {
     return std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
   };
   if (most > kFewMost) {
-    // Eight waves share the dequantization of K and V among twice the rows, but are
-    // one workgroup per CU: they need a tile for each (2048 rows over 16384 tokens,
-    // 512 tiles, 1017 us against 1125 with four waves; 1024 rows, 256 tiles, 537
-    // against 595; 512 rows, 363 against 349; 40 rows of 4 sequences over 8192, 100
-    // against 91).
-    p.waves = a.T * a.G / 256 * Hkv >= cus ? 8 : 4;
+    // Eight waves share the dequantization of K and V among twice the rows, but are one
+    // workgroup per CU: they need a tile for each (2048 rows over 16384 tokens, 512
+    // tiles, 1017 us against 1125 with four waves; 1024 rows, 256 tiles, 537 against
+    // 595; 512 rows, 363 against 349), and a tile that spans few tokens, whose rows see
+    // the same steps (one query head per KV head, 2 x 2048 tokens: 140 against 131).
+    p.waves = a.T * a.G / 256 * Hkv >= cus && a.G >= 4 ? 8 : 4;
     const int64_t rows = 32 * p.waves;
     const int64_t tiles = even ? a.S * ((most + rows - 1) / rows) : a.T * a.G / rows + 1;
     // one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of at

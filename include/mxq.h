@@ -526,9 +526,10 @@ typedef struct {
  * [T]).  y may be x itself with the same strides, else the two must not
  * overlap.  1 <= D <= 4096, D even; x and y 4-byte aligned, strides even.
  * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (negative counts, rot odd or out of
- * range, D < rot, positions out of range, non-finite frequencies or mscale),
- * MXQ_ERR_ALIGN (also for odd strides), MXQ_ERR_UNSUPPORTED (layout),
- * MXQ_ERR_DEVICE.  T == 0 or H == 0 enqueues nothing.
+ * range, D < rot, positions out of range, non-finite frequencies or mscale,
+ * T * H * D / 2 or positions * rot / 2 of 2^32 or more), MXQ_ERR_ALIGN (also for
+ * odd strides), MXQ_ERR_UNSUPPORTED (layout), MXQ_ERR_DEVICE.  T == 0 or H == 0
+ * enqueues nothing.
  */
 mxq_status mxq_rope_table(const double *inv_freq, int32_t rot, int64_t positions,
                           double mscale, float *table, void *stream);
@@ -583,7 +584,8 @@ int64_t mxq_kv_page_exp_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_toke
  * for, q * 2^(E - 127 - (m - 2)), which is exact, into k and v DEVICE bf16
  * [n][Hkv][128], 16-byte aligned (either may be NULL); zeros for a slot
  * outside the cache.
- * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, counts, page_tokens, rot),
+ * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, counts, page_tokens, rot, T / 16 *
+ * (2 Hkv + Hq) of 2^24 or more),
  * MXQ_ERR_UNSUPPORTED (a permutation, layout), MXQ_ERR_NULL, MXQ_ERR_ALIGN (also
  * for strides), MXQ_ERR_DEVICE.  T == 0 (n == 0) enqueues nothing.
  */
@@ -622,8 +624,8 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  *           aligned, strides multiples of 8.
  *   o       DEVICE [T][Hq][128], bf16 or, with o_f32, float32, 16-byte aligned.
  *   work    DEVICE, 16-byte aligned, work_bytes >= mxq_attn_paged_work_bytes:
- *           partial results; needs no initialisation.  Calls that may overlap
- *           in time must not share it.
+ *           partial results (the size is that of the current device); needs no
+ *           initialisation.  Calls that may overlap in time must not share it.
  * Every product is exact (bf16 query, bf16 K and V values), sums and softmax
  * statistics are float32.  For a float32 output the probabilities enter the
  * value product with all their 24 bits, for a bf16 one rounded to bf16; a
@@ -631,8 +633,8 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  * probabilities times values past float32's range is infinite.  Calls repeat
  * bit for bit.
  * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, bad counts, Hq not a multiple
- * of Hkv, Hq / Hkv > 64, non-finite scale or softcap, softcap < 0, window < 0,
- * a short work buffer); MXQ_ERR_UNSUPPORTED (a permutation); MXQ_ERR_NULL;
+ * of Hkv, Hq / Hkv > 64, T * Hq > 2^29, S * Hkv > 2^22, non-finite scale or
+ * softcap, softcap < 0 or in (0, 2^-60), window < 0, a short work buffer); MXQ_ERR_UNSUPPORTED (a permutation); MXQ_ERR_NULL;
  * MXQ_ERR_ALIGN; MXQ_ERR_DEVICE.  S == 0, T == 0 or max_q == 0 enqueues nothing.
  */
 typedef struct {

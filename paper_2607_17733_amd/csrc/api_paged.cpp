@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int64_t kD = 128;
+constexpr int64_t kMaxGrid = (1 << 24) - 1;   // workgroups of 256: fewer than 2^32 threads
 
 bool aligned(const void *p, unsigned n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
@@ -91,6 +92,8 @@ mxq_status attn_shape(const mxq_fmt *fmt, const mxq_paged_kv *c, int64_t S, int6
       max_q > INT32_MAX || max_kv > INT32_MAX)
     return MXQ_ERR_SHAPE;
   if (Hq < c->Hkv || Hq % c->Hkv || Hq / c->Hkv > 64) return MXQ_ERR_SHAPE;
+  // (a dispatch holds fewer than 2^32 threads)
+  if (T * Hq > (int64_t)1 << 29 || S * c->Hkv > (int64_t)1 << 22) return MXQ_ERR_SHAPE;
   a->S = S;
   a->T = T;
   a->Hq = Hq;
@@ -110,7 +113,7 @@ mxq_status mxq_rope_table(const double *inv_freq, int32_t rot, int64_t positions
   const mxq_rotary r = {table, positions, rot, MXQ_ROPE_HALVES};
   const mxq_status st = check_rotary(&r);
   if (st != MXQ_OK) return st;
-  if (!isfinite(mscale)) return MXQ_ERR_SHAPE;
+  if (!isfinite(mscale) || positions > kMaxGrid * 256 / (rot / 2)) return MXQ_ERR_SHAPE;
   for (int i = 0; i < rot / 2; ++i)
     if (!isfinite(inv_freq[i])) return MXQ_ERR_SHAPE;
   return launched(mxq::launch_rope_table(inv_freq, rot, positions, mscale, table,
@@ -129,8 +132,7 @@ mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_
   if (!aligned(x, 4) || !aligned(y, 4) || x_ts % 2 || x_hs % 2 || y_ts % 2 || y_hs % 2)
     return MXQ_ERR_ALIGN;
   if (x == y && (x_ts != y_ts || x_hs != y_hs)) return MXQ_ERR_SHAPE;
-  // (a dispatch holds fewer than 2^31 workgroups of 256)
-  if (T * H > ((int64_t)1 << 38) / (D / 2)) return MXQ_ERR_SHAPE;
+  if (T * H > kMaxGrid * 256 / (D / 2)) return MXQ_ERR_SHAPE;
   mxq::RopeRowsArgs a{};
   a.rope = rope_args(rope);
   a.x = x;
@@ -172,7 +174,7 @@ mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const ui
     if (rope->rot % 16 || rope->rot > kD) return MXQ_ERR_SHAPE;
   }
   if (T < 0 || T > INT32_MAX || Hq < 0 || Hq > 65535) return MXQ_ERR_SHAPE;
-  if ((T + 15) / 16 * (2 * cache->Hkv + Hq) > INT32_MAX) return MXQ_ERR_SHAPE;
+  if ((T + 15) / 16 * (2 * cache->Hkv + Hq) > kMaxGrid) return MXQ_ERR_SHAPE;
   if (T == 0) return MXQ_OK;
   if (!slots || (rope && !pos)) return MXQ_ERR_NULL;
   if ((st = check_rows(k, k_ts, k_hs)) != MXQ_OK) return st;
@@ -214,7 +216,8 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
   mxq::KvReadArgs a{};
   const mxq_status st = check_cache(fmt, cache, &a.geo);
   if (st != MXQ_OK) return st;
-  if (n < 0 || n > INT32_MAX || (n + 15) / 16 * 2 * cache->Hkv > INT32_MAX) return MXQ_ERR_SHAPE;
+  if (n < 0 || n > INT32_MAX || (n + 15) / 16 * 2 * cache->Hkv > kMaxGrid)
+    return MXQ_ERR_SHAPE;
   if (n == 0 || (!k && !v)) return MXQ_OK;
   if (!slots) return MXQ_ERR_NULL;
   if (!aligned(k, 16) || !aligned(v, 16)) return MXQ_ERR_ALIGN;
@@ -248,7 +251,7 @@ mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
       (batch->S > 1 && batch->ld_table < batch->table_pages))
     return MXQ_ERR_SHAPE;
   if (!isfinite(opts->scale) || !isfinite(opts->softcap) || opts->softcap < 0.f ||
-      opts->window < 0)
+      (opts->softcap > 0.f && opts->softcap < 0x1p-60f) || opts->window < 0)
     return MXQ_ERR_SHAPE;
   if (a.S == 0 || a.T == 0 || a.max_q == 0) return MXQ_OK;
   if (!batch->cu_q || !batch->kv_len || (batch->table_pages > 0 && !batch->table) || !o)

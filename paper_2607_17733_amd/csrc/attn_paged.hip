@@ -659,7 +659,8 @@ Plan plan_of(const AttnPagedArgs &a) {
 int64_t attn_paged_work(const AttnPagedArgs &a) {
   const Plan p = plan_of(a);
   const int n = std::max(p.tile, p.few);
-  return n <= 1 ? 0 : n * a.T * a.Hq * (kD + 2) * (int64_t)sizeof(float);
+  const int64_t rows = n * a.T * a.Hq;
+  return n <= 1 ? 0 : ((rows + 1) / 2 * 4 + rows * kD) * (int64_t)sizeof(float);
 }
 
 hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
@@ -670,10 +671,6 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   const int64_t wgs = numbers * a.geo.Hkv * p.tile;
   const int few_rows = p.few ? 16 * p.groups : 0;          // what the tiles leave to the other kernel
   const int most = (int)std::min<int64_t>(a.max_q, few_rows / a.G);
-  // (a dispatch holds fewer than 2^32 threads)
-  const int64_t merged = std::max(p.tile > 1 ? a.T * a.Hq : 0, p.few > 1 ? a.S * most * a.Hq : 0);
-  if (std::max({wgs, a.S * a.geo.Hkv * p.few, merged}) >= ((int64_t)1 << 32) / 512)
-    return hipErrorInvalidValue;
   if (p.few) {
     const hipError_t e = a.o_f32 ? launch_attn_few_f32(a, p.few, p.groups, s)
                                  : launch_attn_few_bf16(a, p.few, p.groups, s);

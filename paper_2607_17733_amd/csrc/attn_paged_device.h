@@ -234,14 +234,14 @@ __device__ inline Steps steps_of(const AttnPagedArgs &a, const Seq &q, int64_t p
   return st;
 }
 
-// Partial results of the splits: (maximum, sum) [parts][T Hq], then the unscaled
-// outputs [parts][T Hq][128], `parts` being the larger number of splits of the two
-// kernels.
+// Partial results of the splits: (maximum, sum) [parts][T Hq], padded to 16 bytes, then
+// the unscaled outputs [parts][T Hq][128], `parts` being the larger number of splits of
+// the two kernels.
 __device__ inline float *part_ml(const AttnPagedArgs &a, int split, int64_t row) {
   return a.work + (split * a.T * a.Hq + row) * 2;
 }
 __device__ inline float *part_o(const AttnPagedArgs &a, int split, int64_t row) {
-  return a.work + a.parts * a.T * a.Hq * 2 + (split * a.T * a.Hq + row) * kD;
+  return a.work + (a.parts * a.T * a.Hq + 1) / 2 * 4 + (split * a.T * a.Hq + row) * kD;
 }
 
 template <bool F32>

@@ -212,14 +212,12 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvReadArgs a) {
 
 hipError_t launch_kv_append(const KvAppendArgs &a, hipStream_t s) {
   const int64_t n = (a.T + kTokens - 1) / kTokens * (2 * a.geo.Hkv + a.Hq);
-  if (n > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvReadArgs &a, hipStream_t s) {
   const int64_t n = (a.n + kTokens - 1) / kTokens * ((a.k ? a.geo.Hkv : 0) + (a.v ? a.geo.Hkv : 0));
-  if (n > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kv_read_kernel, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }

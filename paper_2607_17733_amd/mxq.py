@@ -772,7 +772,11 @@ class PagedCache:
 
     def __init__(self, fmt: Format, Hkv: int, pages: int, page_tokens: int, device="cuda",
                  k=None, v=None):
-        self.fmt, self.Hkv = fmt, int(Hkv)
+        # (its own copy of the widths, which fix the buffers' sizes)
+        self.fmt = Format(fmt.K, np.array(fmt.widths), fmt.perm, ("rne", "rna")[fmt.round],
+                          ("sym", "full")[fmt.clamp])
+        self.fmt.widths.setflags(write=False)
+        fmt, self.Hkv = self.fmt, int(Hkv)
         self.pages, self.page_tokens = int(pages), int(page_tokens)
         L = lib()
         if not 16 <= self.page_tokens <= 1024:

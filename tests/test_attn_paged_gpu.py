@@ -310,3 +310,118 @@ def test_a_layers_steps_together():
     # the rotated, quantized first token attends to itself alone
     _, vv = mxq.kv_read(cache, slots[:1])
     assert torch.equal(whole[0], vv[0].float().repeat_interleave(Hq // Hkv, dim=0))
+
+
+# Batches whose tiles are as many as the CUs (16 x 128 new tokens of 8 query heads for each of 4 KV
+# heads are 256 tiles of 256 rows): the kernel with eight waves
+def _wide(seed, **kw):
+    lens = [(128, 128 + 37 * i) for i in range(15)] + [(128, 128)]
+    kw = {"widths": (4, 4, 6, 8), "page": 64, **kw}
+    b = Batch(seed, lens, 32, 4, **kw)
+    assert b.T * 8 // 256 * 4 >= torch.cuda.get_device_properties(0).multi_processor_count
+    return b
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("widths", [(4, 4, 6, 8), (4, 4, 4, 4), (3, 3, 6, 8), (8, 8, 8, 8)])
+def test_many_tiles(widths, dtype):
+    say("many tiles", widths, dtype)
+    _wide(2000 + sum(widths), widths=widths).check(dtype, seqs=[3, 15])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_tiles_with_masks_caps_and_biases(dtype):
+    slopes = [2.0 ** (-8.0 * (h + 1) / 32) for h in range(32)]
+    _wide(2010, window=70, prefix=[5 * i for i in range(16)]).check(dtype, seqs=[0, 9])
+    _wide(2011, softcap=8.0, slopes=slopes, prefix=[600] * 16).check(dtype, seqs=[6])
+    _wide(2012, slopes=slopes, window=100).check(dtype, seqs=[15])
+
+
+def test_many_tiles_holes_nans_and_repeats():
+    b = _wide(2020, page=16)
+    want = {t: b.run(t) for t in TYPES}
+    for t in TYPES:
+        assert torch.equal(b.run(t), want[t])
+    zero = torch.zeros((16, 4, D), dtype=torch.bfloat16, device="cuda")
+    mxq.kv_append(b.cache, zero, zero, b.slots[16:32])
+    want = {t: b.run(t) for t in TYPES}
+    b.table[0, 1] = -1
+    for t in TYPES:
+        assert torch.equal(b.run(t), want[t])
+    b.q[130, 3, 5] = float("nan")
+    b.q[700, 20, 9] = float("-inf")
+    keep = torch.ones((b.T, 32), dtype=torch.bool, device="cuda")
+    keep[130, 3] = keep[700, 20] = False
+    for t in TYPES:
+        o = b.run(t)
+        assert bool(o[130, 3].isnan().all()) and torch.equal(o[keep], want[t][keep])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_both_kernels_split_and_merged(dtype):
+    # long caches and few sequences: the decoding ones and the chunk are both split, into unlike counts
+    lens = [(1, 5000), (40, 4000), (0, 100), (1, 33), (2, 2600), (1, 1)]
+    b = Batch(2100, lens, 8, 1, widths=(4, 4, 4, 8), page=128)
+    b.check(dtype)
+    # and G = 20 query heads: two groups of sixteen rows beside the tiles
+    Batch(2101, [(1, 1500), (17, 900), (1, 40)], 20, 1).check(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Hq,q", [(8, 4), (8, 3), (32, 1), (24, 1), (1, 32), (1, 17), (5, 6)])
+def test_up_to_32_rows(Hq, q, dtype):
+    say("rows", Hq, q, dtype)
+    Batch(2200 + 10 * Hq + q, [(q, 300), (q, q), (q, 1000)], Hq, 1, widths=(3, 4, 6, 8), window=0).check(dtype)
+
+
+def test_many_sequences():
+    # more than 64: the search of a tile's sequence takes two steps; some have no rows
+    lens = [(3 + (i % 40), 3 + (i % 40) + i) if i % 7 else (0, i) for i in range(150)]
+    Batch(2300, lens, 4, 2).check(seqs=[1, 63, 64, 65, 128, 149])
+    Batch(2301, [(1, 1 + i) for i in range(130)], 8, 1).check(torch.bfloat16, seqs=[0, 64, 129])
+
+
+def test_two_calls_at_once_on_two_streams():
+    b = [Batch(2400 + i, [(1, 900), (30, 400)], 8, 2) for i in range(2)]
+    want = [x.run() for x in b]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for x, s in zip(b, side):
+            with torch.cuda.stream(s):
+                got.append(x.run())
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert torch.equal(g, want[i % 2])
+
+
+def test_pages_past_four_gigabytes():
+    # K's mantissas alone take 4.6 GB: page 0 and the last ones hold the sequences
+    Hkv, page, pages = 16, 1024, 2200
+    assert pages * page * Hkv * 128 > 2 ** 32
+    mk = lambda m: torch.empty(pages * page * Hkv * m, dtype=torch.uint8, device="cuda")  # noqa: E731
+    fmt = mxq.Format(D, [8, 8, 8, 8])
+    far = mxq.PagedCache(fmt, Hkv, pages, page, k=(mk(128), mk(4)), v=(mk(128), mk(4)))
+    near = mxq.PagedCache(fmt, Hkv, 3, page)
+    g = torch.Generator().manual_seed(12)
+    n = 1500
+    k, v = (torch.randn((n, Hkv, D), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    t = torch.arange(n, device="cuda")
+    tables = {}
+    for c, at in ((far, [pages - 1, 0]), (near, [2, 0])):
+        tables[c] = torch.tensor([at], dtype=torch.int32, device="cuda")
+        mxq.kv_append(c, k, v, tables[c][0].long()[t // page] * page + t % page)
+    for q in (1, 70):
+        x = torch.randn((q, 2 * Hkv, D), generator=g).to(torch.bfloat16).cuda()
+        cu = torch.tensor([0, q], dtype=torch.int32, device="cuda")
+        kv = torch.tensor([n], dtype=torch.int32, device="cuda")
+        a, b = (mxq.attn_paged(x, c, cu, kv, tables[c], q, n, 0.1) for c in (far, near))
+        assert torch.equal(a, b) and bool(a.any())
+
+
+def test_odd_counts_of_partial_results():
+    # one query head, one row, an odd number of splits
+    for n in (400, 700, 1000):
+        Batch(2500 + n, [(1, n)], 1, 1).check()
+    Batch(2600, [(1, 900), (1, 500), (1, 77)], 1, 1).check(torch.bfloat16)

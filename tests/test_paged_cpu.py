@@ -82,7 +82,7 @@ def test_rope_refusals(L):
                      (dict(D=62), SHAPE), (dict(D=129), SHAPE), (dict(D=4098), SHAPE), (dict(T=2 ** 31), SHAPE),
                      (dict(x=FAKE + 2), ALIGN), (dict(y=FAKE + 4098), ALIGN), (dict(xs=(255, 128)), ALIGN),
                      (dict(ys=(256, 127)), ALIGN), (dict(y=FAKE, ys=(512, 128)), SHAPE),
-                     (dict(T=2 ** 31 - 1, H=65535, D=4096), SHAPE)):
+                     (dict(T=2 ** 31 - 1, H=65535, D=4096), SHAPE), (dict(T=2 ** 20, H=64, D=128), SHAPE)):
         assert call(**kw) == want, kw
     assert call(T=0, x=0, y=0, pos=0) == 0 and call(H=0, x=0) == 0
 
@@ -95,6 +95,7 @@ def test_rope_table_refusals(L):
     for rot, P, ms in ((63, 10, 1.0), (0, 10, 1.0), (514, 10, 1.0), (64, 0, 1.0), (64, -5, 1.0),
                        (64, 10, math.inf), (64, 10, math.nan)):
         assert L.mxq_rope_table(p, rot, P, ms, FAKE, None) == SHAPE
+    assert L.mxq_rope_table(p, 512, 2 ** 25, 1.0, FAKE, None) == SHAPE
     f[5] = math.nan
     assert L.mxq_rope_table(p, 64, 10, 1.0, FAKE, None) == SHAPE
     f[5] = 1.0
@@ -117,7 +118,7 @@ def test_append_and_read_refusals(L):
               (dict(good_q, qo=None), NULL), (dict(good_q, Hq=0), SHAPE), (dict(good_q, Hq=-1), SHAPE),
               (dict(good_q, qs=(516, 128)), ALIGN), (dict(good_q, qo=FAKE + 8), ALIGN),
               (dict(good_q, qo=FAKE, qs=(1024, 128)), SHAPE), (dict(good_q, Hq=65536), SHAPE),
-              (dict(T=2 ** 31 - 1, Hq=65535), SHAPE)]
+              (dict(good_q, T=2 ** 31 - 1, Hq=65535), SHAPE), (dict(good_q, T=2 ** 24, Hq=64), SHAPE)]
     for kw, want in cases:
         assert call(**kw) == want, kw
     assert call(T=0, k=0, v=0, slots=0) == 0
@@ -152,10 +153,12 @@ def test_attention_refusals(L):
               (dict(Hq=130), SHAPE), (dict(Hq=-8), SHAPE)]
     cases += [(dict(b=b), SHAPE) for b in (dict(S=-1), dict(T=-1), dict(max_q=-1), dict(max_kv=-1), dict(S=2 ** 31),
                                            dict(T=2 ** 31), dict(max_kv=2 ** 31), dict(max_q=2 ** 40),
-                                           dict(table_pages=-1), dict(table_pages=2 ** 31), dict(ld_table=2))]
+                                           dict(table_pages=-1), dict(table_pages=2 ** 31), dict(ld_table=2),
+                                           dict(T=2 ** 27), dict(S=2 ** 22))]
     cases += [(dict(b=dict(cu_q=0)), NULL), (dict(b=dict(kv_len=0)), NULL), (dict(b=dict(table=0)), NULL)]
     cases += [(dict(p=p), SHAPE) for p in (dict(scale=math.inf), dict(scale=math.nan), dict(softcap=-1.0),
-                                           dict(softcap=math.inf), dict(softcap=math.nan), dict(window=-1))]
+                                           dict(softcap=math.inf), dict(softcap=math.nan), dict(softcap=1e-40),
+                                           dict(window=-1))]
     for kw, want in cases:
         assert call(**kw) == want, kw
     for b in (dict(S=0), dict(T=0), dict(max_q=0)):
@@ -248,6 +251,16 @@ def test_binding_refuses_caches(host):
     for k in ((u8(n - 1), u8(e)), (u8(n), u8(e - 1)), (u8(n).float(), u8(e)), (u8(2 * n)[::2], u8(e))):
         with pytest.raises(mxq.MxqError):
             mxq.PagedCache(f, 2, 4, 16, k=k, v=(u8(n), u8(e)))
+
+
+def test_a_cache_keeps_its_own_widths(host):
+    f = fmt((4, 4, 4, 4))
+    c = mxq.PagedCache(f, 2, 4, 16, device="cpu")
+    f.widths[:] = 8                                    # the buffers were sized for 4 bits
+    assert c.fmt.widths.tolist() == [4, 4, 4, 4]
+    assert mxq.lib().mxq_kv_page_bytes(c.fmt.ref, 2, 16) == c.page_bytes
+    with pytest.raises(ValueError):
+        c.fmt.widths[0] = 8
 
 
 def test_binding_refuses_append_and_read(host):

@@ -307,7 +307,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
     wave_sync();
     constexpr int kTerms = F32 ? 3 : 1;
     bf8 pt[NC][kTerms];
-    const bool edge = t0 + kFewChunk - 1 > p0 || last - t0 >= window || t0 + kFewChunk > q.len;
+    // (positions end before the sequence does, and so does the prefix)
+    const bool edge = t0 + kFewChunk - 1 > p0 || last - t0 >= window;
 #pragma unroll
     for (int e = 0; e < NC; ++e) {
       float x[8];                                          // the product's slots: tokens 4 gr + i, 16 + 4 gr + i
@@ -327,11 +328,11 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
         scale = 1.f;
       }
       if (edge) {
-        const int rel = p[e] - t0 - 4 * gr, pre = q.pre - t0 - 4 * gr, end = q.len - t0 - 4 * gr;
+        const int rel = p[e] - t0 - 4 * gr, pre = q.pre - t0 - 4 * gr;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int k = 16 * (i >> 2) + (i & 3);
-          const bool see = (((k <= rel) & (rel - k < window)) | (k < pre)) & (k < end);
+          const bool see = ((uint32_t)(rel - k) < (uint32_t)window) | (k < pre);
           x[i] = see ? x[i] : ninf;
         }
       }

@@ -106,7 +106,7 @@ struct TileRow {
   int p;                                 // the row's position
   int pw0, pw1;                          // the wave's first and last
   int last;                              // the last token that one of the wave's rows may see
-  int window, len, pre;
+  int window, pre;
   float sc, slope, softcap;
   bool biased;
 };
@@ -155,14 +155,18 @@ __device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s
     }
     scale = 1.f;
   }
-  // masks, where not every row of the wave sees all
-  if (t0 + 31 > w.pw0 || w.pw1 - t0 >= w.window || t0 + 32 > w.len) {
-    const int rel = w.p - t0 - 4 * h, pre = w.pre - t0 - 4 * h, end = w.len - t0 - 4 * h;
+  // Masks, where not every row of the wave sees all.  (Positions end before the
+  // sequence does, and so does the prefix: its length needs no test.)
+  if (t0 + 31 > w.pw0 || w.pw1 - t0 >= w.window) {
+    const int rel = w.p - t0 - 4 * h, pre = w.pre - t0 - 4 * h;
+    if (w.pre > t0) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int k = c(i);
-      const bool see = (((k <= rel) & (rel - k < w.window)) | (k < pre)) & (k < end);
-      s[i] = see ? s[i] : -__builtin_inff();
+      for (int i = 0; i < 16; ++i)
+        s[i] = (uint32_t)(rel - c(i)) < (uint32_t)w.window || c(i) < pre ? s[i] : -__builtin_inff();
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[i] = (uint32_t)(rel - c(i)) < (uint32_t)w.window ? s[i] : -__builtin_inff();
     }
   }
   return scale;
@@ -407,7 +411,6 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   w.pw1 = (int)(p0 + (min(wr + 32, rows) - 1) / G);
   w.last = max(w.pw1, q.pre - 1);
   w.window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
-  w.len = q.len;
   w.pre = q.pre;
   w.sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
   w.softcap = a.softcap;

@@ -3,23 +3,28 @@
 //
 // A sequence's n new tokens and the G query heads of a KV head make n G query
 // rows that share K and V (row r: token r / G, head r % G).  A workgroup takes a
-// tile of them and walks the cached tokens, 64 at a time, with a running maximum
-// and sum of the softmax (one pass over K and V):
+// tile of them, 32 a wave, and walks the cached tokens, 64 at a time, with a
+// running maximum and sum of the softmax (one pass over K and V):
 //   S^T = K Q^T     32x32x16 bf16 products, a lane holding one query row's scores
-//                   of 32 of the 64 tokens (its partner, lane ^ 32, the others);
+//                   of 16 of the 32 tokens (its partner, lane ^ 32, the others);
 //   O^T += V^T P^T  takes the same lane's probabilities as they come out of the
 //                   softmax: the order of the tokens over the reduction is free,
 //                   and V follows it.
 // So the statistics and the rescaling of O are a lane's own, and P never leaves
 // the registers.  K and V are dequantized once per workgroup into LDS as bf16,
 // which is exact (at most 8 significant bits): a wave per 32-value block of the
-// row, a lane per token, so that widths are uniform over a wave.
+// row, a lane per token, so that widths are uniform over a wave.  What arrives in
+// LDS by one barrier is V's step and K's half a step further, so that each half
+// step has the next one's score products to put its exponentials behind.
 //
-// Sequences with at most 16 query rows per KV head (decoding, drafted tokens) have
-// a kernel of their own: bytes and dequantization bound them, not products.  There
-// each wave takes chunks of 32 tokens by itself, without a barrier, dequantizes K
-// straight into the operand of 16x16x32 products and V into its own LDS rows, and
-// the waves are merged at the end.  The tokens of a sequence are split over
+// A step's 32 products of a wave hold its matrix core for 1024 cycles; behind them
+// go the exponentials, the sums and the dequantization, about as many issue cycles.
+// 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1017 us, 1.01 PFLOP/s
+// (1.24 to 1.37 by a large library product), the matrix cores 40 % and the vector
+// units 70 % busy: softmax and dequantization bound it.
+//
+// Sequences with at most 32 query rows per KV head (decoding, drafted tokens) have
+// a kernel of their own (attn_few.h).  The tokens of a sequence are split over
 // workgroups where there are few rows; the splits' results are merged in order.
 #include <algorithm>
 

@@ -78,12 +78,6 @@ __device__ __forceinline__ void load_block(const uint8_t *p, RawBlock &r) {
     for (int i = 0; i < 3; ++i) r.w[i] = *(const uint32_t *)(p + 4 * i);
   }
 }
-__device__ __forceinline__ void load_block(const uint8_t *p, int m, RawBlock &r) {
-  if (m == 4) load_block<4>(p, r);
-  else if (m == 8) load_block<8>(p, r);
-  else if (m == 6) load_block<6>(p, r);
-  else load_block<3>(p, r);
-}
 
 // Slot i of eight values holds element slot_elem(m, i): 4- and 6-bit blocks yield
 // the even elements, then the odd ones.

@@ -20,8 +20,8 @@
 // A step's 32 products of a wave hold its matrix core for 1024 cycles; behind them
 // go the exponentials, the sums and the dequantization, about as many issue cycles.
 // 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1017 us, 1.01 PFLOP/s
-// (1.24 to 1.37 by a large library product), the matrix cores 40 % and the vector
-// units 70 % busy: softmax and dequantization bound it.
+// (1.24 to 1.37 by a large library product), the matrix cores 41 % and the vector
+// units 55 % busy by the counters: softmax and dequantization bound it.
 //
 // Sequences with at most 32 query rows per KV head (decoding, drafted tokens) have
 // a kernel of their own (attn_few.h).  The tokens of a sequence are split over

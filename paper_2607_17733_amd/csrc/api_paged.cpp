@@ -131,7 +131,7 @@ mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_
   if (!x || !y || !pos) return MXQ_ERR_NULL;
   if (!aligned(x, 4) || !aligned(y, 4) || x_ts % 2 || x_hs % 2 || y_ts % 2 || y_hs % 2)
     return MXQ_ERR_ALIGN;
-  if (x == y && (x_ts != y_ts || x_hs != y_hs)) return MXQ_ERR_SHAPE;
+  if (x == y && ((T > 1 && x_ts != y_ts) || (H > 1 && x_hs != y_hs))) return MXQ_ERR_SHAPE;
   if (T * H > kMaxGrid * 256 / (D / 2)) return MXQ_ERR_SHAPE;
   mxq::RopeRowsArgs a{};
   a.rope = rope_args(rope);
@@ -183,7 +183,8 @@ mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const ui
     if (Hq < 1) return MXQ_ERR_SHAPE;
     if ((st = check_rows(q, q_ts, q_hs)) != MXQ_OK) return st;
     if ((st = check_rows(q_out, 0, 0)) != MXQ_OK) return st;
-    if (q == q_out && (q_hs != kD || q_ts != Hq * kD)) return MXQ_ERR_SHAPE;
+    // (the stride of a single head or token is any)
+    if (q == q_out && ((Hq > 1 && q_hs != kD) || (T > 1 && q_ts != Hq * kD))) return MXQ_ERR_SHAPE;
   }
   a.rope = rope_args(rope);
   a.k = k;

@@ -219,3 +219,18 @@ def test_no_tokens():
     k, v = mxq.kv_read(c, none)
     torch.cuda.synchronize()
     assert k.shape == (0, 2, D) and torch.equal(before, c.k[0])
+
+
+def test_a_single_token_in_place_in_fused_rows():
+    # torch calls one token's heads contiguous whatever the stride between tokens is
+    table = mxq.rope_table(mxq.rope_inv_freq(D)[0], 64)
+    fused = _rows(1, 12, 9).cuda()
+    want = bits_of(fused.cpu()).copy()
+    pos = torch.tensor([41], dtype=torch.int32, device="cuda")
+    q, k, v = fused[:, :8], fused[:, 8:10], fused[:, 10:]
+    assert q.is_contiguous() and q.stride(0) == 12 * D
+    want[:, :8] = opaged.rope(want[:, :8], pos.cpu().numpy(), table.cpu().numpy(), False)
+    c = _cache([4, 4, 4, 4], 2, 1, 16)
+    got = mxq.kv_append(c, k, v, torch.zeros(1, dtype=torch.int64, device="cuda"), pos=pos, rope=table, q=q, q_out=q)
+    torch.cuda.synchronize()
+    assert got is q and np.array_equal(bits_of(fused.cpu()), want)

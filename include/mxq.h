@@ -524,12 +524,12 @@ typedef struct {
  * mxq_rope: rotates bf16 rows x[t][h][0..D-1] at x + t * x_ts + h * x_hs
  * (elements) into y, likewise strided, with the position pos[t] (DEVICE int32
  * [T]).  y may be x itself with the same strides, else the two must not
- * overlap.  1 <= D <= 4096, D even; x and y 4-byte aligned, strides even.
+ * overlap; nor may rows of y.  1 <= D <= 4096, D even; x and y 4-byte aligned, strides even.
  * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (negative counts, rot odd or out of
- * range, D < rot, positions out of range, non-finite frequencies or mscale,
- * T * H * D / 2 or positions * rot / 2 of 2^32 or more), MXQ_ERR_ALIGN (also for
- * odd strides), MXQ_ERR_UNSUPPORTED (layout), MXQ_ERR_DEVICE.  T == 0 or H == 0
- * enqueues nothing.
+ * range, D < rot, positions out of range, non-finite frequencies or mscale, a
+ * stride of y below D between several rows, T * H * D / 2 or positions * rot / 2
+ * of 2^32 or more), MXQ_ERR_ALIGN (also for odd strides), MXQ_ERR_UNSUPPORTED
+ * (layout), MXQ_ERR_DEVICE.  T == 0 or H == 0 enqueues nothing.
  */
 mxq_status mxq_rope_table(const double *inv_freq, int32_t rot, int64_t positions,
                           double mscale, float *table, void *stream);

@@ -132,6 +132,9 @@ mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_
   if (!aligned(x, 4) || !aligned(y, 4) || x_ts % 2 || x_hs % 2 || y_ts % 2 || y_hs % 2)
     return MXQ_ERR_ALIGN;
   if (x == y && ((T > 1 && x_ts != y_ts) || (H > 1 && x_hs != y_hs))) return MXQ_ERR_SHAPE;
+  // rows of the result that overlap would be written, or turned in place, by several threads
+  auto apart = [&](int64_t n, int64_t stride) { return n == 1 || stride >= D || stride <= -D; };
+  if (!apart(T, y_ts) || !apart(H, y_hs)) return MXQ_ERR_SHAPE;
   if (T * H > kMaxGrid * 256 / (D / 2)) return MXQ_ERR_SHAPE;
   mxq::RopeRowsArgs a{};
   a.rope = rope_args(rope);

@@ -87,6 +87,16 @@ def test_rope_refusals(L):
     assert call(T=0, x=0, y=0, pos=0) == 0 and call(H=0, x=0) == 0
 
 
+def test_rope_refuses_output_rows_that_overlap(L):
+    def call(T=4, H=2, ys=(256, 128), x=FAKE, xs=None):
+        return L.mxq_rope(ref(rotary()), x, T, H, 128, *(xs or ys), FAKE, FAKE, *ys, None)
+
+    for kw in (dict(ys=(0, 128)), dict(ys=(256, 0)), dict(ys=(256, 64)), dict(ys=(64, 256)),
+               dict(ys=(-64, 256)), dict(ys=(256, 126), x=FAKE + 2 ** 20), dict(T=1, ys=(0, 0)),
+               dict(H=1, ys=(126, 0))):
+        assert call(**kw) == SHAPE, kw
+
+
 def test_rope_table_refusals(L):
     f = (ctypes.c_double * 256)(*[1.0] * 256)
     p = ctypes.cast(f, ctypes.c_void_p)

@@ -78,15 +78,31 @@ __device__ __forceinline__ void store_big(const RawBlock &r, int E, uint8_t *to)
   }
 }
 
-// The tiles of `rows` query rows of all sequences are numbered with gaps: those of
-// sequence s begin at floor(cu_q[s] G / rows) + s.  No two sequences meet (a
-// sequence of n rows has at most floor(end / rows) - floor(begin / rows) + 1
-// tiles), and floor(T G / rows) + S numbers are enough, so that the launch needs
-// no look at the device's lengths.  The sequence of a number, by 64-way search; up
-// to 64 sequences cost one load latency, their lengths included.  False: a gap.
-__device__ inline bool find_seq(const AttnPagedArgs &a, int64_t number, int rows, Seq &q, int &tile) {
+// The sum of the lanes up to this one.
+__device__ inline int wave_scan(int x, int lane) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // shifts within 16 lanes
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  const int r0 = __builtin_amdgcn_readlane(x, 15), r1 = __builtin_amdgcn_readlane(x, 31),
+            r2 = __builtin_amdgcn_readlane(x, 47);
+  return x + (lane >= 16 ? r0 : 0) + (lane >= 32 ? r1 : 0) + (lane >= 48 ? r2 : 0);
+}
+
+// Tile `index` of the sequences with more than few_rows query rows, ROWS rows each, a
+// sequence's last first.  The launch has floor(T G / ROWS) + S tiles, which are enough
+// without a look at the device's lengths (n rows have at most floor(end / ROWS) -
+// floor(begin / ROWS) + 1).  Up to 64 sequences are counted, in one load latency, and the
+// tiles too many come last (among the others, say every second one, they leave half of
+// the GPU idle: workgroups are dealt to its parts in turn; 16 sequences of 256 rows over
+// 2000 tokens, 102 us).  More have their numbers with gaps, those of sequence s from
+// floor(cu_q[s] G / ROWS) + s on, found by 64-way search.  False: none.
+template <int ROWS>
+__device__ inline bool find_tile(const AttnPagedArgs &a, int64_t index, int64_t tiles, int few_rows, Seq &q,
+                                 int &tile) {
   const int lane = threadIdx.x & 63, S = (int)a.S;
-  auto start = [&](int s, int cu) { return (int64_t)max(cu, 0) * a.G / rows + s; };
+  auto start = [&](int s, int cu) { return (int64_t)max(cu, 0) * a.G / ROWS + s; };
+  int64_t number = tiles - 1 - index;
   int lo = 0, cnt = S;
   while (cnt > 64) {
     const int step = (cnt + 63) / 64, s = lo + lane * step;
@@ -97,12 +113,27 @@ __device__ inline bool find_seq(const AttnPagedArgs &a, int64_t number, int rows
     cnt = min(step, S - lo);
   }
   const int s = min(lo + lane, S - 1);
-  const int c0 = a.cu_q[s], c1 = a.cu_q[s + 1], len = a.kv_len[s], pre = a.prefix ? a.prefix[s] : 0;
-  const int k = __popcll(__ballot(lane < cnt && start(s, c0) <= number)) - 1;
-  if (k < 0) return false;
-  auto of = [&](int x) { return __builtin_amdgcn_readlane(x, k); };
-  q = seq_of(a, of(s), of(c0), of(c1), of(len), of(pre));
-  tile = (int)(number - start(q.s, of(c0)));
+  const Seq x = seq_at(a, s);
+  const int64_t r = (int64_t)x.n * a.G;
+  int k, first;
+  if (S <= 64) {
+    const int n = lane < S && r > few_rows ? (int)((r + ROWS - 1) / ROWS) : 0, end = wave_scan(n, lane);
+    number = __builtin_amdgcn_readlane(end, 63) - 1 - index;
+    if (number < 0) return false;
+    k = __popcll(__ballot(end <= number));
+    first = __builtin_amdgcn_readlane(end - n, k);
+  } else {
+    const int at = (int)start(s, a.cu_q[s]);
+    k = __popcll(__ballot(lane < cnt && at <= number)) - 1;
+    if (k < 0) return false;
+    first = __builtin_amdgcn_readlane(at, k);
+  }
+  q.s = lo + k;
+  q.row0 = __builtin_amdgcn_readlane(x.row0, k);
+  q.n = __builtin_amdgcn_readlane(x.n, k);
+  q.len = __builtin_amdgcn_readlane(x.len, k);
+  q.pre = __builtin_amdgcn_readlane(x.pre, k);
+  tile = (int)(number - first);
   return true;
 }
 
@@ -382,7 +413,7 @@ __device__ __forceinline__ void tile_steps(const AttnPagedArgs &a, const Loader 
 
 template <bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, 2)
-void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows) {
+void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t tiles, int few_rows) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kStage];         // K and V of two steps
   constexpr int kRows = 32 * NW;
   const PageGeo &g = a.geo;
@@ -393,11 +424,10 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t numbers, int few_rows
   const int Hkv = (int)g.Hkv, G = a.G;
   const uint32_t rest = blockIdx.x / (uint32_t)Hkv;
   const int kvh = (int)(blockIdx.x - rest * (uint32_t)Hkv);
-  const int64_t number = numbers - 1 - rest / (uint32_t)splits;
   const int split = (int)(rest % (uint32_t)splits);
   int tile;
   Seq q;
-  if (!find_seq(a, number, kRows, q, tile)) return;
+  if (!find_tile<kRows>(a, rest / (uint32_t)splits, tiles, few_rows, q, tile)) return;
   const int64_t rows = (int64_t)q.n * G, r0 = (int64_t)tile * kRows;
   if (r0 >= rows || rows <= few_rows) return;
   const int64_t p0 = (int64_t)q.len - q.n;                 // the first row's position
@@ -620,7 +650,7 @@ void launch_merge(const AttnPagedArgs &a, int splits, int few_rows, int most, hi
   else go(a.o_f32 ? attn_merge_kernel<true, 8> : attn_merge_kernel<false, 8>, 8);
 }
 
-int64_t tile_numbers(const AttnPagedArgs &a, int waves) { return a.T * a.G / (32 * waves) + a.S; }
+int64_t most_tiles(const AttnPagedArgs &a, int waves) { return a.T * a.G / (32 * waves) + a.S; }
 
 // Which kernels run, and their splits (0: not launched).  Times in us, 64 query and 8
 // KV heads, 4-bit cache, 256 CUs.
@@ -675,8 +705,8 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   AttnPagedArgs a = args;
   const Plan p = plan_of(a);
   a.parts = std::max(p.tile, p.few);
-  const int64_t numbers = tile_numbers(a, p.waves);
-  const int64_t wgs = numbers * a.geo.Hkv * p.tile;
+  const int64_t tiles = most_tiles(a, p.waves);
+  const int64_t wgs = tiles * a.geo.Hkv * p.tile;
   const int few_rows = p.few ? 16 * p.groups : 0;          // what the tiles leave to the other kernel
   const int most = (int)std::min<int64_t>(a.max_q, few_rows / a.G);
   if (p.few) {
@@ -688,7 +718,7 @@ hipError_t launch_attn_paged(const AttnPagedArgs &args, hipStream_t s) {
   if (p.tile) {
     const auto fn = p.waves == 4 ? (a.o_f32 ? attn_tile_kernel<true, 4> : attn_tile_kernel<false, 4>)
                                  : (a.o_f32 ? attn_tile_kernel<true, 8> : attn_tile_kernel<false, 8>);
-    hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3((unsigned)(64 * p.waves)), 0, s, a, p.tile, numbers,
+    hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3((unsigned)(64 * p.waves)), 0, s, a, p.tile, tiles,
                        few_rows);
     if (p.tile > 1) launch_merge(a, p.tile, few_rows, 0, s);
   }

@@ -668,17 +668,24 @@ Plan plan_of(const AttnPagedArgs &a) {
     return std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
   };
   if (most > kFewMost) {
+    const int64_t steps = (a.max_kv + kTok - 1) / kTok;
+    auto tiles = [&](int64_t rows) { return even ? a.S * ((most + rows - 1) / rows) : a.T * a.G / rows + 1; };
+    // Splits: one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of
+    // at least four steps each; a CU holds one workgroup of eight waves, two of four.
+    const int64_t t4 = tiles(128), t8 = tiles(256);
+    const int64_t n4 = split(t4 * Hkv, 2 * cus, steps, 4), n8 = split(t8 * Hkv, cus, steps, 4);
     // Eight waves share the dequantization of K and V among twice the rows, but are one
-    // workgroup per CU: they need a tile for each (2048 rows over 16384 tokens, 512
-    // tiles, 1017 us against 1125 with four waves; 1024 rows, 256 tiles, 537 against
-    // 595; 512 rows, 363 against 349), and a tile that spans few tokens, whose rows see
-    // the same steps (one query head per KV head, 2 x 2048 tokens: 140 against 131).
-    p.waves = a.T * a.G / 256 * Hkv >= cus && a.G >= 4 ? 8 : 4;
-    const int64_t rows = 32 * p.waves;
-    const int64_t tiles = even ? a.S * ((most + rows - 1) / rows) : a.T * a.G / rows + 1;
-    // one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of at
-    // least four steps each
-    p.tile = (int)split(tiles * Hkv, p.waves == 8 ? cus : 2 * cus, (a.max_kv + kTok - 1) / kTok, 4);
+    // workgroup per CU, whose start and end nothing covers.  They need whole rounds of
+    // workgroups (rows over 16384 tokens: 2048 rows, two rounds, 1050 against 1150 with
+    // four waves; 512 rows, one, 297 and 328; but 1536, one and a half, 1016 and 948; 2
+    // prompts of 2731 in a window, 2.7, 122 and 114), tiles that are full (40 rows of
+    // 4 sequences, 320 of 512: 81 and 79), and rows that see the same
+    // steps, as those of a few tokens do (one query head per KV head, 2 x 2048 tokens:
+    // 135 and 129).
+    const int64_t wgs = t8 * Hkv * n8;
+    const bool whole = 16 * wgs >= 15 * cus * ((wgs + cus - 1) / cus), full = 12 * t8 <= 7 * t4;
+    p.waves = a.G >= 4 && whole && full ? 8 : 4;
+    p.tile = (int)(p.waves == 8 ? n8 : n4);
   }
   // (in a mixed batch the two kernels share the sequences between them)
   if (!p.tile || (a.G <= kFewMost && !even)) {

@@ -425,3 +425,23 @@ def test_odd_counts_of_partial_results():
     for n in (400, 700, 1000):
         Batch(2500 + n, [(1, n)], 1, 1).check()
     Batch(2600, [(1, 900), (1, 500), (1, 77)], 1, 1).check(torch.bfloat16)
+
+
+@pytest.mark.parametrize("S", [63, 64, 65, 130])
+def test_counts_of_sequences_with_tiles(S):
+    # empty, single, few and many rows in turn
+    kinds = [(0, 9), (1, 30), (40, 40), (9, 60), (0, 0), (65, 70), (17, 17)]
+    b = Batch(1600 + S, [kinds[(3 * s) % 7] for s in range(S)], 8, 2, tail_rows=3)
+    b.check(seqs=[0, 1, 2, 3, 4, 5, 6, 61, 62, S - 3, S - 2, S - 1])
+    empty = Batch(1700 + S, [(0, 5)] * (S - 1) + [(50, 90)], 8, 2)
+    empty.check(torch.bfloat16)
+
+
+@pytest.mark.parametrize("lens,kw", [([(256, 2100)], {}),
+                                     ([(300, 2100), (5, 900), (200, 700)], dict(widths=(4, 4, 6, 8))),
+                                     ([(256, 2200)], dict(window=900, prefix=[70])),
+                                     ([(300, 2100), (0, 4), (205, 700)], dict(softcap=30.0))])
+def test_tiles_of_all_rows_with_their_tokens_split(lens, kw):
+    # full tiles of 256 rows, several splits of each
+    for dtype in TYPES:
+        Batch(1800 + len(lens), lens, 32, 8, page=64, **kw).check(dtype, seqs=[0])

@@ -19,7 +19,7 @@
 //
 // A step's 32 products of a wave hold its matrix core for 1024 cycles; behind them
 // go the exponentials, the sums and the dequantization, about as many issue cycles.
-// 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1017 us, 1.01 PFLOP/s
+// 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1050 us, 0.98 PFLOP/s
 // (1.24 to 1.37 by a large library product), the matrix cores 41 % and the vector
 // units 55 % busy by the counters: softmax and dequantization bound it.
 //

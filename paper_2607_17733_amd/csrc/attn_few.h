@@ -178,6 +178,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t Hkv = (uint32_t)g.Hkv;
   const int G = a.G;
+  // KV heads run fastest, then a sequence's splits (32 sequences of 2048 to 8192 tokens of
+  // 4/4/6/8 bits: 80 us; sequences before splits 89, heads last 91)
   const uint32_t rest = blockIdx.x / Hkv;
   const int kvh = (int)(blockIdx.x - rest * Hkv);
   const int s = (int)(rest / (uint32_t)splits), split = (int)(rest - (uint32_t)s * (uint32_t)splits);

@@ -675,7 +675,8 @@ def rope_inv_freq(rot: int, base: float = 10000.0, scaling: str | None = None,
     "ramp"   by the turns r_i = orig_positions f_i / 2 pi that a frequency makes
              in the trained range: f_i for r_i >= high, f_i / factor for r_i <=
              low, between the two their mix, linear in i from the index that
-             makes `high` turns (rounded down) to the one that makes `low` (up);
+             makes `high` turns (rounded down, at least 0) to the one that makes
+             `low` (rounded up, also where it lies past the last frequency);
              cosines and sines are scaled by 1 + 0.1 ln(factor).
     "bands"  the mix linear in r_i instead, and cosines and sines as they are.
     """
@@ -707,7 +708,7 @@ def rope_inv_freq(rot: int, base: float = 10000.0, scaling: str | None = None,
     def index(t):
         return rot * np.log(orig_positions / (t * 2 * np.pi)) / (2 * np.log(base))
 
-    first, last = max(np.floor(index(high)), 0.0), min(np.ceil(index(low)), rot / 2 - 1.0)
+    first, last = max(np.floor(index(high)), 0.0), np.ceil(index(low))
     keep = 1.0 - np.clip((i - first) / max(last - first, 0.001), 0.0, 1.0)
     return keep * f + (1 - keep) * f / factor, 1.0 + 0.1 * float(np.log(factor))
 

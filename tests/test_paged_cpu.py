@@ -348,6 +348,25 @@ def test_frequencies():
             mxq.rope_inv_freq(**kw)
 
 
+@pytest.mark.parametrize("rot,positions", [(128, 131072), (64, 65536), (128, 4096), (128, 16384), (16, 10 ** 6)])
+def test_ramp_by_its_definition(rot, positions):
+    # also where the last frequency makes more than `low` turns in the trained range (2.4 and 1.4 of
+    # them in the first two): the mix goes on to the index that would make `low`
+    factor, low, high = 4.0, 1.0, 32.0
+    g, _ = mxq.rope_inv_freq(rot, scaling="ramp", factor=factor, orig_positions=positions, low=low, high=high)
+
+    def index(turns):                                  # positions base^(-2 i / rot) / 2 pi = turns
+        return rot / 2 * math.log(positions / (2 * math.pi * turns), 10000.0)
+
+    a, b = max(math.floor(index(high)), 0), math.ceil(index(low))
+    for i in range(rot // 2):
+        f = 10000.0 ** (-2.0 * i / rot)
+        new = min(max((i - a) / (b - a), 0.0), 1.0)    # the share of f / factor
+        assert math.isclose(g[i], f * (1 - new) + f / factor * new, rel_tol=1e-12), i
+        if positions * f / (2 * math.pi) > low:
+            assert g[i] > f / factor * (1 + 1e-9), i   # divided in full only from `low` turns down
+
+
 # --------------------------------------------------------------------------
 # the oracle's pins
 

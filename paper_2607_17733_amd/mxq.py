@@ -696,13 +696,13 @@ def rope_inv_freq(rot: int, base: float = 10000.0, scaling: str | None = None,
         return (base * factor ** (rot / (rot - 2.0))) ** (-2.0 * i / rot), 1.0
     if scaling not in ("ramp", "bands"):
         raise MxqError("scaling must be None, 'linear', 'base', 'ramp' or 'bands'")
-    if orig_positions < 1 or not 0 < low < high:
+    if not (1 <= orig_positions < np.inf and 0 < low < high < np.inf):
         raise MxqError("%r needs orig_positions and 0 < low < high" % scaling)
     turns = orig_positions * f / (2 * np.pi)
     if scaling == "bands":
         keep = np.clip((turns - low) / (high - low), 0.0, 1.0)
         return keep * f + (1 - keep) * f / factor, 1.0
-    if base == 1.0:
+    if base <= 1.0:                        # (frequencies that do not fall)
         raise MxqError("'ramp' needs a base above 1")
 
     def index(t):

@@ -348,6 +348,19 @@ def test_frequencies():
             mxq.rope_inv_freq(**kw)
 
 
+def test_scalings_without_a_result_are_refused():
+    # a ramp over frequencies that rise with the index, lengths and turns that are no numbers
+    ok = dict(rot=8, scaling="ramp", factor=2.0, orig_positions=100)
+    assert np.isfinite(mxq.rope_inv_freq(**ok, base=1.5)[0]).all()
+    for kw in (dict(base=0.5), dict(base=1.0), dict(orig_positions=math.nan), dict(orig_positions=math.inf),
+               dict(high=math.inf), dict(high=math.nan), dict(low=math.nan)):
+        with pytest.raises(mxq.MxqError):
+            mxq.rope_inv_freq(**{**ok, **kw})
+        if "base" not in kw:
+            with pytest.raises(mxq.MxqError):
+                mxq.rope_inv_freq(**{**ok, **kw, "scaling": "bands"})
+
+
 @pytest.mark.parametrize("rot,positions", [(128, 131072), (64, 65536), (128, 4096), (128, 16384), (16, 10 ** 6)])
 def test_ramp_by_its_definition(rot, positions):
     # also where the last frequency makes more than `low` turns in the trained range (2.4 and 1.4 of

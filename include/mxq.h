@@ -526,9 +526,8 @@ typedef struct {
  * [T]).  y may be x itself with the same strides, else the two must not
  * overlap; nor may rows of y.  1 <= D <= 4096, D even; x and y 4-byte aligned, strides even.
  * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (negative counts, rot odd or out of
- * range, D < rot, positions out of range, non-finite frequencies or mscale, a
- * stride of y below D between several rows, T * H * D / 2 or positions * rot / 2
- * of 2^32 or more), MXQ_ERR_ALIGN (also for odd strides), MXQ_ERR_UNSUPPORTED
+ * range, D < rot, positions out of range, non-finite frequencies or mscale, rows
+ * of y that overlap, T * H * D / 2 or positions * rot / 2 of 2^32 or more), MXQ_ERR_ALIGN (also for odd strides), MXQ_ERR_UNSUPPORTED
  * (layout), MXQ_ERR_DEVICE.  T == 0 or H == 0 enqueues nothing.
  */
 mxq_status mxq_rope_table(const double *inv_freq, int32_t rot, int64_t positions,

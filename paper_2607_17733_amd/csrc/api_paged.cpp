@@ -84,6 +84,21 @@ mxq_status check_rows(const void *p, int64_t ts, int64_t hs) {
   return MXQ_OK;
 }
 
+// Whether no two of T x H rows of D elements, ts and hs elements apart, overlap:
+// nothing but i = j = 0 brings i ts + j hs, |i| < T, |j| < H, within D of zero.
+bool rows_apart(int64_t T, int64_t ts, int64_t H, int64_t hs, int64_t D) {
+  typedef __int128 wide;                                   // (of strides, and their multiples)
+  const wide a = ts < 0 ? -(wide)ts : ts, b = hs < 0 ? -(wide)hs : hs;
+  if ((T > 1 && a < D) || (H > 1 && b < D)) return false;
+  if (T == 1 || H == 1) return true;
+  if (a >= b ? a >= (H - 1) * b + D : b >= (T - 1) * a + D) return true;   // one within the other
+  for (int64_t j = 1; j < H; ++j) {                        // the multiples of a around j b
+    const wide i = j * b / a, over = j * b - i * a;
+    if ((i < T && over < D) || (i + 1 < T && a - over < D)) return false;
+  }
+  return true;
+}
+
 mxq_status attn_shape(const mxq_fmt *fmt, const mxq_paged_kv *c, int64_t S, int64_t T, int64_t Hq,
                       int64_t max_q, int64_t max_kv, mxq::AttnPagedArgs *a) {
   const mxq_status st = check_cache(fmt, c, &a->geo);
@@ -132,10 +147,9 @@ mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_
   if (!aligned(x, 4) || !aligned(y, 4) || x_ts % 2 || x_hs % 2 || y_ts % 2 || y_hs % 2)
     return MXQ_ERR_ALIGN;
   if (x == y && ((T > 1 && x_ts != y_ts) || (H > 1 && x_hs != y_hs))) return MXQ_ERR_SHAPE;
-  // rows of the result that overlap would be written, or turned in place, by several threads
-  auto apart = [&](int64_t n, int64_t stride) { return n == 1 || stride >= D || stride <= -D; };
-  if (!apart(T, y_ts) || !apart(H, y_hs)) return MXQ_ERR_SHAPE;
   if (T * H > kMaxGrid * 256 / (D / 2)) return MXQ_ERR_SHAPE;
+  // rows of the result that overlap would be written, or turned in place, by several threads
+  if (!rows_apart(T, y_ts, H, y_hs, D)) return MXQ_ERR_SHAPE;
   mxq::RopeRowsArgs a{};
   a.rope = rope_args(rope);
   a.x = x;

@@ -97,6 +97,37 @@ def test_rope_refuses_output_rows_that_overlap(L):
         assert call(**kw) == SHAPE, kw
 
 
+def _overlap(T, ts, H, hs, D):
+    at = sorted(t * ts + h * hs for t in range(T) for h in range(H))
+    return any(b - a < D for a, b in zip(at, at[1:]))
+
+
+def test_rope_refuses_rows_that_overlap_across_tokens_and_heads(L):
+    # each stride alone keeps its rows apart, both together do not: token 1's first head is token 0's second
+    def call(T, ts, H, hs, x=FAKE, D=128):
+        return L.mxq_rope(ref(rotary()), x, T, H, D, ts, hs, FAKE, FAKE, ts, hs, None)
+
+    assert call(2, 128, 2, 128) == SHAPE and call(2, 128, 2, 128, x=FAKE + 2 ** 20) == SHAPE
+    far = 2 ** 62
+    for T, ts, H, hs in ((2, far, 2, far + 126), (3, far, 3, -far), (2 ** 20, 130, 3, 130 * 2 ** 19 + 2),
+                         (9, 256, 40, 896), (2, 384, 4, 128)):
+        assert call(T, ts, H, hs) == SHAPE, (T, ts, H, hs)
+    # every pair of small strides: refused exactly where rows overlap (the others pass every check,
+    # which shows in what comes after them: nothing here has a device to launch on)
+    steps = [-512, -390, -384, -256, -254, -128, -126, 0, 126, 128, 130, 254, 256, 258, 320, 384, 512, 640, 1024]
+    ok = 0
+    for T, H in ((2, 2), (2, 3), (3, 2), (4, 5), (7, 3)):
+        for ts in steps:
+            for hs in steps:
+                want = SHAPE if _overlap(T, ts, H, hs, 128) else None
+                if want is None and torch.cuda.is_available():
+                    continue                           # (the address is not memory)
+                got = call(T, ts, H, hs)
+                assert (got == SHAPE) == (want == SHAPE), (T, ts, H, hs)
+                ok += want is None
+    assert ok > 100 or torch.cuda.is_available()
+
+
 def test_rope_table_refusals(L):
     f = (ctypes.c_double * 256)(*[1.0] * 256)
     p = ctypes.cast(f, ctypes.c_void_p)

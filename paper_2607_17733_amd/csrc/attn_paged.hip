@@ -652,6 +652,13 @@ void launch_merge(const AttnPagedArgs &a, int splits, int few_rows, int most, hi
 
 int64_t most_tiles(const AttnPagedArgs &a, int waves) { return a.T * a.G / (32 * waves) + a.S; }
 
+// A dispatch holds fewer than 2^32 threads, and the tiles of many short sequences are
+// launched whether they have rows or not: the splits that it has room for.
+int64_t most_splits(const AttnPagedArgs &a, int waves) {
+  const int64_t wgs = std::max<int64_t>(1, most_tiles(a, waves) * a.geo.Hkv);
+  return std::max<int64_t>(1, UINT32_MAX / (64 * waves) / wgs);
+}
+
 // Which kernels run, and their splits (0: not launched).  Times in us, 64 query and 8
 // KV heads, 4-bit cache, 256 CUs.
 struct Plan {
@@ -673,7 +680,8 @@ Plan plan_of(const AttnPagedArgs &a) {
     // Splits: one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of
     // at least four steps each; a CU holds one workgroup of eight waves, two of four.
     const int64_t t4 = tiles(128), t8 = tiles(256);
-    const int64_t n4 = split(t4 * Hkv, 2 * cus, steps, 4), n8 = split(t8 * Hkv, cus, steps, 4);
+    const int64_t n4 = std::min(split(t4 * Hkv, 2 * cus, steps, 4), most_splits(a, 4));
+    const int64_t n8 = std::min(split(t8 * Hkv, cus, steps, 4), most_splits(a, 8));
     // Eight waves share the dequantization of K and V among twice the rows, but are one
     // workgroup per CU, whose start and end nothing covers.  They need whole rounds of
     // workgroups (rows over 16384 tokens: 2048 rows, two rounds, 1050 against 1150 with

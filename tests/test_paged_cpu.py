@@ -228,6 +228,18 @@ def test_work_size_is_what_the_call_asks_for(L):
                                 None, n, None) == NULL
 
 
+def test_splits_of_many_sequences_stay_in_a_dispatch(L):
+    # a few rows among many sequences that are mostly empty: tiles are launched for all of them, and
+    # with the splits they have to stay below 2^32 threads.  (The work size tells the splits.)
+    for S, T, Hkv in ((0, 40, 1), (65536, 40, 1), (2 ** 19, 40, 8), (2 ** 22, 40, 1), (300, 40, 8)):
+        c = cache(pages=100, Hkv=Hkv, page_tokens=1024)
+        n = L.mxq_attn_paged_work_bytes(fmt().ref, ref(c), S, T, Hkv, 40, 65536)
+        assert n >= 0
+        splits = max(1, n // (4 * T * Hkv * (128 + 2)))
+        assert (T // 128 + S) * Hkv * splits * 256 < 2 ** 32, (S, splits)
+    assert splits > 8                                  # where there is room they are kept
+
+
 # --------------------------------------------------------------------------
 # the binding
 

@@ -629,8 +629,9 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  * statistics are float32.  For a float32 output the probabilities enter the
  * value product with all their 24 bits, for a bf16 one rounded to bf16; a
  * probability is at most e^4 before the division by their sum, and a sum of
- * probabilities times values past float32's range is infinite.  Calls repeat
- * bit for bit.
+ * probabilities times values past float32's range is infinite.  The tanh of a
+ * bf16 result is good to 2^-21 (of a score at the cap) for caps up to 64, to
+ * 2^-18 of each capped score for larger ones.  Calls repeat bit for bit.
  * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, bad counts, Hq not a multiple
  * of Hkv, Hq / Hkv > 64, T * Hq > 2^29, S * Hkv > 2^22, non-finite scale or
  * softcap, softcap < 0 or in (0, 2^-60), window < 0, a short work buffer); MXQ_ERR_UNSUPPORTED (a permutation); MXQ_ERR_NULL;

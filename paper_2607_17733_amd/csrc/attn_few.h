@@ -236,7 +236,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   // this lane's query rows (columns past the last repeat it); product j of a score
   // takes the values of lane group gr, in slot order
   const int window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
-  const float sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
+  const float sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap.cap > 0.f ? 1.f : kUnit<F32>);
   const float ninf = -__builtin_inff();
   bf8 qop[NC][4];
   float slope[NC], m[NC], ref[NC], l[NC];
@@ -317,9 +317,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = sa[e][i >> 2][i & 3];
       float scale = sc;
-      if (a.softcap > 0.f) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = capped<F32>(x[i] * sc, a.softcap) * kUnit<F32>;
+      if (a.softcap.cap > 0.f) {
+        cap_scores<F32, 8>(x, sc, a.softcap);
         scale = 1.f;
       }
       if (a.slopes) {

@@ -143,7 +143,8 @@ struct TileRow {
   int pw0, pw1;                          // the wave's first and last
   int last;                              // the last token that one of the wave's rows may see
   int window, pre;
-  float sc, slope, softcap;
+  float sc, slope;
+  SoftCap softcap;
   bool biased;
 };
 
@@ -174,9 +175,8 @@ template <bool F32>
 __device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s) {
   auto c = [](int i) { return 8 * (i >> 2) + (i & 3); };
   float scale = w.sc;
-  if (w.softcap > 0.f) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = capped<F32>(s[i] * scale, w.softcap) * kUnit<F32>;
+  if (w.softcap.cap > 0.f) {
+    cap_scores<F32, 16>(s, scale, w.softcap);
     scale = 1.f;
   }
   if (w.biased) {
@@ -447,7 +447,7 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t tiles, int few_rows) 
   w.last = max(w.pw1, q.pre - 1);
   w.window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
   w.pre = q.pre;
-  w.sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap > 0.f ? 1.f : kUnit<F32>);
+  w.sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap.cap > 0.f ? 1.f : kUnit<F32>);
   w.softcap = a.softcap;
   w.biased = a.slopes != nullptr;
   w.slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;

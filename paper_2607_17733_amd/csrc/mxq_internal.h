@@ -184,6 +184,10 @@ hipError_t launch_kv_append(const KvAppendArgs &args, hipStream_t s);
 hipError_t launch_kv_read(const KvReadArgs &args, hipStream_t s);
 
 // Attention over the paged cache (attn_paged.hip).
+struct SoftCap {
+  float cap;               // 0: none
+  float inv, k, two;       // 1 / cap, 2 log2(e) / cap, -2 cap
+};
 struct AttnPagedArgs {
   PageGeo geo;
   const uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
@@ -197,7 +201,8 @@ struct AttnPagedArgs {
   int64_t ld_table, table_pages;
   int64_t S, T, Hq, max_q, max_kv, window;
   int G;
-  float scale, softcap;
+  float scale;
+  SoftCap softcap;
   int parts;               // of the partial results (set by launch_attn_paged)
 };
 int64_t attn_paged_work(const AttnPagedArgs &args);

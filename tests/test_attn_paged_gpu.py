@@ -445,3 +445,19 @@ def test_tiles_of_all_rows_with_their_tokens_split(lens, kw):
     # full tiles of 256 rows, several splits of each
     for dtype in TYPES:
         Batch(1800 + len(lens), lens, 32, 8, page=64, **kw).check(dtype, seqs=[0])
+
+
+@pytest.mark.parametrize("cap", [40.0, 300.0, 1e4, 1e6, 1e9, 1e20, 3e38])
+def test_caps_far_above_the_scores(cap):
+    # almost the identity; what is lost has to be a part of the score, not of the cap.
+    # (A bf16 result's tanh: its exponential and reciprocal are good to 5.2 x 2^-24 of the cap from an
+    # eighth of the cap on, 42 x 2^-24 of the score; the score's own sum is allowed 131 in tol32.)
+    lens = [(1, 333), (50, 210), (5, 64)]
+    for Hq, scale in ((8, D ** -0.5), (2, 1.0)):
+        b = Batch(3000, lens, Hq, 2, softcap=cap, scale=scale)
+        b.check(torch.float32)
+        o, tol32, tol16 = b.expected()
+        d = np.abs(b.run(torch.bfloat16).double().cpu().numpy() - o)
+        assert np.all(d <= tol16 + tol32 * (42 / 131))
+    slopes = [2.0 ** -(i + 1) for i in range(8)]
+    Batch(3001, lens, 8, 2, softcap=cap, slopes=slopes, window=70, prefix=[2, 0, 60]).check(torch.bfloat16)

@@ -299,7 +299,7 @@ mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
   a.window = opts->window;
   a.scale = opts->scale;
   const float cap = opts->softcap;
-  if (cap > 0.f) a.softcap = {cap, 1.f / cap, (float)(2.0 * M_LOG2E / cap), -2.f * cap};
+  if (cap > 0.f) a.softcap = {cap, (float)(2.0 * M_LOG2E / cap), -2.f * cap};
   return launched(mxq::launch_attn_paged(a, (hipStream_t)stream));
 }
 

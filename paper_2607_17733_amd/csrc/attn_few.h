@@ -318,7 +318,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
       for (int i = 0; i < 8; ++i) x[i] = sa[e][i >> 2][i & 3];
       float scale = sc;
       if (a.softcap.cap > 0.f) {
-        cap_scores<F32, 8>(x, sc, a.softcap);
+        cap_scores<F32, 8>(x, sc, a.softcap.cap, a.softcap.k, a.softcap.two);
         scale = 1.f;
       }
       if (a.slopes) {

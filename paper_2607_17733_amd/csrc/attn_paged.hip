@@ -143,8 +143,7 @@ struct TileRow {
   int pw0, pw1;                          // the wave's first and last
   int last;                              // the last token that one of the wave's rows may see
   int window, pre;
-  float sc, slope;
-  SoftCap softcap;
+  float sc, slope, cap, cap_k;
   bool biased;
 };
 
@@ -175,8 +174,8 @@ template <bool F32>
 __device__ __forceinline__ float adjust(const TileRow &w, int t0, int h, f16v &s) {
   auto c = [](int i) { return 8 * (i >> 2) + (i & 3); };
   float scale = w.sc;
-  if (w.softcap.cap > 0.f) {
-    cap_scores<F32, 16>(s, scale, w.softcap);
+  if (w.cap > 0.f) {
+    cap_scores<F32, 16>(s, scale, w.cap, w.cap_k, -2.f * w.cap);
     scale = 1.f;
   }
   if (w.biased) {
@@ -448,7 +447,8 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t tiles, int few_rows) 
   w.window = (int)(a.window && a.window < INT32_MAX ? a.window : INT32_MAX);
   w.pre = q.pre;
   w.sc = (a.scale == 0.f ? 1.f : fabsf(a.scale)) * (a.softcap.cap > 0.f ? 1.f : kUnit<F32>);
-  w.softcap = a.softcap;
+  w.cap = a.softcap.cap;
+  w.cap_k = a.softcap.k;
   w.biased = a.slopes != nullptr;
   w.slope = a.slopes ? a.slopes[hd] * kUnit<F32> : 0.f;
 

@@ -240,27 +240,28 @@ __device__ inline float *part_o(const AttnPagedArgs &a, int split, int64_t row) 
 
 // The N scores x, capped: cap tanh(x sc / cap), in the unit of the softmax.
 template <bool F32, int N, class V>
-__device__ __forceinline__ void cap_scores(V &x, float sc, const SoftCap &c) {
+__device__ __forceinline__ void cap_scores(V &x, float sc, float cap, float k, float two) {
   // tanh y = 1 - 2 / (e^2y + 1) is good to 2.6 x 2^-23 of 1, so the score to that part of
   // the cap: 2e-5 at 64, a hundredth of what rounding its weight to bf16 costs.  Larger caps
   // take the series below 1/8 (its next term is 2^-29 of it), so that the error is a part
   // of the score.  (2048 tokens over 8192, 64 query and 8 KV heads: 690 us and 778.)
   if constexpr (F32) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = c.cap * tanhf(x[i] * sc / c.cap);
-  } else if (c.cap <= 64.f) {
+    for (int i = 0; i < N; ++i) x[i] = cap * tanhf(x[i] * sc / cap);
+  } else if (cap <= 64.f) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float e = __builtin_amdgcn_exp2f(x[i] * sc * c.k);
-      x[i] = fmaf(c.two, __builtin_amdgcn_rcpf(e + 1.f), c.cap) * kUnit<F32>;
+      const float e = __builtin_amdgcn_exp2f(x[i] * sc * k);
+      x[i] = fmaf(two, __builtin_amdgcn_rcpf(e + 1.f), cap) * kUnit<F32>;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float z = x[i] * sc, y = z * c.inv, y2 = y * y;
-      const float e = __builtin_amdgcn_exp2f(y * (2.f * kLog2e));
-      const float p = fmaf(y2, fmaf(y2, fmaf(y2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
-      x[i] = (fabsf(y) < 0.125f ? z * p : c.cap * fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f)) * kUnit<F32>;
+      const float z = x[i] * sc, t = z * k, u = t * t;   // y = t s, s = ln 2 / 2
+      constexpr float s2 = 0.120113253f;
+      const float e = __builtin_amdgcn_exp2f(t);
+      const float p = fmaf(u, fmaf(u, fmaf(u, -17.f / 315.f * s2 * s2 * s2, 2.f / 15.f * s2 * s2), s2 / -3.f), 1.f);
+      x[i] = (fabsf(t) < 0.36f ? z * p : cap * fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f)) * kUnit<F32>;
     }
   }
 }

@@ -185,8 +185,7 @@ hipError_t launch_kv_read(const KvReadArgs &args, hipStream_t s);
 
 // Attention over the paged cache (attn_paged.hip).
 struct SoftCap {
-  float cap;               // 0: none
-  float inv, k, two;       // 1 / cap, 2 log2(e) / cap, -2 cap
+  float cap, k, two;       // (0: none), 2 log2(e) / cap, -2 cap
 };
 struct AttnPagedArgs {
   PageGeo geo;

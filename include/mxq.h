@@ -615,9 +615,10 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  *   batch   S sequences; T rows of q and o; cu_q DEVICE int32 [S + 1], from 0
  *           up, not decreasing, at most T; kv_len DEVICE int32 [S]; table DEVICE
  *           int32, row s at table + s * ld_table, table_pages entries.  max_q >=
- *           every n and max_kv >= every kv_len (HOST: they size the launch; rows
- *           past max_q are not computed, longer lengths are cut).  A length also
- *           ends after table_pages pages.  A table entry outside [0, pages) is
+ *           every n and max_kv >= every kv_len (HOST: they size the launch; a
+ *           sequence's rows past its first max_q are not computed and stay as
+ *           they are, longer lengths are cut).  A length also ends after
+ *           table_pages pages.  A table entry outside [0, pages) is
  *           never followed: its tokens read as zero rows.
  *   q       DEVICE bf16, row t, head h at q + t * q_ts + h * q_hs, 16-byte
  *           aligned, strides multiples of 8.

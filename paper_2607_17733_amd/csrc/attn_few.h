@@ -186,8 +186,8 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
   const Seq q = seq_at(a, s);
   if (q.n == 0 || (int64_t)q.n * G > 16 * NC) return;
   const int rows = q.n * G;
-  const int p0 = q.len - q.n;                              // the first row's position
-  const Steps st = steps_of<kFewChunk>(a, q, p0, (int64_t)q.len - 1);
+  const int p0 = q.p0;
+  const Steps st = steps_of<kFewChunk>(a, q, p0, (int64_t)p0 + q.n - 1);
   const int v0 = (int)((int64_t)st.count * split / splits);
   const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
 

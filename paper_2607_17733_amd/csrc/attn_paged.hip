@@ -131,6 +131,7 @@ __device__ inline bool find_tile(const AttnPagedArgs &a, int64_t index, int64_t 
   q.s = lo + k;
   q.row0 = __builtin_amdgcn_readlane(x.row0, k);
   q.n = __builtin_amdgcn_readlane(x.n, k);
+  q.p0 = __builtin_amdgcn_readlane(x.p0, k);
   q.len = __builtin_amdgcn_readlane(x.len, k);
   q.pre = __builtin_amdgcn_readlane(x.pre, k);
   tile = (int)(number - first);
@@ -429,7 +430,7 @@ void attn_tile_kernel(AttnPagedArgs a, int splits, int64_t tiles, int few_rows) 
   if (!find_tile<kRows>(a, rest / (uint32_t)splits, tiles, few_rows, q, tile)) return;
   const int64_t rows = (int64_t)q.n * G, r0 = (int64_t)tile * kRows;
   if (r0 >= rows || rows <= few_rows) return;
-  const int64_t p0 = (int64_t)q.len - q.n;                 // the first row's position
+  const int64_t p0 = q.p0;
   const Steps st = steps_of<kTok>(a, q, p0 + r0 / G, p0 + (min(r0 + kRows, rows) - 1) / G);
   const int v0 = (int)((int64_t)st.count * split / splits);
   const int v1 = (int)((int64_t)st.count * (split + 1) / splits);
@@ -546,22 +547,28 @@ void attn_merge_kernel(AttnPagedArgs a, int splits, int few_rows, int most, int6
   if (!here) {
   } else if (most > 0) {                                   // row id % (most Hq) of a short sequence
     const int64_t per = most * a.Hq;
-    const int s = (int)(id / per), c0 = a.cu_q[s], n = a.cu_q[s + 1] - c0;
+    const int s = (int)(id / per), c0 = a.cu_q[s], n = min(a.cu_q[s + 1] - c0, (int)a.max_q);
     const int64_t r = id - s * per;
     here = r < n * a.Hq && n * (int64_t)a.G <= few_rows && c0 >= 0 && c0 + (int64_t)n <= a.T;
     row = here ? c0 * a.Hq + r : 0;
   } else {
-    const int tok = (int)(row / a.Hq);
+    const int tok = (int)(row / a.Hq), even = min(tok / (int)a.max_q, (int)a.S - 1);
+    // its sequence: as if all had max_q rows, the loads in flight together (32 sequences of 40 rows:
+    // 96.3 us, always searched 97.7), else the last one that begins at tok or before
+    int c0 = a.cu_q[even], c1 = a.cu_q[even + 1];
     here = tok >= a.cu_q[0] && tok < a.cu_q[a.S];          // else no sequence's row
-    if (here && few_rows > 0) {                            // not the other kernel's rows
-      int lo = 0, hi = (int)a.S - 1;                       // the last sequence that begins at tok or before
+    if (here && (tok < c0 || tok >= c1)) {
+      int lo = 0, hi = (int)a.S - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
         if (a.cu_q[mid] <= tok) lo = mid;
         else hi = mid - 1;
       }
-      here = (int64_t)(a.cu_q[lo + 1] - a.cu_q[lo]) * a.G > few_rows;
+      c0 = a.cu_q[lo];
+      c1 = a.cu_q[lo + 1];
     }
+    const int n = min(c1 - c0, (int)a.max_q);              // not the other kernel's rows, nor those past max_q
+    here = here && tok - c0 < n && (int64_t)n * a.G > few_rows;
   }
   if (!here) splits = 0;
   const float ninf = -__builtin_inff();

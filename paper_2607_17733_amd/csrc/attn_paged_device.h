@@ -186,7 +186,8 @@ __device__ inline int pick(const int (&v)[4], int i) {
 
 // A sequence's rows and tokens, as the kernel may use them.
 struct Seq {
-  int s, row0, n;                        // its first query row, and how many
+  int s, row0, n;                        // its first query row, and how many are computed
+  int p0;                                // that row's position: the rows of q are the last tokens
   int len;                               // cached tokens
   int pre;                               // the tokens that every row sees
 };
@@ -196,10 +197,11 @@ __device__ inline Seq seq_of(const AttnPagedArgs &a, int s, int begin, int end, 
   const int T = (int)a.T;
   const int c0 = min(max(begin, 0), T), c1 = min(max(end, c0), T);
   q.row0 = c0;
-  q.n = c1 - c0;
+  q.n = min(c1 - c0, (int)a.max_q);
   int64_t len = min((int64_t)kv_len, a.max_kv);
   len = min(len, a.table_pages << a.geo.lg_page);
   q.len = (int)max(len, (int64_t)0);
+  q.p0 = q.len - (c1 - c0);
   q.pre = min(max(prefix, 0), q.len);
   return q;
 }

@@ -881,7 +881,8 @@ def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: in
     Hq, 128] (strided), sequence s owning the rows cu_q[s] .. cu_q[s + 1] (int32
     [S + 1]), which are the last of its kv_len[s] (int32 [S]) cached tokens; its
     pages are table[s] (int32 [S, n]).  max_q and max_kv bound the sequences'
-    rows and lengths.  A row sees the tokens up to its own, of those the last
+    rows and lengths (of more rows the first max_q are computed; the others, as
+    rows of no sequence, stay as `out` holds them).  A row sees the tokens up to its own, of those the last
     `window` (0: all), and the first prefix[s] (int32 [S]); scores are capped by
     softcap * tanh(x / softcap) and lowered by slopes[h] (float32 [Hq]) times the
     distance.  Returns bf16 or float32 (`dtype`) [T, Hq, 128]."""

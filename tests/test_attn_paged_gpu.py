@@ -461,3 +461,29 @@ def test_caps_far_above_the_scores(cap):
         assert np.all(d <= tol16 + tol32 * (42 / 131))
     slopes = [2.0 ** -(i + 1) for i in range(8)]
     Batch(3001, lens, 8, 2, softcap=cap, slopes=slopes, window=70, prefix=[2, 0, 60]).check(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,Hq,Hkv,max_q", [
+    ([(3, 100), (1, 50), (0, 20), (40, 200)], 16, 2, 1),             # the kernel for few rows alone
+    ([(3, 5000), (1, 2050), (7, 7)], 8, 1, 2),                       # and its splits
+    ([(60, 300), (1, 200), (5, 90), (41, 41)], 8, 2, 40),            # both kernels
+    ([(60, 3000), (1, 2000), (5, 90)], 8, 1, 33),                    # and the splits of both
+    ([(60, 300), (3, 90)], 40, 1, 20),                               # tiles alone
+    ([(60, 3000), (20, 500)], 8, 1, 40),                             # as many rows as 2 x max_q: tiles, split
+    ([(5 + i % 50, 60 + i) for i in range(70)], 4, 2, 17)])          # more than 64 sequences
+def test_rows_past_max_q_are_not_computed(lens, Hq, Hkv, max_q, dtype):
+    say("max_q", len(lens), Hq, Hkv, max_q, dtype)
+    b = Batch(3100 + max_q, lens, Hq, Hkv)
+    assert b.max_q > max_q
+    b.max_q = max_q
+    out = torch.full((b.T, Hq, D), 7.0, dtype=dtype, device="cuda")
+    work = torch.full((max(16, mxq.attn_paged_work_bytes(b.cache, b.S, b.T, Hq, max_q, b.max_kv)),), 0x41,
+                      dtype=torch.uint8, device="cuda")
+    b.run(dtype, out=out, work=work)
+    o, tol32, tol16 = b.expected()
+    got = out.double().cpu().numpy()
+    first = np.concatenate([np.arange(n) < max_q for n, _ in lens])
+    assert np.all(got[~first] == 7.0)
+    # (the others stand where they stood: at their own positions)
+    assert np.all(np.abs(got - o)[first] <= (tol32 if dtype is torch.float32 else tol16)[first])

@@ -582,7 +582,8 @@ int64_t mxq_kv_page_exp_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_toke
  * mxq_kv_read: the rows of the given slots as the bf16 values that they stand
  * for, q * 2^(E - 127 - (m - 2)), which is exact, into k and v DEVICE bf16
  * [n][Hkv][128], 16-byte aligned (either may be NULL); zeros for a slot
- * outside the cache.
+ * outside the cache.  Only -2^128 (the lowest mantissa of MXQ_CLAMP_FULL with
+ * E = 254) is out of bf16's range: it reads as bf16's lowest value.
  * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, counts, page_tokens, rot, T / 16 *
  * (2 Hkv + Hq) of 2^24 or more),
  * MXQ_ERR_UNSUPPORTED (a permutation, layout), MXQ_ERR_NULL, MXQ_ERR_ALIGN (also

@@ -203,10 +203,13 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvReadArgs a) {
     int q[8];
     load_packed(mant, m, j, q);
     const int sh = (int)(is_v ? a.v_exp : a.k_exp)[(base + i) * 4 + b] - 127 - (m - 2);
+    // exact, at most 8 significant bits, but for -2^128 (the full clamp's lowest mantissa with
+    // E = 254), which is out of bf16's range: its lowest value, not an infinity
+    auto value = [&](int i) {
+      return f32_to_bf16(fmaxf(__builtin_amdgcn_ldexpf((float)q[i], sh), -0x1.FEp127f));
+    };
 #pragma unroll
-    for (int k = 0; k < 4; ++k)                            // exact: at most 8 significant bits
-      y[k] = f32_to_bf16(__builtin_amdgcn_ldexpf((float)q[2 * k], sh)) |
-             f32_to_bf16(__builtin_amdgcn_ldexpf((float)q[2 * k + 1], sh)) << 16;
+    for (int k = 0; k < 4; ++k) y[k] = value(2 * k) | value(2 * k + 1) << 16;
   }
   *(rope_u4 *)((is_v ? a.v : a.k) + (t * g.Hkv + head) * kD + 8 * lane) = y;
 }

@@ -234,3 +234,23 @@ def test_a_single_token_in_place_in_fused_rows():
     got = mxq.kv_append(c, k, v, torch.zeros(1, dtype=torch.int64, device="cuda"), pos=pos, rope=table, q=q, q_out=q)
     torch.cuda.synchronize()
     assert got is q and np.array_equal(bits_of(fused.cpu()), want)
+
+
+def test_lowest_values_of_the_full_clamp_read_as_the_lowest_bf16():
+    # E = 254 and the lowest mantissa stand for -2^128, which bf16 does not hold: the lowest one it has,
+    # which goes back into a cache as the same row (an infinity would take its whole block with it)
+    low = float(torch.finfo(torch.bfloat16).min)
+    x = _rows(16, 2, 11)
+    x[::3, :, ::5] = low
+    x[1, 0] = -low
+    for widths in ([3, 3, 3, 3], [4, 4, 4, 4], [6, 6, 6, 6], [8, 8, 8, 8], [3, 4, 6, 8]):
+        c, again = (_cache(widths, 2, 1, 16, seed=s, clamp="full") for s in (1, 9))
+        slots = torch.arange(16, device="cuda")
+        mxq.kv_append(c, x.cuda(), x.cuda(), slots)
+        k, v = mxq.kv_read(c, slots)
+        ref = opaged.values(bits_of(x), widths, 0, 1)
+        assert ref.min() == -2.0 ** 128
+        assert np.array_equal(k.cpu().double().numpy(), np.maximum(ref, low)) and torch.equal(k, v)
+        mxq.kv_append(again, k, v, slots)
+        k2, v2 = mxq.kv_read(again, slots)
+        assert torch.equal(k2[::3], k[::3]) and torch.equal(v2[::3], v[::3])

@@ -603,7 +603,7 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  * tokens, mixed in one ragged batch.  Sequence s has kv_len[s] tokens in the
  * pages table[s][0], table[s][1], ..., and its n = cu_q[s+1] - cu_q[s] query
  * rows cu_q[s] .. are its last n tokens: row i stands at position
- * p = kv_len[s] - n + i.  With the dequantized K and V, per query head h over
+ * p = kv_len[s] - n + i.  With K and V as mxq_kv_read gives them, per query head h over
  * KV head h / (Hq / Hkv),
  *   x_j = scale * sum_d q[h][d] K[j][d];
  *   x_j = softcap * tanh(x_j / softcap)           (softcap > 0);

@@ -19,6 +19,7 @@ typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
+typedef unsigned short us8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s4 lds_s4;
 
 constexpr int kD = 128;
@@ -93,7 +94,7 @@ __device__ inline uint32_t low_nibbles_else(uint32_t a, uint32_t b) {
 
 // The largest exponent whose scale keeps the arithmetic below inside the float
 // range; a block beyond it is dequantized there and scaled again.
-constexpr int max_exp(int m) { return m == 3 ? 255 : m == 4 ? 247 : 253; }
+constexpr int max_exp(int m) { return m == 4 ? 247 : 253; }
 
 // Group j (eight values) of a block, in slot order: q * 2^(E - 127 - (m - 2)), in two
 // parts (so that a caller can put other work between them): integers, four values each.
@@ -167,13 +168,17 @@ __device__ __forceinline__ bf8 dequant8(const RawBlock &r, int j, int E) {
 }
 
 // The rest of the scale of blocks beyond max_exp.  (E = 255 is no exception: the
-// quantizer writes zero mantissas with it.)
+// quantizer writes zero mantissas with it.)  -2^128, the full clamp's lowest mantissa
+// with E = 254, counts as bf16's lowest value: as an infinity it would be a NaN in the
+// rows that do not see its token, times their probability of zero.  (As bits it is the one
+// above the lowest value; a float maximum spills registers in the kernel for few rows.)
 template <int M>
 __device__ __forceinline__ void big_scale(bf8 &v, int E) {
-  if constexpr (M == 3) return;
   const float f = __builtin_amdgcn_ldexpf(1.f, max(E - max_exp(M), 0));
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (__bf16)((float)v[i] * f);
+  const us8 low = {0xFF7F, 0xFF7F, 0xFF7F, 0xFF7F, 0xFF7F, 0xFF7F, 0xFF7F, 0xFF7F};
+  v = __builtin_bit_cast(bf8, __builtin_elementwise_min(__builtin_bit_cast(us8, v), low));
 }
 
 // ---------------------------------------------------------------------------

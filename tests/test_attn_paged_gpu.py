@@ -487,3 +487,35 @@ def test_rows_past_max_q_are_not_computed(lens, Hq, Hkv, max_q, dtype):
     assert np.all(got[~first] == 7.0)
     # (the others stand where they stood: at their own positions)
     assert np.all(np.abs(got - o)[first] <= (tol32 if dtype is torch.float32 else tol16)[first])
+
+
+@pytest.mark.parametrize("widths", [(3, 3, 3, 3), (4, 4, 4, 4), (6, 6, 6, 6), (8, 8, 8, 8), (3, 4, 6, 8)])
+def test_lowest_values_of_the_full_clamp_stay_out_of_rows_that_do_not_see_them(widths):
+    # -2^128, which the full clamp's lowest mantissa stands for with E = 254, has no bf16: in a token that
+    # a row does not see it must not reach the row (0 x infinity)
+    b = Batch(3200, [(1, 60), (40, 100), (5, 40)], 4, 2, widths=widths, window=9)
+    fmt = mxq.Format(D, list(widths), clamp="full")
+    cache = mxq.PagedCache(fmt, 2, b.cache.pages, b.page)
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((200, 2, D), generator=g).to(torch.bfloat16)
+    y = x.clone()
+    low = torch.tensor([5, 59, 60, 120, 159, 160 + 39, 160])     # the batch's rows in the cache, by sequence
+    y[low] = torch.finfo(torch.bfloat16).min
+    b.cache = cache
+    rows = torch.arange(b.T)
+    pos = torch.cat([torch.tensor([59]), torch.arange(60, 100), torch.arange(35, 40)])
+    seq = torch.tensor([0] + [1] * 40 + [2] * 5)
+    sees = torch.zeros(b.T, dtype=torch.bool)
+    for t in low.tolist():
+        s = 0 if t < 60 else 1 if t < 160 else 2
+        j = t - (0, 60, 160)[s]
+        sees |= (seq == s) & (j <= pos) & (pos - j < 9)
+    assert sees.any() and not sees.all()
+    for dtype in TYPES:
+        mxq.kv_append(cache, x.cuda(), x.cuda(), b.slots)
+        want = b.run(dtype)
+        mxq.kv_append(cache, x.cuda(), y.cuda(), b.slots)
+        got = b.run(dtype)
+        keep = rows[~sees].cuda()
+        assert torch.equal(got[keep], want[keep])
+        assert not got.isnan().any()

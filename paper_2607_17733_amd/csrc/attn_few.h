@@ -276,7 +276,7 @@ void attn_few_kernel(AttnPagedArgs a, int splits) {
         for (int k = 0; k < Mx::kWords; ++k) c.k[mt].w[k] = c.v[mt].w[k] = 0u;
         c.k[mt].ex = c.v[mt].ex = 0u;
       }
-    if (t0 + kFewChunk > q.len) {                          // places past the last token: tiny values
+    if (t0 > q.len - kFewChunk) {                          // places past the last token: tiny values
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
         if (t0 + 16 * mt + n > last) c.k[mt].ex = c.v[mt].ex = 0u;

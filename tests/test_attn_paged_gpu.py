@@ -519,3 +519,25 @@ def test_lowest_values_of_the_full_clamp_stay_out_of_rows_that_do_not_see_them(w
         keep = rows[~sees].cuda()
         assert torch.equal(got[keep], want[keep])
         assert not got.isnan().any()
+
+
+@pytest.mark.parametrize("q", [1, 40])
+def test_the_longest_cache(q):
+    # 2^31 - 1 tokens, every table entry the same page, a window that ends at the last one: the places are
+    # those of 1023 tokens, and so is the result, bit for bit; the place behind them holds infinities
+    n, short = 2 ** 31 - 1, 1023
+    cache = mxq.PagedCache(mxq.Format(D, [4, 4, 6, 8]), 1, 2, 1024)
+    for t in cache.k + cache.v:
+        t.fill_(0x77)
+    cache.k[1].fill_(255)
+    cache.v[1].fill_(255)
+    g = torch.Generator().manual_seed(7)
+    x = torch.randn((short, 1, D), generator=g).to(torch.bfloat16).cuda()
+    mxq.kv_append(cache, x, x.flip(0), torch.arange(1024, 1024 + short, device="cuda"))
+    table = torch.ones((1, 2 ** 21), dtype=torch.int32, device="cuda")
+    cu = torch.tensor([0, q], dtype=torch.int32, device="cuda")
+    xq = torch.randn((q, 8, D), generator=g).to(torch.bfloat16).cuda()
+    for dtype in TYPES:
+        got, want = (mxq.attn_paged(xq, cache, cu, torch.tensor([L], dtype=torch.int32, device="cuda"), table,
+                                    q, n, 0.1, window=50, dtype=dtype) for L in (n, short))
+        assert torch.equal(got, want) and bool(torch.isfinite(got).all()) and bool(got.any())

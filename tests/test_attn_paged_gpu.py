@@ -541,3 +541,34 @@ def test_the_longest_cache(q):
         got, want = (mxq.attn_paged(xq, cache, cu, torch.tensor([L], dtype=torch.int32, device="cuda"), table,
                                     q, n, 0.1, window=50, dtype=dtype) for L in (n, short))
         assert torch.equal(got, want) and bool(torch.isfinite(got).all()) and bool(got.any())
+
+
+@pytest.mark.parametrize("q", [1, 64])
+def test_float32_results_use_all_bits_of_the_probabilities(q):
+    # Two tokens, both in the prefix that every row sees.  Scores 0 and x, x a value of q itself (the key is
+    # one in a single place: an exact product); the values 0 and 1: o = e^x / (1 + e^x).  The exponential: a
+    # few units and one of its argument, as in paged_util, on each side; one rounding each of the sum, the
+    # reciprocal and the product.  The value product is exact with three bf16 terms of the probability; with
+    # two it would be off by up to 2^-18 of it.
+    cache = mxq.PagedCache(mxq.Format(D, [4, 4, 4, 8]), 1, 1, 16)
+    k = torch.zeros((2, 1, D), dtype=torch.bfloat16)
+    v = k.clone()
+    k[1, 0, 40], v[1] = 1.0, 1.0
+    mxq.kv_append(cache, k.cuda(), v.cuda(), torch.arange(2, device="cuda"))
+    xq = torch.zeros((q, 16, D), dtype=torch.bfloat16)
+    g = torch.Generator().manual_seed(11)
+    x = -(torch.rand((q, 16), generator=g) * 2).to(torch.bfloat16)
+    xq[:, :, 40] = x
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = mxq.attn_paged(xq.cuda(), cache, i32(0, q), i32(2), i32(0).view(1, 1), q, 2, 1.0, prefix=i32(2),
+                         dtype=torch.float32).double().cpu()
+    e = x.double().exp()
+    ref = e / (1 + e)
+    u = 2.0 ** -24
+    bound = ref * u * ((4 + 4 * x.double().abs()) + 3)
+    assert bool(((got - ref[..., None]).abs() <= bound[..., None]).all())
+    # (the inputs tell two terms from three)
+    p = e.float()
+    hi = p.to(torch.bfloat16).float()
+    two = (hi + (p - hi).to(torch.bfloat16).float()).double()
+    assert bool(((two - e).abs() / (1 + e) > 2 * bound).any())

@@ -572,3 +572,31 @@ def test_float32_results_use_all_bits_of_the_probabilities(q):
     hi = p.to(torch.bfloat16).float()
     two = (hi + (p - hi).to(torch.bfloat16).float()).double()
     assert bool(((two - e).abs() / (1 + e) > 2 * bound).any())
+
+
+def _waves(T, G, Hkv, max_kv, cus):
+    """Waves per tile and splits of the tiles, by the plan's rule for an uneven batch."""
+    steps, t4, t8 = -(-max_kv // 64), T * G // 128 + 1, T * G // 256 + 1
+    n4, n8 = (max(1, min(w // (t * Hkv), steps // 4, 256)) for w, t in ((2 * cus, t4), (cus, t8)))
+    wgs = t8 * Hkv * n8
+    eight = G >= 4 and 16 * wgs >= 15 * cus * -(-wgs // cus) and 12 * t8 <= 7 * t4
+    return (8, n8) if eight else (4, n4)
+
+
+@pytest.mark.parametrize("S,T,kv,Hq,Hkv,waves,split", [
+    (65, 1940, 1500, 32, 4, 8, False),              # whole rounds of full tiles
+    (130, 1290, 1500, 16, 2, 8, True),              # and split
+    (100, 580, 3000, 8, 1, 4, True)])               # few rows over long caches
+def test_more_than_64_sequences_in_every_kind_of_tile(S, T, kv, Hq, Hkv, waves, split):
+    say("many sequences", S, T, kv, Hq, Hkv)
+    # two chunks among sequences that decode, draft or bring nothing
+    lens = [((1, 30 + s), (0, 9), (3, 50), (0, 0), (17, 70))[s % 5] for s in range(S)]
+    rest = T - sum(n for s, (n, _) in enumerate(lens) if s not in (3, S - 2))
+    lens[3], lens[S - 2] = (rest // 8, kv), (rest - rest // 8, rest)
+    b = Batch(3300 + S, lens, Hq, Hkv, page=64, widths=(4, 4, 6, 8))
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    got, n = _waves(T, Hq // Hkv, Hkv, b.max_kv, cus)
+    if cus == 256:
+        assert got == waves and (n > 1) == split, (got, n)
+    for dtype in TYPES:
+        b.check(dtype, seqs=[0, 1, 2, 3, 4, 34, 63, 64, S - 1])

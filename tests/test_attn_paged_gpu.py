@@ -600,3 +600,15 @@ def test_more_than_64_sequences_in_every_kind_of_tile(S, T, kv, Hq, Hkv, waves, 
         assert got == waves and (n > 1) == split, (got, n)
     for dtype in TYPES:
         b.check(dtype, seqs=[0, 1, 2, 3, 4, 34, 63, 64, S - 1])
+
+
+def test_a_few_rows_among_many_empty_sequences():
+    # tiles are launched for all 65536 of them, with as many splits as a dispatch has room for
+    lens = [(0, 0)] * 65536
+    lens[7], lens[40000], lens[65535] = (1, 20), (34, 60), (5, 300)
+    b = Batch(3400, lens, 8, 1)
+    b.max_kv = 65536
+    n = mxq.attn_paged_work_bytes(b.cache, b.S, b.T, 8, b.max_q, b.max_kv) // (4 * b.T * 8 * (D + 2))
+    assert n > 100
+    for dtype in TYPES:
+        b.check(dtype, seqs=[7, 40000, 65535])

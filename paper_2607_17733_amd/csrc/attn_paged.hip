@@ -19,12 +19,16 @@
 //
 // A step's 32 products of a wave hold its matrix core for 1024 cycles; behind them
 // go the exponentials, the sums and the dequantization, about as many issue cycles.
-// 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1050 us, 0.98 PFLOP/s
+// 2048 tokens over 16384, 64 query and 8 KV heads, 4-bit: 1040 us, 0.99 PFLOP/s
 // (1.24 to 1.37 by a large library product), the matrix cores 41 % and the vector
 // units 55 % busy by the counters: softmax and dequantization bound it.
+// For a bf16 result the probabilities enter the second product rounded to bf16 (the
+// result is then 0.0018 to 0.0022 off the exact one, 0.0017 of it its own rounding), for
+// a float32 one as three bf16 terms, which are they exactly: 1945 us.
 //
-// Sequences with at most 32 query rows per KV head (decoding, drafted tokens) have
-// a kernel of their own (attn_few.h).  The tokens of a sequence are split over
+// Sequences with few query rows per KV head (decoding, drafted tokens) have a kernel of
+// their own (attn_few.h): up to 32 where no sequence of the batch has more, beside tiles
+// up to 16 (32 with 17 to 32 query heads per KV head).  The tokens of a sequence are split over
 // workgroups where there are few rows; the splits' results are merged in order.
 #include <algorithm>
 
@@ -676,7 +680,7 @@ struct Plan {
 Plan plan_of(const AttnPagedArgs &a) {
   Plan p = {0, 0, 4, 1};
   const int64_t Hkv = a.geo.Hkv, most = a.max_q * a.G, cus = device_cu_count();
-  const bool even = a.T == a.S * a.max_q;                  // every sequence has max_q rows
+  const bool even = a.T == a.S * a.max_q;                  // every sequence has max_q tokens
   auto split = [](int64_t wgs, int64_t want, int64_t steps, int64_t least) {
     const int64_t n = std::min(want / std::max<int64_t>(wgs, 1), steps / least);
     return std::max<int64_t>(1, std::min<int64_t>(n, kMaxSplits));
@@ -684,19 +688,23 @@ Plan plan_of(const AttnPagedArgs &a) {
   if (most > kFewMost) {
     const int64_t steps = (a.max_kv + kTok - 1) / kTok;
     auto tiles = [&](int64_t rows) { return even ? a.S * ((most + rows - 1) / rows) : a.T * a.G / rows + 1; };
-    // Splits: one round of workgroups (40 rows of 4 sequences: 384 in 91, 864 in 107), of
-    // at least four steps each; a CU holds one workgroup of eight waves, two of four.
+    // Splits: one round of workgroups (40 tokens of 4 sequences: 384 in 91, 864 in 107), of
+    // at least four steps each (of max_kv tokens: a window is not looked at); a CU holds one
+    // workgroup of eight waves, two of four.
     const int64_t t4 = tiles(128), t8 = tiles(256);
     const int64_t n4 = std::min(split(t4 * Hkv, 2 * cus, steps, 4), most_splits(a, 4));
     const int64_t n8 = std::min(split(t8 * Hkv, cus, steps, 4), most_splits(a, 8));
-    // Eight waves share the dequantization of K and V among twice the rows, but are one
-    // workgroup per CU, whose start and end nothing covers.  They need whole rounds of
-    // workgroups (rows over 16384 tokens: 2048 rows, two rounds, 1050 against 1150 with
-    // four waves; 512 rows, one, 297 and 328; but 1536, one and a half, 1016 and 948; 2
-    // prompts of 2731 in a window, 2.7, 122 and 114), tiles that are full (40 rows of
-    // 4 sequences, 320 of 512: 81 and 79), and rows that see the same
-    // steps, as those of a few tokens do (one query head per KV head, 2 x 2048 tokens:
-    // 135 and 129).
+    // Eight waves share the dequantization of K and V among twice the query rows, but are
+    // one workgroup per CU, whose start and end nothing covers.  They need whole rounds of
+    // workgroups: new tokens over 16384, 2048 (two rounds) take 1036 against 1125 with four
+    // waves, 480 (15 / 16 of one) 290 and 317, but 1536 (one and a half) 1011 and 930.  The
+    // border is on the safe side of the crossing: 1664 (1.6 rounds) take 1012 and 1099, but
+    // 2 prompts of 2731 in a window (2.7) 128 and 126.
+    // They need tiles that are full: 112 tokens of 16 sequences, 896 rows of 1024, take 279
+    // and 330, 40 of 4, 320 of 512, 82 and 80; safe again, 48 of 8, 384 of 512, take 87 and
+    // 98, 80 of 32, 640 of 768, 410 and 436.
+    // And rows that see the same steps, as those of a few tokens do: one query head per
+    // KV head, 2 x 2048 tokens, 135 and 130.
     const int64_t wgs = t8 * Hkv * n8;
     const bool whole = 16 * wgs >= 15 * cus * ((wgs + cus - 1) / cus), full = 12 * t8 <= 7 * t4;
     p.waves = a.G >= 4 && whole && full ? 8 : 4;

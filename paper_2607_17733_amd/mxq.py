@@ -885,7 +885,9 @@ def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: in
     rows of no sequence, stay as `out` holds them).  A row sees the tokens up to its own, of those the last
     `window` (0: all), and the first prefix[s] (int32 [S]); scores are capped by
     softcap * tanh(x / softcap) and lowered by slopes[h] (float32 [Hq]) times the
-    distance.  Returns bf16 or float32 (`dtype`) [T, Hq, 128]."""
+    distance.  Returns bf16 or float32 (`dtype`) [T, Hq, 128]: a bf16 result weighs
+    the values with probabilities rounded to bf16 (and their sum, in float32), a
+    float32 one with all their 24 bits, at up to twice the time."""
     dev = cache.device
     stream = _current(dev, "the cache")
     T, Hq, _ = _heads(q, "q", dev, None, 128)

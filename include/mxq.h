@@ -623,7 +623,8 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  *           never followed: its tokens read as zero rows.
  *   q       DEVICE bf16, row t, head h at q + t * q_ts + h * q_hs, 16-byte
  *           aligned, strides multiples of 8.
- *   o       DEVICE [T][Hq][128], bf16 or, with o_f32, float32, 16-byte aligned.
+ *   o       DEVICE [T][Hq][128], bf16 or, with o_f32, float32, 16-byte aligned;
+ *           must not overlap q.
  *   work    DEVICE, 16-byte aligned, work_bytes >= mxq_attn_paged_work_bytes:
  *           partial results (the size is that of the current device); needs no
  *           initialisation.  Calls that may overlap in time must not share it.
@@ -631,7 +632,8 @@ mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int6
  * statistics are float32.  For a float32 output the probabilities enter the
  * value product with all their 24 bits, for a bf16 one rounded to bf16; a
  * probability is at most e^4 before the division by their sum, and a sum of
- * probabilities times values past float32's range is infinite.  The tanh of a
+ * probabilities times values past float32's range is lost (infinite, or NaN
+ * where it is weighed with zero).  The tanh of a
  * bf16 result is good to 2^-21 (of a score at the cap) for caps up to 64, to
  * 2^-18 of each capped score for larger ones.  Calls repeat bit for bit.
  * Errors: check_fmt's; MXQ_ERR_SHAPE (K != 128, bad counts, Hq not a multiple

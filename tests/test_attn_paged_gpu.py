@@ -612,3 +612,55 @@ def test_a_few_rows_among_many_empty_sequences():
     assert n > 100
     for dtype in TYPES:
         b.check(dtype, seqs=[7, 40000, 65535])
+
+
+def test_a_layers_step_captured_and_replayed_with_other_inputs():
+    # append (queries rotated by the same launch), attention, rows read back, all in one graph with its own
+    # allocations, replayed with other rows, positions, slots and lengths, beside eager calls
+    Hq, Hkv, page, S, most = 8, 2, 16, 3, 400
+    g = torch.Generator().manual_seed(21)
+    fmt = mxq.Format(D, [3, 4, 6, 8])
+    pages = S * most // page
+    table = torch.randperm(pages, generator=g).int().view(S, -1).cuda()
+    rope = mxq.rope_table(mxq.rope_inv_freq(D)[0], most)
+    new = [1, 40, 5]
+    T = sum(new)
+    cu = torch.tensor([0, 1, 41, 46], dtype=torch.int32, device="cuda")
+    rows = torch.empty((T, Hq + 2 * Hkv, D), dtype=torch.bfloat16, device="cuda")
+    slots, pos = torch.empty(T, dtype=torch.int64, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda")
+    kv_len = torch.empty(S, dtype=torch.int32, device="cuda")
+
+    def fill(lens):
+        rows.copy_(torch.randn(rows.shape, generator=g))
+        at = torch.cat([torch.arange(L - n, L) for L, n in zip(lens, new)])
+        seq = torch.repeat_interleave(torch.arange(S), torch.tensor(new))
+        pos.copy_(at.int())
+        slots.copy_(table.cpu()[seq, at // page].long() * page + at % page)
+        kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+
+    def step(cache):
+        q, k, v = rows.split([Hq, Hkv, Hkv], dim=1)
+        qr = mxq.kv_append(cache, k, v, slots, pos=pos, rope=rope, q=q)
+        o = mxq.attn_paged(qr, cache, cu, kv_len, table, max(new), most, D ** -0.5, window=150, prefix=cu[1:])
+        return (qr, o, mxq.rope(qr, pos, rope)) + tuple(mxq.kv_read(cache, slots))
+
+    eager, graphed = (mxq.PagedCache(fmt, Hkv, pages, page) for _ in range(2))
+    fill([1, 40, 5])
+    for c in (eager, graphed):
+        step(c)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(graphed)
+    for lens in ([2, 80, 10], [3, 120, 15], [390, 333, 400], [4, 41, 16]):
+        fill(lens)
+        want = step(eager)
+        for t in got:
+            t.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        for a, b in zip(eager.k + eager.v, graphed.k + graphed.v):
+            assert torch.equal(a, b)

@@ -132,3 +132,24 @@ def test_no_rows_and_another_stream():
     side.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rows_past_four_billion_elements(interleaved):
+    # 70001 tokens of 512 heads of 128 values: 4.6e9 elements, in place; sampled rows against the oracle
+    T, H, D, rot = 70001, 512, 128, 64
+    x = torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 32
+    small = torch.randn((1001, H, D), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    for t in range(0, T, 1001):
+        n = min(1001, T - t)
+        x[t:t + n] = small[:n]
+    pos = torch.randint(0, 700, (T,), generator=torch.Generator().manual_seed(3)).int()
+    table = mxq.rope_table(mxq.rope_inv_freq(rot)[0], 700)
+    at = [0, 1, 32767, 32768, 65535, 65536, 65537, T - 1]          # (2^31 elements are 32768 tokens)
+    before = bits_of(x[at])
+    say("rope of 9 GB", interleaved)
+    y = mxq.rope(x, pos.cuda(), table, interleaved, out=x)
+    torch.cuda.synchronize()
+    assert y is x
+    assert _same(bits_of(x[at]), opaged.rope(before, pos.numpy()[at], table.cpu().numpy(), interleaved))

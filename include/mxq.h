@@ -58,7 +58,8 @@ extern "C" {
 #endif
 
 /* Raised when an entry point that was there changes; one that was added since
- * (mxq_calib_colsq_list) is found by its name. */
+ * (mxq_calib_colsq_list; what layers with experts and norms of queries and
+ * keys take) is found by its name. */
 #define MXQ_ABI_VERSION 12
 #define MXQ_BLOCK 32
 /* mxq_gemm uses the weight-streaming decode kernel up to this M (up to four
@@ -658,6 +659,168 @@ mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
                           const mxq_paged_batch *batch, const mxq_attn_opts *opts,
                           const uint16_t *q, int64_t Hq, int64_t q_ts, int64_t q_hs, void *o,
                           int o_f32, float *work, int64_t work_bytes, void *stream);
+
+/*
+ * Layers with experts: a router chooses k of E experts for every token, the
+ * tokens of an expert are multiplied with its weights, and a token's k results
+ * are added with the router's weights.  (The paper quantizes every linear of a
+ * decoder layer, Section 5; an expert's linears are such.)  Pair p = t * k + j
+ * is the j-th choice of token t; an id outside [0, E) is no choice: its pair
+ * takes no part and its rows are neither read nor written anywhere below.
+ *
+ * The plan of a batch lays the pairs out in rows of the operand image (layout
+ * (A)), each expert's rows from a multiple of 16 on, in the order of the pairs:
+ *   pairs    T * k, 0 .. 2^26.
+ *   experts  E, 1 .. 1024.
+ *   first    DEVICE int32 [E + 1], 16-byte aligned: expert e's rows are first[e]
+ *            .. first[e + 1] - 1 (its count rounded up to 16); first[0] = 0.
+ *   pair     DEVICE int32 [mxq_expert_rows(pairs, E)], 16-byte aligned: the pair
+ *            of each row, -1 for a row that holds none.
+ * mxq_expert_rows: the most rows that any choice needs, (pairs + 15 min(E,
+ * pairs)) rounded down to 16; negative mxq_status on bad counts.  So buffers and
+ * launches have the same size whatever the choice, and a captured step serves
+ * every batch of T tokens.  The calls that take a plan read it on the device: it
+ * is what mxq_route or mxq_expert_plan wrote for the same pairs and experts.
+ */
+typedef struct {
+  int64_t pairs;
+  int32_t experts;
+  int32_t reserved;        /* must be 0 */
+  int32_t *first;
+  int32_t *pair;
+} mxq_experts;
+
+int64_t mxq_expert_rows(int64_t pairs, int32_t experts);
+
+/*
+ * mxq_route: token t's experts from its scores x[e] = logits[t * ld + e].
+ *   MXQ_SCORE_SOFTMAX: s[e] = exp(x[e] - max x) / sum_e exp(x[e] - max x);
+ *   MXQ_SCORE_SIGMOID: s[e] = 1 / (1 + exp(-x[e])).
+ * Chosen are the k largest x[e] (both scores rise with x) or, with bias (DEVICE
+ * float [E], not NULL), the k largest s[e] + bias[e], formed in float64; equal
+ * ones go to the lowest index; ids[t][j] in falling order.  weights[t][j] = scale *
+ * s[ids[t][j]], or with normalise scale * s / (sum of the chosen s), in float32
+ * (relative error below 1e-6 where s is a normal float32); the bias enters the
+ * choice only.  A logit of -Inf or NaN, and a bias that makes s + bias -Inf or NaN,
+ * keeps its expert from being chosen, the former out of every sum too; +Inf
+ * counts as the largest float.  Where fewer than k are left, the other ids are -1
+ * and their weights 0; so are the weights of chosen scores that sum to 0.
+ *   T >= 0; E = plan's experts; k 1 .. min(E, 32); T * k = plan's pairs.
+ *   logits   DEVICE, float32 or (logits_f32 == 0) bf16, ld >= E, read only; any
+ *            alignment of its type.
+ *   ids      DEVICE int32 [T][k], weights DEVICE float [T][k], written, 16-byte
+ *            aligned.
+ *   plan     first and pair are written.
+ * mxq_expert_plan: the plan alone, from ids DEVICE int32 [pairs] (16-byte aligned).
+ * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (counts, ld, a scale that is not finite),
+ * MXQ_ERR_ALIGN, MXQ_ERR_UNSUPPORTED (score, reserved), MXQ_ERR_DEVICE.  With no
+ * pairs first is written (zeros).
+ */
+typedef enum { MXQ_SCORE_SOFTMAX = 0, MXQ_SCORE_SIGMOID = 1 } mxq_score;
+typedef struct {
+  int32_t k;
+  int32_t score;           /* mxq_score */
+  int32_t normalise;
+  float scale;
+  const float *bias;
+} mxq_route_opts;
+mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_f32, int64_t T,
+                     int64_t ld, int32_t *ids, float *weights, const mxq_experts *plan,
+                     void *stream);
+mxq_status mxq_expert_plan(const int32_t *ids, const mxq_experts *plan, void *stream);
+
+/*
+ * mxq_quantize_act and mxq_quantize_act_swiglu by a plan: image row r takes
+ * source row pair[r] / per_row (per_row = k: a row per token; 1: a row per pair),
+ * quantized as those calls quantize it; rows that hold no pair are not written.
+ *   fmt      as there; perms DEVICE int32 [E][K] (16-byte aligned), expert e's
+ *            permutation in place of fmt's, or NULL.
+ *   a, gate, up  DEVICE bf16 [pairs / per_row][ld].
+ *   per_row  divides pairs.
+ *   a_mant, a_exp  of mxq_act_bytes(fmt, R) and mxq_act_exp_bytes(fmt, R), R =
+ *            mxq_expert_rows(pairs, E).
+ * Errors: as those calls, and the plan's.
+ */
+mxq_status mxq_quantize_act_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                    const int32_t *perms, const uint16_t *a, int64_t per_row,
+                                    int64_t lda, uint8_t *a_mant, uint8_t *a_exp, void *stream);
+mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                           const int32_t *perms, const uint16_t *gate,
+                                           const uint16_t *up, int64_t per_row, int64_t ld,
+                                           uint8_t *a_mant, uint8_t *a_exp, void *stream);
+
+/*
+ * mxq_gemm for every expert's rows with its weights: y[p] = row of pair p times
+ * What of its expert, for the pairs of the plan; other rows of y stay as they are.
+ *   a_mant/a_exp  of mxq_quantize_act_experts (or its SiLU form) with the same fmt
+ *                 widths, round and clamp, and the same plan.
+ *   w_mant/w_exp  DEVICE: the experts' weights one after the other, each as
+ *                 mxq_pack_weights writes it for N columns, mxq_weight_bytes(fmt, N)
+ *                 and mxq_weight_exp_bytes(fmt, N) apart.
+ *   y             DEVICE [pairs][ldy], float32 or (y_f32 == 0) bf16 (the float32 sum
+ *                 rounded to nearest even), ldy >= N, 16-byte aligned.
+ * A row's result does not depend on the other rows of its call; which kernel runs
+ * goes by pairs and E, as for mxq_gemm, and the kernels differ in the order of
+ * their float32 sums.
+ * Errors: as mxq_gemm, and the plan's.
+ */
+mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t N,
+                            const uint8_t *a_mant, const uint8_t *a_exp, const uint8_t *w_mant,
+                            const uint8_t *w_exp, void *y, int y_f32, int64_t ldy, void *stream);
+
+/*
+ * out[t] = residual[t] + sum_j weights[t][j] * y[t * k + j], in float32, the
+ * choices in order (a product and its sum in one rounding), rounded once to out's
+ * type.  Pairs whose id lies outside [0, experts) are left out, whatever their
+ * rows and weights hold.
+ *   y         DEVICE [T * k][ldy], float32 or bf16 (y_f32).
+ *   ids, weights  DEVICE int32, float [T][k].
+ *   residual  DEVICE bf16 [T][ldr] or NULL (zeros); may be a bf16 out with ldo = ldr.
+ *   out       DEVICE [T][ldo], float32 or bf16 (out_f32); must not overlap y.
+ * Any alignment of the types; rows whose addresses and strides are multiples of 16
+ * bytes are read and written in such pieces.
+ * Errors: MXQ_ERR_NULL, MXQ_ERR_SHAPE (T < 0, N < 0, k < 1, experts < 1, T * k >
+ * 2^26, a leading dimension below N), MXQ_ERR_ALIGN, MXQ_ERR_DEVICE.
+ */
+mxq_status mxq_combine_experts(const void *y, int y_f32, int64_t ldy, const int32_t *ids,
+                               const float *weights, int64_t T, int64_t k, int32_t experts,
+                               int64_t N, const uint16_t *residual, int64_t ldr, void *out,
+                               int out_f32, int64_t ldo, void *stream);
+
+/*
+ * Queries and keys normalised per head and rotated in one pass.  A head's values
+ * x[0..D-1] become
+ *   ms = sum x^2 / D (float64),  r = 1 / sqrt(ms + eps) (float64),
+ *   v[d] = float32(float32(x[d] * r) * gain[d]),
+ * and v is rotated as mxq_rope rotates x, its results rounded once to bf16 (values at
+ * rot and above are bf16(v)).  A head of zeros gives zeros, also with eps = 0.
+ *   q_gain, k_gain  DEVICE bf16 [D], 16-byte aligned.
+ *   eps             >= 0, finite.
+ * mxq_rope_qk: q [T][Hq] and k [T][Hk] heads of D values, strided as mxq_rope's x,
+ * into q_out and k_out likewise (each may be its source with the same strides, else
+ * the four must not overlap).  Either may be absent (Hq or Hk 0).  1 <= D <= 4096, D even; 4-byte
+ * aligned, strides even.
+ * mxq_kv_append_norm: mxq_kv_append whose keys (and queries, where there are any)
+ * pass through this first: the rows are those of mxq_rope_qk followed by
+ * mxq_quantize_rows, bit for bit.  rope must not be NULL.
+ * Errors: as mxq_rope and mxq_kv_append; MXQ_ERR_NULL for a gain that is needed;
+ * MXQ_ERR_SHAPE for eps < 0, NaN or infinite.
+ */
+typedef struct {
+  const uint16_t *q_gain, *k_gain;
+  float eps;
+} mxq_qk_norm;
+mxq_status mxq_rope_qk(const mxq_rotary *rope, const mxq_qk_norm *norm, const int32_t *pos,
+                       int64_t T, int64_t D, const uint16_t *q, int64_t Hq, int64_t q_ts,
+                       int64_t q_hs, uint16_t *q_out, int64_t qo_ts, int64_t qo_hs,
+                       const uint16_t *k, int64_t Hk, int64_t k_ts, int64_t k_hs,
+                       uint16_t *k_out, int64_t ko_ts, int64_t ko_hs, void *stream);
+mxq_status mxq_kv_append_norm(const mxq_fmt *fmt, const mxq_paged_kv *cache,
+                              const mxq_qk_norm *norm, const uint16_t *k, int64_t k_ts,
+                              int64_t k_hs, const uint16_t *v, int64_t v_ts, int64_t v_hs,
+                              int64_t T, const int64_t *slots, const int32_t *pos,
+                              const mxq_rotary *rope, const uint16_t *q, int64_t Hq,
+                              int64_t q_ts, int64_t q_hs, uint16_t *q_out, void *stream);
 
 #ifdef __cplusplus
 }

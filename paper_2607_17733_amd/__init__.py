@@ -6,7 +6,9 @@ The compute path is the HIP library ``libmxq.so`` behind the C ABI in
 """
 _BINDING = ("Format", "MxqError", "quantize_act", "quantize_rows", "pack_weights", "gemm",
             "gemm_partials", "unpack_act", "unpack_weights", "lib", "rope_inv_freq", "rope_table",
-            "rope", "PagedCache", "kv_append", "kv_read", "attn_paged", "attn_paged_work_bytes")
+            "rope", "PagedCache", "kv_append", "kv_read", "attn_paged", "attn_paged_work_bytes",
+            "rope_qk", "ExpertPlan", "route", "expert_plan", "quantize_act_experts",
+            "quantize_act_swiglu_experts", "pack_experts", "gemm_experts", "combine_experts")
 
 
 def __getattr__(name):

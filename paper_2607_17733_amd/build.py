@@ -18,7 +18,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.cpp", "quantize.hip", "quantize_act.hip", "gemm_prefill.hip", "gemm_partials.hip",
            "decode.hip", "unpack.hip", "peaks.hip", "calib.hip", "attn.hip", "api_paged.cpp",
            "rope.hip", "kv_paged.hip", "attn_paged.hip", "attn_few_bf16.hip",
-           "attn_few_f32.hip"]
+           "attn_few_f32.hip", "api_experts.cpp", "experts.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

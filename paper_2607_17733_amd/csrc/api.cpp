@@ -92,7 +92,8 @@ enum QuantKind { kWeights, kImage, kRows };
 mxq_status quantize_common(const mxq_fmt *fmt, const uint16_t *src, int64_t rows,
                            int64_t ld, uint8_t *mant, uint8_t *exp, void *stream,
                            QuantKind kind, const uint16_t *gain = nullptr, float eps = 0.f,
-                           const uint16_t *src2 = nullptr) {
+                           const uint16_t *src2 = nullptr, const mxq::Groups *by = nullptr,
+                           int64_t per_row = 1, const int32_t *perms = nullptr) {
   Segs s;
   mxq_status st = check_fmt(fmt, &s);
   if (st != MXQ_OK) return st;
@@ -145,13 +146,19 @@ mxq_status quantize_common(const mxq_fmt *fmt, const uint16_t *src, int64_t rows
     a.out_erb = exp_rb(fmt);
   } else {
     a.out_rows = round_up(rows, mxq::kATileRows);
+    if (by) {
+      a.x = *by;
+      a.out_rows = by->rows;
+      a.per_row = (uint32_t)per_row;
+      a.perms = perms;
+    }
     a.img = mant;
     a.img_exp = exp;
     a.a_tile = mxq::a_tile_bytes(l_geo(s));
     a.a_tile_sc = mxq::a_tile_scale_bytes(l_geo(s));
   }
   // the activation quantizer stages its rows in LDS: one row must fit
-  if (mxq::quantize_act_lds(fmt->K, gain != nullptr) > mxq::kMaxLds)
+  if (mxq::quantize_act_lds(fmt->K, gain != nullptr) + (by ? mxq::kGroupLds : 0) > mxq::kMaxLds)
     return MXQ_ERR_UNSUPPORTED;
   return launched(mxq::launch_quantize_act(a, (hipStream_t)stream));
 }
@@ -314,6 +321,55 @@ mxq_status mxq_gemm(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_m
   return launched(M <= MXQ_DECODE_MAX_M && !mxq::gemm_takes_split(g)
                       ? mxq::launch_gemm_decode(g, s)
                       : mxq::launch_gemm_prefill(g, s));
+}
+
+static mxq_status quantize_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                   const int32_t *perms, const uint16_t *src, const uint16_t *src2,
+                                   int64_t per_row, int64_t ld, uint8_t *mant, uint8_t *exp,
+                                   void *stream) {
+  mxq::Groups g;
+  const mxq_status st = mxq::check_experts(plan, &g);
+  if (st != MXQ_OK) return st;
+  if (per_row < 1 || per_row > INT32_MAX || g.pairs % per_row) return MXQ_ERR_SHAPE;
+  if (!aligned16(perms)) return MXQ_ERR_ALIGN;
+  return quantize_common(fmt, src, g.pairs / per_row, ld, mant, exp, stream, kImage, nullptr, 0.f,
+                         src2, &g, per_row, perms);
+}
+
+mxq_status mxq_quantize_act_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                    const int32_t *perms, const uint16_t *a, int64_t per_row,
+                                    int64_t lda, uint8_t *a_mant, uint8_t *a_exp, void *stream) {
+  return quantize_experts(fmt, plan, perms, a, nullptr, per_row, lda, a_mant, a_exp, stream);
+}
+
+mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                           const int32_t *perms, const uint16_t *gate,
+                                           const uint16_t *up, int64_t per_row, int64_t ld,
+                                           uint8_t *a_mant, uint8_t *a_exp, void *stream) {
+  if (plan && plan->pairs > 0 && !up) return MXQ_ERR_NULL;
+  return quantize_experts(fmt, plan, perms, gate, up, per_row, ld, a_mant, a_exp, stream);
+}
+
+mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t N,
+                            const uint8_t *a_mant, const uint8_t *a_exp, const uint8_t *w_mant,
+                            const uint8_t *w_exp, void *y, int y_f32, int64_t ldy, void *stream) {
+  mxq::Groups x;
+  mxq_status st = mxq::check_experts(plan, &x);
+  if (st != MXQ_OK) return st;
+  mxq::GemmArgs g;
+  st = gemm_args(fmt, x.pairs, N, a_mant, a_exp, w_mant, w_exp, y, &g);
+  if (st != MXQ_OK) return st;
+  if (x.pairs == 0 || N == 0) return MXQ_OK;
+  if (ldy < N || N > INT32_MAX) return MXQ_ERR_SHAPE;
+  // (every kernel has fewer workgroups than one of 256 threads per 16 rows and 32 columns)
+  if ((x.rows / 16 + x.E) * ((N + 31) / 32) >= 1 << 23) return MXQ_ERR_SHAPE;
+  g.x = x;
+  g.w_expert = g.w_super * w_supers(N);
+  g.w_expert_sc = g.w_super_sc * w_supers(N);
+  g.y = (float *)y;
+  g.y_bf16 = !y_f32;
+  g.ldy = ldy;
+  return launched(mxq::launch_gemm_experts(g, (hipStream_t)stream));
 }
 
 mxq_status mxq_gemm_partials(const mxq_fmt *fmt, int64_t M, int64_t N,

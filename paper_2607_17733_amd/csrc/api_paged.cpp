@@ -29,6 +29,11 @@ mxq_status check_rotary(const mxq_rotary *r) {
   return MXQ_OK;
 }
 
+mxq_status check_norm(const mxq_qk_norm *n) {
+  if (!(n->eps >= 0.f) || !isfinite(n->eps)) return MXQ_ERR_SHAPE;
+  return aligned(n->q_gain, 16) && aligned(n->k_gain, 16) ? MXQ_OK : MXQ_ERR_ALIGN;
+}
+
 mxq::RopeArgs rope_args(const mxq_rotary *r) {
   mxq::RopeArgs a{};
   if (r) {
@@ -165,6 +170,56 @@ mxq_status mxq_rope(const mxq_rotary *rope, const uint16_t *x, int64_t T, int64_
   return launched(mxq::launch_rope(a, (hipStream_t)stream));
 }
 
+mxq_status mxq_rope_qk(const mxq_rotary *rope, const mxq_qk_norm *norm, const int32_t *pos,
+                       int64_t T, int64_t D, const uint16_t *q, int64_t Hq, int64_t q_ts,
+                       int64_t q_hs, uint16_t *q_out, int64_t qo_ts, int64_t qo_hs,
+                       const uint16_t *k, int64_t Hk, int64_t k_ts, int64_t k_hs, uint16_t *k_out,
+                       int64_t ko_ts, int64_t ko_hs, void *stream) {
+  mxq_status st = check_rotary(rope);
+  if (st != MXQ_OK) return st;
+  if (!norm) return MXQ_ERR_NULL;
+  if ((st = check_norm(norm)) != MXQ_OK) return st;
+  if (T < 0 || T > INT32_MAX || Hq < 0 || Hq > 65535 || Hk < 0 || Hk > 65535 || D < rope->rot ||
+      D > 4096 || D % 2)
+    return MXQ_ERR_SHAPE;
+  if (T == 0 || Hq + Hk == 0) return MXQ_OK;
+  // (a wave, or 16 lanes for every 128 values, to a head)
+  if (T * (Hq + Hk) > kMaxGrid * 256 / 64) return MXQ_ERR_SHAPE;
+  if (!pos) return MXQ_ERR_NULL;
+  auto rows = [&](const uint16_t *x, int64_t H, int64_t ts, int64_t hs, const uint16_t *y,
+                  int64_t yts, int64_t yhs, const uint16_t *gain) {
+    if (H == 0) return MXQ_OK;
+    if (!x || !y || !gain) return MXQ_ERR_NULL;
+    if (!aligned(x, 4) || !aligned(y, 4) || ts % 2 || hs % 2 || yts % 2 || yhs % 2)
+      return MXQ_ERR_ALIGN;
+    if (x == y && ((T > 1 && ts != yts) || (H > 1 && hs != yhs))) return MXQ_ERR_SHAPE;
+    return rows_apart(T, yts, H, yhs, D) ? MXQ_OK : MXQ_ERR_SHAPE;
+  };
+  if ((st = rows(q, Hq, q_ts, q_hs, q_out, qo_ts, qo_hs, norm->q_gain)) != MXQ_OK) return st;
+  if ((st = rows(k, Hk, k_ts, k_hs, k_out, ko_ts, ko_hs, norm->k_gain)) != MXQ_OK) return st;
+  mxq::RopeQkArgs a{};
+  a.rope = rope_args(rope);
+  a.norm = {norm->q_gain, norm->k_gain, norm->eps};
+  a.pos = pos;
+  a.T = T;
+  a.D = D;
+  a.q = q;
+  a.Hq = Hq;
+  a.q_ts = q_ts;
+  a.q_hs = q_hs;
+  a.q_out = q_out;
+  a.qo_ts = qo_ts;
+  a.qo_hs = qo_hs;
+  a.k = k;
+  a.Hk = Hk;
+  a.k_ts = k_ts;
+  a.k_hs = k_hs;
+  a.k_out = k_out;
+  a.ko_ts = ko_ts;
+  a.ko_hs = ko_hs;
+  return launched(mxq::launch_rope_qk(a, (hipStream_t)stream));
+}
+
 int64_t mxq_kv_page_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_tokens) {
   mxq::PageGeo g;
   const mxq_status st = check_page(fmt, Hkv, page_tokens, &g);
@@ -177,11 +232,12 @@ int64_t mxq_kv_page_exp_bytes(const mxq_fmt *fmt, int64_t Hkv, int32_t page_toke
   return st == MXQ_OK ? Hkv * page_tokens * 4 : -(int64_t)st;
 }
 
-mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const uint16_t *k,
-                         int64_t k_ts, int64_t k_hs, const uint16_t *v, int64_t v_ts, int64_t v_hs,
-                         int64_t T, const int64_t *slots, const int32_t *pos,
-                         const mxq_rotary *rope, const uint16_t *q, int64_t Hq, int64_t q_ts,
-                         int64_t q_hs, uint16_t *q_out, void *stream) {
+static mxq_status kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const mxq_qk_norm *norm,
+                            const uint16_t *k, int64_t k_ts, int64_t k_hs, const uint16_t *v,
+                            int64_t v_ts, int64_t v_hs, int64_t T, const int64_t *slots,
+                            const int32_t *pos, const mxq_rotary *rope, const uint16_t *q,
+                            int64_t Hq, int64_t q_ts, int64_t q_hs, uint16_t *q_out,
+                            void *stream) {
   mxq::KvAppendArgs a{};
   mxq_status st = check_cache(fmt, cache, &a.geo);
   if (st != MXQ_OK) return st;
@@ -190,6 +246,7 @@ mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const ui
     if (st != MXQ_OK) return st;
     if (rope->rot % 16 || rope->rot > kD) return MXQ_ERR_SHAPE;
   }
+  if (norm && (st = check_norm(norm)) != MXQ_OK) return st;
   if (T < 0 || T > INT32_MAX || Hq < 0 || Hq > 65535) return MXQ_ERR_SHAPE;
   if ((T + 15) / 16 * (2 * cache->Hkv + Hq) > kMaxGrid) return MXQ_ERR_SHAPE;
   if (T == 0) return MXQ_OK;
@@ -202,6 +259,10 @@ mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const ui
     if ((st = check_rows(q_out, 0, 0)) != MXQ_OK) return st;
     // (the stride of a single head or token is any)
     if (q == q_out && ((Hq > 1 && q_hs != kD) || (T > 1 && q_ts != Hq * kD))) return MXQ_ERR_SHAPE;
+  }
+  if (norm) {
+    if (!norm->k_gain || (q && !norm->q_gain)) return MXQ_ERR_NULL;
+    a.norm = {norm->q_gain, norm->k_gain, norm->eps};
   }
   a.rope = rope_args(rope);
   a.k = k;
@@ -226,7 +287,28 @@ mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const ui
   a.v_exp = cache->v_exp;
   a.ties_away = fmt->round == MXQ_ROUND_NEAREST_AWAY;
   a.full_clamp = fmt->clamp == MXQ_CLAMP_FULL;
-  return launched(mxq::launch_kv_append(a, (hipStream_t)stream));
+  return launched(norm ? mxq::launch_kv_append_norm(a, (hipStream_t)stream)
+                       : mxq::launch_kv_append(a, (hipStream_t)stream));
+}
+
+mxq_status mxq_kv_append(const mxq_fmt *fmt, const mxq_paged_kv *cache, const uint16_t *k,
+                         int64_t k_ts, int64_t k_hs, const uint16_t *v, int64_t v_ts, int64_t v_hs,
+                         int64_t T, const int64_t *slots, const int32_t *pos,
+                         const mxq_rotary *rope, const uint16_t *q, int64_t Hq, int64_t q_ts,
+                         int64_t q_hs, uint16_t *q_out, void *stream) {
+  return kv_append(fmt, cache, nullptr, k, k_ts, k_hs, v, v_ts, v_hs, T, slots, pos, rope, q, Hq,
+                   q_ts, q_hs, q_out, stream);
+}
+
+mxq_status mxq_kv_append_norm(const mxq_fmt *fmt, const mxq_paged_kv *cache,
+                              const mxq_qk_norm *norm, const uint16_t *k, int64_t k_ts,
+                              int64_t k_hs, const uint16_t *v, int64_t v_ts, int64_t v_hs,
+                              int64_t T, const int64_t *slots, const int32_t *pos,
+                              const mxq_rotary *rope, const uint16_t *q, int64_t Hq, int64_t q_ts,
+                              int64_t q_hs, uint16_t *q_out, void *stream) {
+  if (!norm || !rope) return MXQ_ERR_NULL;
+  return kv_append(fmt, cache, norm, k, k_ts, k_hs, v, v_ts, v_hs, T, slots, pos, rope, q, Hq, q_ts,
+                   q_hs, q_out, stream);
 }
 
 mxq_status mxq_kv_read(const mxq_fmt *fmt, const mxq_paged_kv *cache, const int64_t *slots,

@@ -128,6 +128,8 @@ __device__ inline int64_t page_run(const PageGeo &g, int64_t slot, int head) {
   return ((slot >> g.lg_page) * g.Hkv + head) << g.lg_page;
 }
 
+// NORM: queries and keys are normalised before they turn.
+template <bool NORM>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvAppendArgs a) {
   const PageGeo &g = a.geo;
   // the heads of sixteen tokens run together: K's, V's, then the queries'
@@ -141,7 +143,10 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvAppendArgs a) {
   const int pos = a.rope.table ? a.pos[t] : 0;
   if (head >= 2 * g.Hkv) {
     head -= (int)(2 * g.Hkv);
-    const rope_u4 x = load_rotated(a.rope, a.q + t * a.q_ts + head * a.q_hs, d0, pos);
+    const uint16_t *src = a.q + t * a.q_ts + head * a.q_hs;
+    const rope_u4 x = NORM ? load_normalised_rotated(a.rope, pos, src, a.norm.q_gain, a.norm.eps, kD,
+                                                     d0, kLanesPerRow, true)
+                           : load_rotated(a.rope, src, d0, pos);
     // (in place, a row's lanes have all read, their partners' values too, before one writes)
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -154,8 +159,11 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvAppendArgs a) {
   const bool keep = in && slot >= 0 && slot < g.pages << g.lg_page;
   RopeArgs none = a.rope;
   if (is_v) none.table = nullptr;
-  const rope_u4 x = load_rotated(none, is_v ? a.v + t * a.v_ts + head * a.v_hs
-                                            : a.k + t * a.k_ts + head * a.k_hs, d0, pos);
+  const uint16_t *src = is_v ? a.v + t * a.v_ts + head * a.v_hs : a.k + t * a.k_ts + head * a.k_hs;
+  const rope_u4 x = NORM && !is_v
+                        ? load_normalised_rotated(a.rope, pos, src, a.norm.k_gain, a.norm.eps, kD, d0,
+                                                  kLanesPerRow, true)
+                        : load_rotated(none, src, d0, pos);
   uint32_t top = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -216,10 +224,15 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvReadArgs a) {
 
 }  // namespace
 
-hipError_t launch_kv_append(const KvAppendArgs &a, hipStream_t s) {
+template <bool NORM>
+static hipError_t go_append(const KvAppendArgs &a, hipStream_t s) {
   const int64_t n = (a.T + kTokens - 1) / kTokens * (2 * a.geo.Hkv + a.Hq);
-  hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)n), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(kv_append_kernel<NORM>, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   return hipGetLastError();
+}
+hipError_t launch_kv_append(const KvAppendArgs &a, hipStream_t s) { return go_append<false>(a, s); }
+hipError_t launch_kv_append_norm(const KvAppendArgs &a, hipStream_t s) {
+  return go_append<true>(a, s);
 }
 
 hipError_t launch_kv_read(const KvReadArgs &a, hipStream_t s) {

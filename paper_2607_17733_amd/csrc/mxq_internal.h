@@ -9,6 +9,15 @@
 
 namespace mxq {
 
+// Rows by expert (mxq_experts): expert e's rows of an operand image are first[e]
+// .. first[e + 1] - 1, row r holding pair[r] (none: -1).
+struct Groups {
+  const int32_t *first, *pair;
+  int E;                   // 0: no groups
+  int64_t rows;            // the most rows of an image
+  int64_t pairs;
+};
+
 struct QuantArgs {
   const uint16_t *src;     // bf16 rows [src_rows][ld]
   int64_t ld;
@@ -45,6 +54,10 @@ struct QuantArgs {
   // activations: the rows are SiLU(src) * src2 (gate and up, same layout)
   int swiglu;
   const uint16_t *src2;
+  // activations: image row r is source row x.pair[r] / per_row (x.E: 0, none)
+  Groups x;
+  uint32_t per_row;
+  const int32_t *perms;    // [E][K], or nullptr: perm for all experts
 };
 
 struct GemmArgs {
@@ -60,6 +73,11 @@ struct GemmArgs {
   int64_t w_super, w_super_sc;    // weight bytes per 128-column super-slab
   int n3, n4, n6, n8;
   int full;                // full clamp: the weights' full-range encodings
+  // rows by expert: a tile's rows are an expert's, row r of the image is row
+  // x.pair[r] of y, and the experts' weights lie so many bytes apart
+  Groups x;
+  int64_t w_expert, w_expert_sc;
+  int y_bf16;              // y holds bf16
 };
 
 struct UnpackArgs {
@@ -75,6 +93,8 @@ struct UnpackArgs {
 };
 
 constexpr int64_t kMaxLds = 160 * 1024;   // LDS per workgroup on gfx950
+// of it, a workgroup of the activation quantizer whose rows a plan names
+constexpr int64_t kGroupLds = 4 * (64 + 4);
 
 hipError_t launch_quantize(const QuantArgs &args, hipStream_t s);
 hipError_t launch_quantize_act(const QuantArgs &args, hipStream_t s);
@@ -153,6 +173,57 @@ hipError_t launch_rope_table(const double *inv_freq, int rot, int64_t positions,
                              float *table, hipStream_t s);
 hipError_t launch_rope(const RopeRowsArgs &args, hipStream_t s);
 
+// Experts (experts.hip).
+constexpr int kMaxExperts = 1024;
+mxq_status check_experts(const mxq_experts *plan, Groups *g);   // (api_experts.cpp)
+struct RouteArgs {
+  const void *logits;
+  int logits_f32;
+  int64_t T, ld;
+  int E, k, score, normalise;
+  float scale;
+  const float *bias;       // or nullptr
+  int32_t *ids;
+  float *weights;
+};
+struct PlanArgs {
+  const int32_t *ids;
+  int64_t pairs, rows;
+  int E;
+  int32_t *first, *pair;
+};
+struct CombineArgs {
+  const void *y;
+  int y_f32, out_f32;
+  int64_t ldy, T, k, N, ldr, ldo;
+  int E;
+  const int32_t *ids;
+  const float *weights;
+  const uint16_t *residual;
+  void *out;
+};
+hipError_t launch_expert_plan(const PlanArgs &args, hipStream_t s);
+hipError_t launch_route(const RouteArgs &args, const PlanArgs &plan, hipStream_t s);
+hipError_t launch_combine(const CombineArgs &args, hipStream_t s);
+// The products of every expert's rows (decode.hip, gemm_prefill.hip).
+hipError_t launch_gemm_experts(const GemmArgs &args, hipStream_t s);
+
+// Norms of queries and keys with their rotation (rope.hip).
+struct NormArgs {
+  const uint16_t *q_gain, *k_gain;
+  float eps;
+};
+struct RopeQkArgs {
+  RopeArgs rope;
+  NormArgs norm;
+  const int32_t *pos;
+  int64_t T, D, Hq, Hk;
+  const uint16_t *q, *k;
+  uint16_t *q_out, *k_out;
+  int64_t q_ts, q_hs, qo_ts, qo_hs, k_ts, k_hs, ko_ts, ko_hs;
+};
+hipError_t launch_rope_qk(const RopeQkArgs &args, hipStream_t s);
+
 // The paged KV cache (kv_paged.hip): head dimension 128, four blocks a row.
 struct PageGeo {
   int m[4];                // widths
@@ -172,6 +243,7 @@ struct KvAppendArgs {
   const int32_t *pos;
   uint8_t *k_mant, *k_exp, *v_mant, *v_exp;
   int ties_away, full_clamp;
+  NormArgs norm;           // of launch_kv_append_norm
 };
 struct KvReadArgs {
   PageGeo geo;
@@ -181,6 +253,7 @@ struct KvReadArgs {
   uint16_t *k, *v;         // either null
 };
 hipError_t launch_kv_append(const KvAppendArgs &args, hipStream_t s);
+hipError_t launch_kv_append_norm(const KvAppendArgs &args, hipStream_t s);
 hipError_t launch_kv_read(const KvReadArgs &args, hipStream_t s);
 
 // Attention over the paged cache (attn_paged.hip).

@@ -440,13 +440,15 @@ __device__ inline void quantize_item(const QuantArgs &q, const LGeo &lg, const I
   }
 }
 
-// Item `i` of segment SEG: block i >> lg_rows of row i mod 2^lg_rows.
+// Item `i` of segment SEG: block i >> lg_rows of row i mod 2^lg_rows.  from: the
+// source rows of a group by experts (none: -1), or null.
 template <bool RNA, int MODE, int SEG>
 __device__ inline void quantize_chunk(const QuantArgs &q, const LGeo &lg, int i, int64_t r0,
-                                      const uint8_t *rows, int rowB) {
+                                      const uint8_t *rows, int rowB, const int *from) {
   const int rem = i >> q.lg_rows, lr = i & ((1 << q.lg_rows) - 1);
   const int64_t row = r0 + lr;
   if (rem >= lg.S[SEG] * (SEG < 2 ? 4 : 2) || row >= q.out_rows) return;
+  if (from && from[lr] < 0) return;
   quantize_item<RNA, MODE, SEG>(q, lg, item_geo_seg<SEG>(lg, rem), row, rows + lr * rowB);
 }
 
@@ -635,7 +637,8 @@ __device__ inline u4 swiglu8_table(const uint16_t *tab, u4 g, u4 u) {
   return o;
 }
 
-template <bool RNA, int MODE, int PROD>
+// BY: the rows of a plan (QuantArgs::x); image rows that hold no pair are left.
+template <bool RNA, int MODE, int PROD, bool BY>
 __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   const int t = threadIdx.x;
@@ -661,6 +664,9 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
     }
     __syncthreads();
   }
+  // (the source rows and the expert, after all else)
+  int *const from = !BY ? nullptr
+                        : (int *)(smem + ((R * rowB + rms + 15) & ~15) + (silu ? 2 * kSiluN : 0));
   for (int lr = t; lr < R; lr += nthr) *(u4 *)(smem + lr * rowB + 2 * K) = u4{0u, 0u, 0u, 0u};
 
   // With SiLU * up a workgroup takes every nwg-th row group, so that its table
@@ -671,6 +677,25 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
   const int64_t groups = PROD == kProdSwiglu ? (q.out_rows + R - 1) >> lgR : w0 + 1;
   for (int64_t grp = w0; grp < groups; grp += nwg) {
     const int64_t r0 = grp << lgR;
+    if (BY) {
+      // rows behind the last expert's are nobody's
+      if (r0 >= q.x.first[q.x.E]) break;
+      for (int lr = t; lr < R; lr += nthr) {
+        const int p = r0 + lr < q.out_rows ? q.x.pair[r0 + lr] : -1;
+        from[lr] = p < 0 || p >= q.x.pairs ? -1 : (int)((uint32_t)p / q.per_row);
+      }
+      // (a group's rows are one expert's: at most 16, and its first row a multiple of them)
+      if (q.perms)
+        for (int e = t; e < q.x.E; e += nthr)
+          if (q.x.first[e] <= r0 && r0 < q.x.first[e + 1]) from[R] = e;
+      __syncthreads();
+      if (q.perms) {
+        const int e = (int)min((unsigned)__builtin_amdgcn_readfirstlane(from[R]), (unsigned)q.x.E - 1);
+        q.perm = q.perms + (int64_t)e * K;
+      }
+    }
+    auto source = [&](int lr) { return BY ? (int64_t)from[lr] : r0 + lr; };
+    auto live = [&](int lr) { return BY ? from[lr] >= 0 : r0 + lr < q.src_rows; };
     // the geometry is formed per group (an opaque zero): held over the loop
     // its scalars would spill
     int z = 0;
@@ -681,14 +706,33 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
     // any of them, so the batch costs one memory latency instead of one per
     // load.
     constexpr int kBatch = 8;
-    if (PROD != kProdSwiglu && q.vec16 && K % 512 == 0 && R * q.ld * 2 <= 0x7fffffff) {
+    if (BY && PROD != kProdSwiglu && q.vec16 && K % 512 == 0) {
+      // (as below, a buffer per row: none where no pair is)
+      const int per_row = K / 512;
+      int lr = wave / per_row, j = wave - lr * per_row;
+      const int dl = nwaves / per_row, dj = nwaves - dl * per_row;
+      while (lr < R) {
+        const int row = __builtin_amdgcn_readfirstlane(from[lr]);
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+            (void *)(q.src + (row < 0 ? 0 : row) * q.ld), 0, row < 0 ? 0 : 2 * K, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)(smem + lr * rowB + j * 1024),
+                                                 16, lane * 16, j * 1024, 0, 0);
+        lr += dl;
+        j += dj;
+        if (j >= per_row) {
+          j -= per_row;
+          ++lr;
+        }
+      }
+    } else if (!BY && PROD != kProdSwiglu && q.vec16 && K % 512 == 0 &&
+               R * q.ld * 2 <= 0x7fffffff) {
       // Rows of whole 1 KB pieces go straight into LDS (direct-to-LDS loads,
       // one piece per wave instruction), all in flight until the wait before the
       // barrier below.  Rows past the source's end read zeros: the buffer
       // resource ends at its last row.
-      const int64_t live = q.src_rows > r0 ? q.src_rows - r0 : 0;
+      const int64_t rows = q.src_rows > r0 ? q.src_rows - r0 : 0;
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-          (void *)(q.src + r0 * q.ld), 0, (int)min(live * q.ld * 2, (int64_t)0x7fffffff),
+          (void *)(q.src + r0 * q.ld), 0, (int)min(rows * q.ld * 2, (int64_t)0x7fffffff),
           0x00020000);
       const int per_row = K / 512;
       int lr = wave / per_row, j = wave - lr * per_row;
@@ -717,8 +761,8 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
         for (int k = 0; k < kPairs; ++k) {
           off[k] = lr * rowB + 16 * c;
           g[k] = u[k] = u4{0u, 0u, 0u, 0u};
-          if (v0 + k * nthr < nv && r0 + lr < q.src_rows) {
-            const int64_t src = (r0 + lr) * q.ld + 8 * c;
+          if (v0 + k * nthr < nv && live(lr)) {
+            const int64_t src = source(lr) * q.ld + 8 * c;
             g[k] = *(const u4 *)(q.src + src);
             u[k] = *(const u4 *)(q.src2 + src);
           }
@@ -748,8 +792,8 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
           lrk[k] = lr;
           ck[k] = c;
           if (v0 + k * nthr < nv) {
-            if (r0 + lr < q.src_rows)
-              d[k] = *(const u4 *)(q.src + (r0 + lr) * q.ld + 8 * c);
+            if (live(lr))
+              d[k] = *(const u4 *)(q.src + source(lr) * q.ld + 8 * c);
             else
               d[k] = u4{0u, 0u, 0u, 0u};
           }
@@ -768,11 +812,11 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
       }
     } else {
       for (int lr = 0; lr < R; ++lr) {
-        const bool live = r0 + lr < q.src_rows;
-        const uint16_t *src = q.src + (r0 + lr) * q.ld;
+        const bool in = live(lr);
+        const int64_t src = source(lr) * q.ld;
         for (int c = t; c < K; c += nthr) {
-          uint32_t v = live ? src[c] : 0u;
-          if (PROD == kProdSwiglu && live) v = swiglu1(v, q.src2[(r0 + lr) * q.ld + c]);
+          uint32_t v = in ? q.src[src + c] : 0u;
+          if (PROD == kProdSwiglu && in) v = swiglu1(v, q.src2[src + c]);
           *(uint16_t *)(smem + lr * rowB + 2 * c) = (uint16_t)v;
         }
       }
@@ -786,13 +830,13 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
     for (int wc = wave; wc < ch.total; wc += nwaves) {
       int x = wc;
       if (x < ch.W[3])
-        quantize_chunk<RNA, MODE, 3>(q, lg, 64 * x + lane, r0, smem, rowB);
+        quantize_chunk<RNA, MODE, 3>(q, lg, 64 * x + lane, r0, smem, rowB, from);
       else if ((x -= ch.W[3]) < ch.W[2])
-        quantize_chunk<RNA, MODE, 2>(q, lg, 64 * x + lane, r0, smem, rowB);
+        quantize_chunk<RNA, MODE, 2>(q, lg, 64 * x + lane, r0, smem, rowB, from);
       else if ((x -= ch.W[2]) < ch.W[1])
-        quantize_chunk<RNA, MODE, 1>(q, lg, 64 * x + lane, r0, smem, rowB);
+        quantize_chunk<RNA, MODE, 1>(q, lg, 64 * x + lane, r0, smem, rowB, from);
       else
-        quantize_chunk<RNA, MODE, 0>(q, lg, 64 * (x - ch.W[1]) + lane, r0, smem, rowB);
+        quantize_chunk<RNA, MODE, 0>(q, lg, 64 * (x - ch.W[1]) + lane, r0, smem, rowB, from);
     }
     // zero the padding of the packed and exponent rows
     if (MODE == kModeRows)
@@ -860,8 +904,10 @@ struct RowGroups {
   int lg, threads, per_cu;
 };
 static RowGroups row_groups(const QuantArgs &a, int cus) {
-  const int64_t row = row_lds(a.K, a.rmsnorm != 0), extra = a.swiglu ? 2 * kSiluN : 0;
+  const int64_t row = row_lds(a.K, a.rmsnorm != 0);
+  const int64_t extra = (a.swiglu ? 2 * kSiluN : 0) + (a.x.E ? kGroupLds : 0);
   auto fits = [&](int lg, int n) { return n * ((row << lg) + 16 + extra) <= kMaxLds; };
+  const int most = a.perms ? 4 : 6;                        // (16 rows are one expert's)
   const LGeo g(a.n3, a.n4, a.n6, a.n8);
   auto waves = [&](int lg) {
     int w = 0;
@@ -870,10 +916,10 @@ static RowGroups row_groups(const QuantArgs &a, int cus) {
   };
   constexpr int kMaxWaves = kMaxThreads / 64;
   auto one = [&](int lg) { return RowGroups{lg, 64 * std::min(waves(lg), kMaxWaves), 1}; };
-  for (int lg = 0; lg <= 6 && fits(lg, 1) && waves(lg) <= 2 * kMaxWaves; ++lg)
+  for (int lg = 0; lg <= most && fits(lg, 1) && waves(lg) <= 2 * kMaxWaves; ++lg)
     if (((a.out_rows - 1) >> lg) + 1 <= cus) return one(lg);
   int lg = 0;
-  while (lg < 6 && fits(lg + 1, 2) && waves(lg + 1) <= kMaxWaves + 2) ++lg;
+  while (lg < most && fits(lg + 1, 2) && waves(lg + 1) <= kMaxWaves + 2) ++lg;
   if (!fits(lg, 2)) return one(0);
   // SiLU * up of long rows: its tables and arithmetic outweigh the overlap
   // (K = 14336, M = 4096: 4 rows and 1024 threads, one per CU, 82 us, 2 rows
@@ -890,11 +936,11 @@ static RowGroups row_groups(const QuantArgs &a, int cus) {
   return RowGroups{lg, 64 * std::min(waves(lg), kMaxWaves / 2), 2};
 }
 
-template <int MODE, int PROD>
+template <int MODE, int PROD, bool BY = false>
 static hipError_t go_quantize(const QuantArgs &a, int64_t grid, int threads, int64_t lds,
                               hipStream_t stream) {
-  const auto fn = a.ties_away ? quantize_act_kernel<true, MODE, PROD>
-                              : quantize_act_kernel<false, MODE, PROD>;
+  const auto fn = a.ties_away ? quantize_act_kernel<true, MODE, PROD, BY>
+                              : quantize_act_kernel<false, MODE, PROD, BY>;
   // the LDS limit, once per kernel and device
   static std::atomic<uint64_t> raised[2] = {};
   int dev = 0;
@@ -928,9 +974,13 @@ hipError_t launch_quantize_act(const QuantArgs &args, hipStream_t stream) {
   const int64_t grid = a.swiglu ? std::min<int64_t>(groups, (int64_t)rg.per_cu * cus) : groups;
   int64_t lds = ((row_lds(a.K, a.rmsnorm != 0) << rg.lg) + 15) & ~15;
   a.silu_table = a.swiglu && a.vec16 && ((groups / grid * a.K) << rg.lg) >= 6 * kSiluN &&
-                 lds + 2 * kSiluN <= kMaxLds;
+                 lds + 2 * kSiluN + (a.x.E ? kGroupLds : 0) <= kMaxLds;
   if (a.silu_table) lds += 2 * kSiluN;
+  if (a.x.E) lds += kGroupLds;
   if (lds > kMaxLds) return hipErrorInvalidValue;
+  if (a.x.E)
+    return a.swiglu ? go_quantize<kModeImage, kProdSwiglu, true>(a, grid, rg.threads, lds, stream)
+                    : go_quantize<kModeImage, kProdNone, true>(a, grid, rg.threads, lds, stream);
   if (a.weights) return go_quantize<kModeWeights, kProdNone>(a, grid, rg.threads, lds, stream);
   if (a.write_rows) return go_quantize<kModeRows, kProdNone>(a, grid, rg.threads, lds, stream);
   if (a.rmsnorm) return go_quantize<kModeImage, kProdRms>(a, grid, rg.threads, lds, stream);

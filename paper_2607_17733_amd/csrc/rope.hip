@@ -96,6 +96,68 @@ __global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeRowsArgs a, int6
   y[j] = (uint16_t)f32_to_bf16(rotated(v, u, row[0], row[1], true));
 }
 
+// Queries and keys normalised per head and rotated: L lanes of eight values hold a
+// head (a power of two, so that their sum is an exchange within the wave), the
+// queries' heads before the keys'.  The values stay in registers between the two;
+// those of the partners of a rotation in halves are read again, from the cache.
+__global__ __launch_bounds__(kThreads) void rope_qk_kernel(RopeQkArgs a, int lg_lanes,
+                                                           int64_t total) {
+  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int d0 = 8 * (int)(id & ((1 << lg_lanes) - 1));
+  const int64_t head = id >> lg_lanes;
+  const bool in = head < total && d0 < a.D;                // (every lane takes part in the sum)
+  const uint32_t heads = (uint32_t)(a.Hq + a.Hk);
+  const int64_t t = (in ? head : 0) / heads;
+  const int h = (int)((in ? head : 0) - t * heads);
+  const bool is_k = h >= a.Hq;
+  const uint16_t *x = is_k ? a.k + t * a.k_ts + (h - a.Hq) * a.k_hs : a.q + t * a.q_ts + h * a.q_hs;
+  uint16_t *y = is_k ? a.k_out + t * a.ko_ts + (h - a.Hq) * a.ko_hs
+                     : a.q_out + t * a.qo_ts + h * a.qo_hs;
+  const rope_u4 v = load_normalised_rotated(a.rope, a.pos[t], x, is_k ? a.norm.k_gain : a.norm.q_gain,
+                                            a.norm.eps, (int)a.D, d0, 1 << lg_lanes, in);
+  // (in place, a head's lanes have all read, their partners' values too, before one writes)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (in) *(rope_u4 *)(y + d0) = v;
+}
+
+// Heads whose sizes or strides rule the 16-byte accesses out: a wave per head, the
+// squares added in the same order.
+__global__ __launch_bounds__(kThreads) void rope_qk_any_kernel(RopeQkArgs a, int64_t total) {
+  const int lane = threadIdx.x & 63;
+  const int64_t head = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (head >= total) return;
+  const int64_t heads = a.Hq + a.Hk, t = head / heads;
+  const int h = (int)(head - t * heads);
+  const bool is_k = h >= a.Hq;
+  const uint16_t *x = is_k ? a.k + t * a.k_ts + (h - a.Hq) * a.k_hs : a.q + t * a.q_ts + h * a.q_hs;
+  uint16_t *y = is_k ? a.k_out + t * a.ko_ts + (h - a.Hq) * a.ko_hs
+                     : a.q_out + t * a.qo_ts + h * a.qo_hs;
+  const uint16_t *gain = is_k ? a.norm.k_gain : a.norm.q_gain;
+  const int D = (int)a.D, rot = a.rope.rot, half = rot / 2;
+  double s = 0.0;
+  for (int c = 8 * lane; c < D; c += 512)
+    for (int d = c; d < min(c + 8, D); ++d) {
+      const double v = (double)bf16_to_f32(x[d]);
+      s = fma(v, v, s);
+    }
+  const double r = norm_factor(sum_lanes(s, 64), (double)D, a.norm.eps);
+  const int p = a.pos[t];
+  const bool out = p < 0 || p >= a.rope.positions;
+  const float *row = a.rope.table + (int64_t)(out ? 0 : p) * rot;
+  for (int e = lane; e < half + (D - rot); e += 64) {
+    if (e >= half) {
+      const int d = rot + e - half;
+      y[d] = (uint16_t)f32_to_bf16(normalised1(x[d], r, gain[d]));
+      continue;
+    }
+    const int i = a.rope.pairs ? 2 * e : e, j = a.rope.pairs ? 2 * e + 1 : e + half;
+    const float u = normalised1(x[i], r, gain[i]), v = normalised1(x[j], r, gain[j]);
+    y[i] = out ? 0xFFFF : (uint16_t)f32_to_bf16(rotated(u, v, row[2 * e], row[2 * e + 1], false));
+    y[j] = out ? 0xFFFF : (uint16_t)f32_to_bf16(rotated(v, u, row[2 * e], row[2 * e + 1], true));
+  }
+}
+
 }  // namespace
 
 hipError_t launch_rope_table(const double *inv_freq, int rot, int64_t positions, double mscale,
@@ -124,6 +186,27 @@ hipError_t launch_rope(const RopeRowsArgs &a, hipStream_t s) {
   } else {
     const int64_t n = a.T * a.H * (a.D / 2);
     hipLaunchKernelGGL(rope_any_kernel, grid(n), dim3(kThreads), 0, s, a, n);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_qk(const RopeQkArgs &a, hipStream_t s) {
+  const int rot = a.rope.rot;
+  const int64_t total = a.T * (a.Hq + a.Hk);
+  const int64_t strides = (a.Hq ? a.q_ts | a.q_hs | a.qo_ts | a.qo_hs : 0) |
+                          (a.Hk ? a.k_ts | a.k_hs | a.ko_ts | a.ko_hs : 0);
+  const uintptr_t at = (a.Hq ? (uintptr_t)a.q | (uintptr_t)a.q_out : 0) |
+                       (a.Hk ? (uintptr_t)a.k | (uintptr_t)a.k_out : 0);
+  if (a.D % 8 == 0 && a.D <= 512 && rot % (a.rope.pairs ? 8 : 16) == 0 && strides % 8 == 0 &&
+      (at & 15) == 0) {
+    int lg = 0;
+    while (8 << lg < a.D) ++lg;
+    hipLaunchKernelGGL(rope_qk_kernel, dim3((unsigned)(((total << lg) + kThreads - 1) / kThreads)),
+                       dim3(kThreads), 0, s, a, lg, total);
+  } else {
+    constexpr int per = kThreads / 64;
+    hipLaunchKernelGGL(rope_qk_any_kernel, dim3((unsigned)((total + per - 1) / per)), dim3(kThreads),
+                       0, s, a, total);
   }
   return hipGetLastError();
 }

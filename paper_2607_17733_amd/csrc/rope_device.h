@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mxq_internal.h"
+
 namespace mxq {
 
 typedef unsigned rope_u4 __attribute__((ext_vector_type(4)));
@@ -48,6 +50,109 @@ __device__ inline rope_u4 rotate_pairs8(rope_u4 x, const rope_f4 (&cs)[4]) {
     y[i] = f32_to_bf16(rotated(a, b, c, s, false)) | f32_to_bf16(rotated(b, a, c, s, true)) << 16;
   }
   return y;
+}
+
+// Eight values of a head, normalised: float32(float32(x r) gain), r in float64.
+struct rope_f8 {
+  float v[8];
+};
+__device__ inline rope_f8 normalised8(rope_u4 x, double r, rope_u4 gain) {
+#pragma clang fp contract(off)
+  rope_f8 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y.v[2 * i] = (float)((double)bf16_to_f32(x[i]) * r) * bf16_to_f32(gain[i]);
+    y.v[2 * i + 1] = (float)((double)__uint_as_float(x[i] & 0xFFFF0000u) * r) *
+                     __uint_as_float(gain[i] & 0xFFFF0000u);
+  }
+  return y;
+}
+__device__ inline rope_u4 to_bf16x8(const rope_f8 &x) {
+  rope_u4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = f32_to_bf16(x.v[2 * i]) | f32_to_bf16(x.v[2 * i + 1]) << 16;
+  return y;
+}
+__device__ inline rope_f8 rotate_half8(const rope_f8 &x, const rope_f8 &p, const rope_f4 (&cs)[4],
+                                       bool plus) {
+  rope_f8 y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    y.v[i] = rotated(x.v[i], p.v[i], cs[i >> 1][2 * (i & 1)], cs[i >> 1][2 * (i & 1) + 1], plus);
+  return y;
+}
+__device__ inline rope_f8 rotate_pairs8(const rope_f8 &x, const rope_f4 (&cs)[4]) {
+  rope_f8 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = x.v[2 * i], b = x.v[2 * i + 1];
+    const float c = cs[i >> 1][2 * (i & 1)], s = cs[i >> 1][2 * (i & 1) + 1];
+    y.v[2 * i] = rotated(a, b, c, s, false);
+    y.v[2 * i + 1] = rotated(b, a, c, s, true);
+  }
+  return y;
+}
+// The sum of eight squares in float64, and 1 / sqrt(sum / D + eps); a head of zeros
+// has no direction, and stays zero.
+__device__ inline double squares8(rope_u4 x) {
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double a = (double)bf16_to_f32(x[i]), b = (double)__uint_as_float(x[i] & 0xFFFF0000u);
+    s = fma(a, a, s);
+    s = fma(b, b, s);
+  }
+  return s;
+}
+__device__ inline double norm_factor(double squares, double D, float eps) {
+  const double m = squares / D + (double)eps;
+  return m == 0.0 ? 0.0 : 1.0 / sqrt(m);
+}
+// Over the n lanes of a head (a power of two), the same in each.
+__device__ inline double sum_lanes(double v, int n) {
+  for (int i = 1; i < n; i *= 2) v += __shfl_xor(v, i);
+  return v;
+}
+
+__device__ inline float normalised1(uint32_t x, double r, uint32_t gain) {
+  return (float)((double)bf16_to_f32(x) * r) * bf16_to_f32(gain);
+}
+
+// Values d0 .. d0 + 7 of a head of D values at x, normalised and rotated, in one of the
+// n lanes (a power of two) that hold it; all n call, `in` those with values.
+__device__ inline rope_u4 load_normalised_rotated(const RopeArgs &rope, int p, const uint16_t *x,
+                                                  const uint16_t *gain, float eps, int D, int d0,
+                                                  int n, bool in) {
+  rope_u4 u = {0u, 0u, 0u, 0u}, g = u;
+  if (in) {
+    u = *(const rope_u4 *)(x + d0);
+    g = *(const rope_u4 *)(gain + d0);
+  }
+  const int rot = rope.rot, half = rot / 2;
+  const bool turns = in && d0 < rot, out = p < 0 || p >= rope.positions;
+  const bool second = d0 >= half;
+  const int i0 = second ? d0 - half : d0;                  // (of a rotation in halves)
+  rope_f4 cs[4] = {};
+  rope_u4 pu = u, pg = g;
+  if (turns) {
+    const float *row = rope.table + (int64_t)(out ? 0 : p) * rot;
+    if (rope.pairs) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) cs[i] = *(const rope_f4 *)(row + d0 + 4 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cs[i] = *(const rope_f4 *)(row + 2 * i0 + 4 * i);
+      const int partner = second ? i0 : d0 + half;
+      pu = *(const rope_u4 *)(x + partner);
+      pg = *(const rope_u4 *)(gain + partner);
+    }
+  }
+  const double r = norm_factor(sum_lanes(squares8(u), n), (double)D, eps);
+  const rope_f8 v = normalised8(u, r, g);
+  if (!turns) return to_bf16x8(v);
+  if (out) return rope_u4{~0u, ~0u, ~0u, ~0u};
+  if (rope.pairs) return to_bf16x8(rotate_pairs8(v, cs));
+  return to_bf16x8(rotate_half8(v, normalised8(pu, r, pg), cs, second));
 }
 
 }  // namespace mxq

@@ -54,6 +54,23 @@ class _AttnOpts(ctypes.Structure):
                 ("slopes", ctypes.c_void_p)]
 
 
+class _Experts(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int64), ("experts", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("first", ctypes.c_void_p),
+                ("pair", ctypes.c_void_p)]
+
+
+class _RouteOpts(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int32), ("score", ctypes.c_int32), ("normalise", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("bias", ctypes.c_void_p)]
+
+
+class _QkNorm(ctypes.Structure):
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
 _lib = None
 
 # name -> (restype, argtypes)
@@ -103,6 +120,20 @@ _SIGS = {
     "mxq_attn_paged_work_bytes": (_I64, [_P, _P, _I64, _I64, _I64, _I64, _I64]),
     "mxq_attn_paged": (ctypes.c_int, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _P, ctypes.c_int,
                                       _P, _I64, _P]),
+    "mxq_expert_rows": (_I64, [_I64, ctypes.c_int32]),
+    "mxq_route": (ctypes.c_int, [_P, _P, ctypes.c_int, _I64, _I64, _P, _P, _P, _P]),
+    "mxq_expert_plan": (ctypes.c_int, [_P, _P, _P]),
+    "mxq_quantize_act_experts": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _P, _P, _P]),
+    "mxq_quantize_act_swiglu_experts": (ctypes.c_int, [_P, _P, _P, _P, _P, _I64, _I64, _P, _P,
+                                                       _P]),
+    "mxq_gemm_experts": (ctypes.c_int, [_P, _P, _I64, _P, _P, _P, _P, _P, ctypes.c_int, _I64, _P]),
+    "mxq_combine_experts": (ctypes.c_int, [_P, ctypes.c_int, _I64, _P, _P, _I64, _I64,
+                                           ctypes.c_int32, _I64, _P, _I64, _P, ctypes.c_int, _I64,
+                                           _P]),
+    "mxq_rope_qk": (ctypes.c_int, [_P, _P, _P, _I64, _I64] + [_P, _I64, _I64, _I64, _P, _I64,
+                                                              _I64] * 2 + [_P]),
+    "mxq_kv_append_norm": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _P, _I64, _I64, _I64, _P, _P,
+                                          _P, _P, _I64, _I64, _I64, _P, _P]),
 }
 
 
@@ -764,6 +795,51 @@ def rope(x, pos, table, interleaved: bool = False, out=None):
     return out
 
 
+def _gain(t, D: int, what: str, dev):
+    """A contiguous bf16 device tensor of D elements: its address."""
+    return _index(t, D, torch.bfloat16, what, dev)
+
+
+def rope_qk(q, k, pos, table, q_gain, k_gain, eps: float, interleaved: bool = False, q_out=None,
+            k_out=None):
+    """Queries q [T, Hq, D] and keys k [T, Hk, D] (bf16, strided; either may be None)
+    normalised per head (x / sqrt(mean x^2 + eps) times its gain, bf16 [D]) and
+    rotated as rope does, rounded once: (q_out, k_out).  Each may be its source (in
+    place), else a tensor that overlaps none."""
+    first = q if q is not None else k
+    if first is None:
+        raise MxqError("rope_qk needs q or k")
+    T, _, D = _heads(first, "q or k")
+    dev = first.device
+    stream = _current(dev, "q or k")
+    sides, outs, gains = [], [], []
+    for x, gain, out, what in ((q, q_gain, q_out, "q"), (k, k_gain, k_out, "k")):
+        if x is None:
+            if out is not None:
+                raise MxqError("%s_out needs %s" % (what, what))
+            sides += [None, 0, 0, 0, None, 0, 0]
+            outs.append(None)
+            gains.append(None)
+            continue
+        Tx, H, _ = _heads(x, what, dev, None, D)
+        if Tx != T:
+            raise MxqError("q and k have %d and %d tokens" % (T, Tx))
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        elif out is not x and _heads(out, what + "_out", dev, H, D)[0] != T:
+            raise MxqError("%s_out is %s, not %s" % (what, tuple(out.shape), tuple(x.shape)))
+        sx, so = x.stride(), out.stride()
+        sides += [x.data_ptr(), H, sx[0], sx[1], out.data_ptr(), so[0], so[1]]
+        outs.append(out)
+        gains.append(_gain(gain, D, what + "_gain", dev))
+    status = lib().mxq_rope_qk(_rotary(table, dev, interleaved),
+                               ctypes.byref(_QkNorm(gains[0], gains[1], eps)),
+                               _index(pos, T, torch.int32, "pos", dev), T, D, *sides, stream)
+    if status:
+        _check(status, "mxq_rope_qk")
+    return tuple(outs)
+
+
 class PagedCache:
     """A paged MXINT KV cache of one layer (include/mxq.h mxq_paged_kv): `pages`
     pages of `page_tokens` tokens (a power of two, 16 to 1024) of Hkv heads of
@@ -808,13 +884,14 @@ class PagedCache:
 
 
 def kv_append(cache: PagedCache, k, v, slots, pos=None, rope=None, interleaved: bool = False,
-              q=None, q_out=None):
+              q=None, q_out=None, q_gain=None, k_gain=None, eps: float = 0.0):
     """New tokens into the cache: keys k (rotated at positions pos int32 [T] with
     the table `rope`, where it is given) and values v, bf16 [T, Hkv, 128]
     (strided), quantized into slots (int64 [T], distinct; one outside the cache
     is padding).  With q (bf16 [T, Hq, 128], strided) the queries are rotated by
     the same launch, and returned (contiguous; q_out may be q if that is
-    contiguous)."""
+    contiguous).  With k_gain (bf16 [128]; q_gain for the queries, and a `rope`) both
+    are normalised per head before they turn, as rope_qk does."""
     dev = cache.device
     stream = _current(dev, "the cache")
     T = _heads(k, "k", dev, cache.Hkv, 128)[0]
@@ -837,10 +914,18 @@ def kv_append(cache: PagedCache, k, v, slots, pos=None, rope=None, interleaved: 
     elif q_out is not None:
         raise MxqError("q_out needs q")
     ks, vs = k.stride(), v.stride()
-    status = lib().mxq_kv_append(cache.fmt._ref, cache._ref, k.data_ptr(), ks[0], ks[1],
-                                 v.data_ptr(), vs[0], vs[1], T,
-                                 _index(slots, T, torch.int64, "slots", dev), at, r, qp, Hq, qs[0],
-                                 qs[1], op, stream)
+    args = (k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], T,
+            _index(slots, T, torch.int64, "slots", dev), at, r, qp, Hq, qs[0], qs[1], op, stream)
+    if k_gain is None:
+        if q_gain is not None:
+            raise MxqError("q_gain needs k_gain")
+        status = lib().mxq_kv_append(cache.fmt._ref, cache._ref, *args)
+    else:
+        if r is None or (q is None) != (q_gain is None):
+            raise MxqError("gains need rope, and q_gain goes with q")
+        norm = _QkNorm(None if q is None else _gain(q_gain, 128, "q_gain", dev),
+                       _gain(k_gain, 128, "k_gain", dev), eps)
+        status = lib().mxq_kv_append_norm(cache.fmt._ref, cache._ref, ctypes.byref(norm), *args)
     if status:
         _check(status, "mxq_kv_append")
     return q_out
@@ -925,4 +1010,240 @@ def attn_paged(q, cache: PagedCache, cu_q, kv_len, table, max_q: int, max_kv: in
                                   work.data_ptr(), work.numel(), stream)
     if status:
         _check(status, "mxq_attn_paged")
+    return out
+
+
+# --------------------------------------------------------------------------
+# Layers with experts
+
+def _bf16_or_f32(t, what: str, dim: int = 2):
+    """A `dim`-D bf16 or float32 device tensor with unit column stride: whether float32."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == dim
+            and t.dtype in (torch.bfloat16, torch.float32)
+            and (t.stride(-1) == 1 or t.shape[-1] <= 1)):
+        raise MxqError("%s must be a %d-D bf16 or float32 device tensor with unit column stride"
+                       % (what, dim))
+    return t.dtype is torch.float32
+
+
+def _choices(t, dtype, what: str, dev, shape=None):
+    """A contiguous 2-D device tensor [tokens, k]: its shape."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 2
+            and t.is_contiguous()):
+        raise MxqError("%s must be a contiguous 2-D %s device tensor" % (what, dtype))
+    if t.device != dev:
+        raise MxqError("%s is on %s, not %s" % (what, t.device, dev))
+    if shape is not None and t.shape != shape:
+        raise MxqError("%s is %s, not %s" % (what, tuple(t.shape), tuple(shape)))
+    return t.shape
+
+
+class ExpertPlan:
+    """Where the chosen token-expert pairs of a batch lie (include/mxq.h mxq_experts):
+    `rows` rows of an operand image, expert e's from first[e] (int32 [experts + 1])
+    on, row r holding pair[r] (int32 [rows], -1: none).  The buffers are the
+    caller's, or new ones, which route or expert_plan fills; the sizes go by pairs
+    and experts alone, so a plan serves every batch of as many tokens."""
+
+    def __init__(self, pairs: int, experts: int, device="cuda", first=None, pair=None):
+        self.pairs, self.experts = int(pairs), int(experts)
+        self.rows = _size(lib().mxq_expert_rows(self.pairs, self.experts), "mxq_expert_rows")
+        if first is None and pair is None:
+            # (one allocation; both 16-byte aligned)
+            at = self.experts + 4 & ~3
+            both = torch.empty(at + self.rows, dtype=torch.int32, device=device)
+            first, pair = both[:self.experts + 1], both[at:]
+        elif first is None or pair is None:
+            raise MxqError("a plan takes first and pair, or neither")
+        self.device = first.device if isinstance(first, torch.Tensor) else None
+        f = _index(first, self.experts + 1, torch.int32, "first", self.device)
+        p = _index(pair, self.rows, torch.int32, "pair", self.device)
+        self.first, self.pair = first, pair
+        self._c = _Experts(self.pairs, self.experts, 0, f, p)
+        self._ref = ctypes.byref(self._c)
+
+
+def route(logits, k: int, score: str = "softmax", normalise: bool = True, scale: float = 1.0,
+          bias=None, out=None):
+    """The k best of E experts for every token, from its scores logits (bf16 or
+    float32 [T, E]), and their plan: (ids int32 [T, k], weights float32 [T, k],
+    ExpertPlan).  score: "softmax" over all experts, or "sigmoid"; normalise:
+    a token's weights are divided by their sum; bias (float32 [E]) is added to the
+    score for the choice only; equal ones go to the lowest index.  out: such a
+    triple, written."""
+    f32 = _bf16_or_f32(logits, "logits")
+    dev = logits.device
+    stream = _current(dev, "logits")
+    T, E = logits.shape
+    if out is None:
+        ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+        plan = ExpertPlan(T * k, E, device=dev)
+    else:
+        ids, weights, plan = out
+        _choices(ids, torch.int32, "ids", dev, (T, k))
+        _choices(weights, torch.float32, "weights", dev, (T, k))
+        if plan.pairs != T * k or plan.experts != E or plan.device != dev:
+            raise MxqError("the plan is of %d pairs and %d experts on %s, not %d and %d on %s"
+                           % (plan.pairs, plan.experts, plan.device, T * k, E, dev))
+    if bias is not None:
+        bias = _index(bias, E, torch.float32, "bias", dev)
+    if score not in _SCORES:
+        raise MxqError("score must be 'softmax' or 'sigmoid'")
+    opts = _RouteOpts(k, _SCORES[score], 1 if normalise else 0, scale, bias)
+    status = lib().mxq_route(ctypes.byref(opts), logits.data_ptr(), 1 if f32 else 0, T,
+                             logits.stride(0), ids.data_ptr(), weights.data_ptr(), plan._ref,
+                             stream)
+    if status:
+        _check(status, "mxq_route")
+    return ids, weights, plan
+
+
+def expert_plan(ids, experts: int, out=None):
+    """The plan of chosen experts ids (int32 [T, k], contiguous); ids outside [0,
+    experts) are no choice.  out: an ExpertPlan, written."""
+    T, k = _choices(ids, torch.int32, "ids", ids.device if isinstance(ids, torch.Tensor) else None)
+    stream = _current(ids.device, "ids")
+    if out is None:
+        out = ExpertPlan(T * k, experts, device=ids.device)
+    elif out.pairs != T * k or out.experts != experts or out.device != ids.device:
+        raise MxqError("the plan is of %d pairs and %d experts on %s, not %d and %d on %s"
+                       % (out.pairs, out.experts, out.device, T * k, experts, ids.device))
+    _check(lib().mxq_expert_plan(ids.data_ptr(), out._ref, stream), "mxq_expert_plan")
+    return out
+
+
+def _perms(perms, fmt: Format, experts: int, dev):
+    if perms is None:
+        return None
+    if not (isinstance(perms, torch.Tensor) and perms.is_cuda and perms.dtype is torch.int32
+            and perms.is_contiguous() and perms.shape == (experts, fmt.K)):
+        raise MxqError("perms must be a contiguous int32 device tensor [%d, %d]" % (experts, fmt.K))
+    if perms.device != dev:
+        raise MxqError("perms is on %s, not %s" % (perms.device, dev))
+    return perms.data_ptr()
+
+
+def _per_row(rows: int, plan: ExpertPlan, what: str, dev) -> int:
+    """Pairs per source row: as many as a token has, or one."""
+    if plan.device != dev:
+        raise MxqError("the plan is on %s, not %s" % (plan.device, dev))
+    if rows == plan.pairs:
+        return 1
+    if rows == 0 or plan.pairs % rows:
+        raise MxqError("%s has %d rows: a row per token or per pair (%d) is needed"
+                       % (what, rows, plan.pairs))
+    return plan.pairs // rows
+
+
+def quantize_act_experts(x, fmt: Format, plan: ExpertPlan, perms=None, out=None):
+    """quantize_act of bf16 rows x (a row per token, or per pair) by a plan: the
+    operand image of its rows, for gemm_experts.  perms (int32 [experts, K]): a
+    permutation for each expert in place of fmt's."""
+    _bf16_2d(x, fmt.K, "activations")
+    per = _per_row(x.shape[0], plan, "activations", x.device)
+    stream = _current(x.device, "activations")
+    mant, exp = _act_out(out, fmt, plan.rows, x.device)
+    _check(lib().mxq_quantize_act_experts(fmt.ref, plan._ref,
+                                          _perms(perms, fmt, plan.experts, x.device), _ptr(x), per,
+                                          x.stride(0), _ptr(mant), _ptr(exp), stream),
+           "mxq_quantize_act_experts")
+    return mant, exp
+
+
+def quantize_act_swiglu_experts(gate, up, fmt: Format, plan: ExpertPlan, perms=None, out=None):
+    """quantize_act_swiglu of gate and up (a row per pair, as gemm_experts gives
+    them, or per token) by a plan."""
+    _bf16_2d(gate, fmt.K, "gate")
+    _bf16_2d(up, fmt.K, "up")
+    if up.shape != gate.shape or up.stride() != gate.stride():
+        raise MxqError("gate and up must have the same shape and strides")
+    if up.device != gate.device:
+        raise MxqError("gate and up must be on one device")
+    per = _per_row(gate.shape[0], plan, "gate", gate.device)
+    stream = _current(gate.device, "gate")
+    mant, exp = _act_out(out, fmt, plan.rows, gate.device)
+    _check(lib().mxq_quantize_act_swiglu_experts(
+        fmt.ref, plan._ref, _perms(perms, fmt, plan.experts, gate.device), _ptr(gate), _ptr(up), per,
+        gate.stride(0), _ptr(mant), _ptr(exp), stream), "mxq_quantize_act_swiglu_experts")
+    return mant, exp
+
+
+def pack_experts(w, fmt: Format, perms=None):
+    """pack_weights of every expert's weights w (bf16 [experts, N, >= K]), one after
+    the other: (mant uint8 [experts, weight_bytes(N)], exp uint8 [experts,
+    weight_exp_bytes(N)])."""
+    if not (isinstance(w, torch.Tensor) and w.is_cuda and w.dim() == 3):
+        raise MxqError("weights must be a 3-D bf16 device tensor [experts, N, K]")
+    E, N, _ = w.shape
+    stream = _current(w.device, "weights")
+    _perms(perms, fmt, E, w.device)
+    mant = torch.empty((E, fmt.weight_bytes(N)), dtype=torch.uint8, device=w.device)
+    exp = torch.empty((E, fmt.weight_exp_bytes(N)), dtype=torch.uint8, device=w.device)
+    for e in range(E):
+        f = fmt if perms is None else Format(fmt.K, fmt.widths, perms[e], ("rne", "rna")[fmt.round],
+                                             ("sym", "full")[fmt.clamp])
+        _check(lib().mxq_pack_weights(f.ref, _ptr(_bf16_2d(w[e], fmt.K, "weights")), N, w.stride(1),
+                                      _ptr(mant[e]), _ptr(exp[e]), stream), "mxq_pack_weights")
+    return mant, exp
+
+
+def gemm_experts(a_mant, a_exp, w_mant, w_exp, fmt: Format, plan: ExpertPlan, N: int, out=None,
+                 dtype=torch.bfloat16):
+    """Every pair's row times its expert's weights (pack_experts): [pairs, N], bf16
+    or float32 (`dtype`); rows of pairs that chose no expert stay as `out` holds
+    them."""
+    dev = plan.device
+    stream = _current(dev, "the plan")
+    if N < 0:
+        raise MxqError("N must be non-negative")
+    _dev_bytes(a_mant, fmt.act_bytes(plan.rows), "a_mant", dev)
+    _dev_bytes(a_exp, fmt.act_exp_bytes(plan.rows), "a_exp", dev)
+    _dev_bytes(w_mant, plan.experts * fmt.weight_bytes(N), "w_mant", dev)
+    _dev_bytes(w_exp, plan.experts * fmt.weight_exp_bytes(N), "w_exp", dev)
+    if out is None:
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise MxqError("dtype must be torch.bfloat16 or torch.float32")
+        out = torch.empty((plan.pairs, N), dtype=dtype, device=dev)
+    f32 = _bf16_or_f32(out, "out")
+    if out.device != dev or out.shape[0] < plan.pairs or out.shape[1] < N:
+        raise MxqError("out is %s on %s, smaller than [%d, %d] or not on %s"
+                       % (tuple(out.shape), out.device, plan.pairs, N, dev))
+    _check(lib().mxq_gemm_experts(fmt.ref, plan._ref, N, _ptr(a_mant), _ptr(a_exp), _ptr(w_mant),
+                                  _ptr(w_exp), _ptr(out), 1 if f32 else 0, out.stride(0), stream),
+           "mxq_gemm_experts")
+    return out
+
+
+def combine_experts(y, ids, weights, plan: ExpertPlan, residual=None, out=None,
+                    dtype=torch.bfloat16):
+    """A token's weighted sum over its experts' rows of y (bf16 or float32 [T * k,
+    N]), on top of residual (bf16 [T, N]) where it is given: bf16 or float32
+    (`dtype`) [T, N].  out may be residual."""
+    f32 = _bf16_or_f32(y, "y")
+    dev = y.device
+    stream = _current(dev, "y")
+    T, k = _choices(ids, torch.int32, "ids", dev)
+    _choices(weights, torch.float32, "weights", dev, (T, k))
+    if T * k != plan.pairs or y.shape[0] < T * k:
+        raise MxqError("y has %d rows and ids %d pairs, the plan %d" % (y.shape[0], T * k, plan.pairs))
+    N = y.shape[1]
+    if residual is not None:
+        if _bf16_or_f32(residual, "residual") or residual.device != dev:
+            raise MxqError("residual must be bf16, on %s" % dev)
+        if residual.shape != (T, N):
+            raise MxqError("residual is %s, not [%d, %d]" % (tuple(residual.shape), T, N))
+    if out is None:
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
+            raise MxqError("dtype must be torch.bfloat16 or torch.float32")
+        out = torch.empty((T, N), dtype=dtype, device=dev)
+    of32 = _bf16_or_f32(out, "out")
+    if out.device != dev or out.shape != (T, N):
+        raise MxqError("out is %s on %s, not [%d, %d] on %s" % (tuple(out.shape), out.device, T, N, dev))
+    status = lib().mxq_combine_experts(
+        y.data_ptr(), 1 if f32 else 0, y.stride(0), ids.data_ptr(), weights.data_ptr(), T, k,
+        plan.experts, N, _ptr(residual), 0 if residual is None else residual.stride(0),
+        out.data_ptr(), 1 if of32 else 0, out.stride(0), stream)
+    if status:
+        _check(status, "mxq_combine_experts")
     return out

@@ -1,0 +1,464 @@
+"""Routing, plans, the quantizers by a plan, the grouped products and their weighted
+sum against the oracle, and a layer's step of them together.
+
+Bounds.  Choices and plans are whole numbers and have to be equal.  A weight's
+relative error is documented as below 1e-6.  A product sums K exact digit products
+in float32: each of at most K / 64 + 16 additions (64 at least to an instruction;
+the waves' sums) rounds by 2^-24 of what the terms add up to, and an instruction
+aligns its terms to the largest, 2^-24 of it each: (K / 64 + 16) 2^-23 of the terms'
+absolute sum.  bf16 results are off by half a step, 2^-8, more.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import experts as oe
+from oracle.paged import to_bf16, to_f32
+from paper_2607_17733_amd import mxq
+from parity_util import say, to_dev_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def bits_of(t):
+    return t.cpu().contiguous().view(torch.int16).numpy().view(np.uint16)
+
+
+def _randn(shape, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+def _widths(nb, mix):
+    """About a tenth of the blocks each of the wider widths of the mix."""
+    n = max(1, nb // 10)
+    rest = [m for m in mix[1:]]
+    rest = rest[-max(0, nb - 1) // n:] if nb > 1 else []
+    w = [m for m in rest for _ in range(n)][-(nb - 1):] if nb > 1 else []
+    return [mix[0]] * (nb - len(w)) + w
+
+
+# --------------------------------------------------------------------------
+# routing and plans
+
+def _check_route(x, k, **kw):
+    ids, w, plan = mxq.route(x.cuda(), k, **{n: v.cuda() if isinstance(v, torch.Tensor) else v
+                                            for n, v in kw.items()})
+    torch.cuda.synchronize()
+    ref = {n: v.numpy() if isinstance(v, torch.Tensor) else v for n, v in kw.items()}
+    want, ww = oe.route(x.float().numpy(), k, **ref)
+    assert np.array_equal(ids.cpu().numpy(), want)
+    got = w.cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(got - ww) <= 1e-6 * np.abs(ww) + 1e-37)
+    first, pair = oe.plan(want, x.shape[1])
+    assert np.array_equal(plan.first.cpu().numpy(), first)
+    assert np.array_equal(plan.pair.cpu().numpy(), pair)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 64, 6), (3, 3, 3), (17, 65, 7), (33, 8, 2), (130, 200, 8),
+                                   (257, 256, 8), (64, 128, 8), (9, 512, 32), (5, 1000, 10), (4, 1024, 32)])
+def test_route(T, E, k, score, bias):
+    say("route", T, E, k, score, bias)
+    x = 2 * _randn((T, E), T + E)
+    b = 0.3 * _randn((E,), E) if bias else None
+    _check_route(x, k, score=score, bias=b, normalise=T % 2 == 0, scale=2.5)
+    _check_route(x.to(torch.bfloat16), k, score=score, bias=b, normalise=T % 2 == 1)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_route_ties_masks_and_infinities(score, bias):
+    inf, nan = float("inf"), float("nan")
+    rows = [[0.0] * 70, [-inf] * 70, [nan] * 70, [-inf] * 69 + [1.0], [nan] * 30 + [2.0, 2.0] + [-inf] * 38,
+            [inf] * 3 + [0.0] * 67, [3e38] * 2 + [inf] + [-3e38] * 67, [-200.0] * 70, [200.0] * 70,
+            [-0.0, 0.0] * 35, [1e-45, -1e-45] * 35, [-3e38] * 70]
+    x = torch.tensor(rows)
+    b = torch.zeros(70) if bias else None
+    for k in (1, 4, 32):
+        for normalise in (False, True):
+            _check_route(x, k, score=score, bias=b, normalise=normalise)
+
+
+def test_route_bias_that_rules_experts_out():
+    inf, nan = float("inf"), float("nan")
+    x = _randn((20, 40), 1)
+    b = 0.1 * _randn((40,), 2)
+    b[3], b[7], b[11], b[12], b[39] = -inf, nan, inf, inf, 1e30
+    for score in ("softmax", "sigmoid"):
+        _check_route(x, 6, score=score, bias=b)
+    b[:] = -inf
+    b[5] = 0.0
+    _check_route(x, 3, score="sigmoid", bias=b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_route_strided_and_odd_rows(dtype):
+    full = _randn((37, 101), 5).to(dtype).cuda()
+    x = full[:, 3:96]
+    ids, w, plan = mxq.route(x, 5)
+    want, ww = oe.route(x.float().cpu().numpy(), 5)
+    assert np.array_equal(ids.cpu().numpy(), want)
+    assert np.all(np.abs(w.cpu().numpy() - ww) <= 1e-6 * ww)
+
+
+@pytest.mark.parametrize("T,E,k,how", [(0, 5, 2, "any"), (1, 1, 1, "any"), (1, 1024, 4, "any"), (5, 4, 3, "one"),
+                                       (100, 7, 3, "any"), (333, 128, 8, "any"), (4096, 8, 2, "any"),
+                                       (4099, 300, 8, "any"), (700, 16, 4, "none"), (700, 16, 4, "one"),
+                                       (70000, 64, 1, "any"), (16, 1024, 32, "any")])
+def test_expert_plan(T, E, k, how):
+    say("plan", T, E, k, how)
+    g = torch.Generator().manual_seed(T + E)
+    ids = torch.randint(-2, E + 3, (T, k), generator=g).int()
+    if how == "one":
+        ids[:] = E - 1
+    if how == "none":
+        ids[:] = -1
+        ids[::2] = 2 ** 31 - 1
+    plan = mxq.expert_plan(ids.cuda(), E)
+    first, pair = oe.plan(ids.numpy(), E)
+    assert np.array_equal(plan.first.cpu().numpy(), first)
+    assert np.array_equal(plan.pair.cpu().numpy(), pair)
+
+
+def test_plan_is_written_again():
+    g = torch.Generator().manual_seed(3)
+    plan = None
+    for i in range(4):
+        ids = torch.randint(-1, 9, (50, 3), generator=g).int()
+        plan = mxq.expert_plan(ids.cuda(), 9, out=plan)
+        first, pair = oe.plan(ids.numpy(), 9)
+        assert np.array_equal(plan.first.cpu().numpy(), first) and np.array_equal(plan.pair.cpu().numpy(), pair)
+
+
+# --------------------------------------------------------------------------
+# the quantizers by a plan
+
+def _byte_rows(widths, rows):
+    """The image row that each byte of the mantissas and of the scales belongs to."""
+    n = [sum(1 for w in widths if w == m) for m in (3, 4, 6, 8)]
+    S = [-(-n[0] // 4), -(-n[1] // 4), -(-n[2] // 2), -(-n[3] // 2)]
+    lane = np.arange(64) % 16
+    tile = np.concatenate([np.tile(lane.repeat(24), S[0] + S[1] + S[2]), np.tile(lane.repeat(32), S[3])])
+    scale = np.tile(lane.repeat(4), sum(-(-s // 4) for s in S))
+    at = np.arange(rows // 16)[:, None] * 16
+    return (at + tile).reshape(-1), (at + scale).reshape(-1)
+
+
+def _image_case(T, E, k, K, mix, perms, swiglu=False, per_pair=False, seed=0, clamp="sym", round_="rne", ld=0,
+                skip=0.1):
+    g = torch.Generator().manual_seed(seed + T + E + K)
+    widths = _widths(K // 32, mix)
+    ids = torch.randint(0, E, (T, k), generator=g).int()
+    ids[torch.rand((T, k), generator=g) < skip] = -1
+    plan = mxq.expert_plan(ids.cuda(), E)
+    order = torch.stack([torch.randperm(K, generator=g) for _ in range(E)]).int().cuda()
+    fmt = mxq.Format(K, widths, order[0].clone() if perms == "shared" else None, round=round_, clamp=clamp)
+    n = T * k if per_pair or swiglu else T
+    x = (torch.randn((n, K + ld), generator=g) * 3).to(torch.bfloat16).cuda()[:, :K]
+    u = torch.randn((n, K + ld), generator=g).to(torch.bfloat16).cuda()[:, :K]
+    return ids, plan, fmt, order if perms == "each" else None, x, u
+
+
+@pytest.mark.parametrize("perms", ["none", "shared", "each"])
+@pytest.mark.parametrize("T,E,k,K,mix", [(1, 4, 1, 32, (4,)), (1, 64, 6, 512, (4, 6, 8)),
+                                         (7, 3, 2, 96, (3, 6, 8)), (40, 16, 4, 1408, (4, 6, 8)),
+                                         (300, 8, 2, 1024, (4, 8)), (64, 128, 8, 640, (3, 8)),
+                                         (2000, 5, 3, 160, (6,)), (129, 2, 2, 4096, (4, 6, 8)),
+                                         (3, 2, 2, 20480, (4, 6, 8))])
+@pytest.mark.parametrize("kind", ["tokens", "pairs", "swiglu"])
+def test_images_are_those_of_the_plain_quantizers(T, E, k, K, mix, perms, kind):
+    say("image", T, E, k, K, mix, perms, kind)
+    ids, plan, fmt, each, x, u = _image_case(T, E, k, K, mix, perms, kind == "swiglu", kind == "pairs",
+                                             ld=8 if T % 2 else 3)
+    pair = plan.pair.cpu().numpy()
+    first = plan.first.cpu().numpy()
+    live = pair >= 0
+    noise = [torch.randint(0, 256, (n,), dtype=torch.uint8).cuda()
+             for n in (fmt.act_bytes(plan.rows), fmt.act_exp_bytes(plan.rows))]
+    out = tuple(t.clone() for t in noise)
+    if kind == "swiglu":
+        got = mxq.quantize_act_swiglu_experts(x, u, fmt, plan, perms=each, out=out)
+    else:
+        got = mxq.quantize_act_experts(x, fmt, plan, perms=each, out=out)
+    # the same rows, gathered by hand, through the plain quantizers (one expert's at a time)
+    src = torch.from_numpy(np.where(live, pair, 0) // (1 if x.shape[0] == ids.numel() else k)).cuda()
+    rows = x[src].contiguous()
+    ups = u[src].contiguous()
+    want = tuple(t.clone() for t in noise)
+    tb, sb = fmt.act_bytes(16), fmt.act_exp_bytes(16)
+    for e in range(E):
+        a, b = int(first[e]), int(first[e + 1])
+        if a == b:
+            continue
+        f = fmt if each is None else mxq.Format(K, fmt.widths, each[e])
+        part = (want[0][a // 16 * tb:b // 16 * tb], want[1][a // 16 * sb:b // 16 * sb])
+        if kind == "swiglu":
+            mxq.quantize_act_swiglu(rows[a:b], ups[a:b], f, out=part)
+        else:
+            mxq.quantize_act(rows[a:b], f, out=part)
+    torch.cuda.synchronize()
+    for g, w, z, at in zip(got, want, noise, _byte_rows(list(fmt.widths), plan.rows)):
+        g, w, z = g.cpu().numpy(), w.cpu().numpy(), z.cpu().numpy()
+        assert np.array_equal(g[live[at]], w[live[at]])
+        assert np.array_equal(g[~live[at]], z[~live[at]])
+
+
+# --------------------------------------------------------------------------
+# the grouped products
+
+def _product_case(T, E, k, K, N, mix=(4, 6, 8), perms="none", out=torch.float32, clamp="sym", round_="rne",
+                  how="any", ldy=0, seed=0, skip=0.1, sample=None):
+    say("product", T, E, k, K, N, mix, perms, out, clamp, how)
+    g = torch.Generator().manual_seed(seed + T + E + K + N)
+    widths = _widths(K // 32, mix)
+    ids = torch.randint(0, E, (T, k), generator=g).int()
+    if how == "one":
+        ids[:] = E - 1
+    elif how == "skewed":
+        ids = (ids.float() ** 2 / max(1, E - 1)).int()
+    if skip:
+        ids[torch.rand((T, k), generator=g) < skip] = -1
+    x = torch.randn((T, K), generator=g)
+    x[:, 5] *= 20
+    x = x.to(torch.bfloat16)
+    w = (0.02 * torch.randn((E, N, K), generator=g)).to(torch.bfloat16)
+    order = torch.stack([torch.randperm(K, generator=g) for _ in range(E)]).int()
+    shared = order[0].clone().cuda() if perms == "shared" else None
+    fmt = mxq.Format(K, widths, shared, round=round_, clamp=clamp)
+    each = order.cuda() if perms == "each" else None
+    plan = mxq.expert_plan(ids.cuda(), E)
+    wm, we = mxq.pack_experts(w.cuda(), fmt, perms=each)
+    am, ae = mxq.quantize_act_experts(x.cuda(), fmt, plan, perms=each)
+    y = torch.full((T * k, N + ldy), 7.0, dtype=out, device="cuda")
+    got = mxq.gemm_experts(am, ae, wm, we, fmt, plan, N, out=y)
+    torch.cuda.synchronize()
+    p = None if perms == "none" else order[0].numpy() if perms == "shared" else order.numpy()
+    f = ids.reshape(-1).numpy().copy()
+    if sample is not None:                               # the oracle of some of the pairs
+        keep = np.zeros(f.size, bool)
+        keep[np.random.RandomState(seed).permutation(f.size)[:sample]] = True
+        chosen = f >= 0
+        f[~keep] = -1
+    want, big = oe.product(bits_of(x).repeat(k, axis=0), bits_of(w), f, p, widths,
+                           1 if round_ == "rna" else 0, 1 if clamp == "full" else 0)
+    y = got.float().cpu().numpy().astype(np.float64)
+    here = f >= 0
+    tol = (K / 64 + 16) * 2.0 ** -23 * big[here]
+    if out is torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (np.abs(want[here]) + tol)
+    d = np.abs(y[here][:, :N] - want[here])
+    assert np.all(d <= tol), (float(d.max()), float(tol.min()), np.unravel_index(np.argmax(d - tol), d.shape))
+    gone = f < 0 if sample is None else ~chosen
+    assert np.all(y[gone] == 7.0) and np.all(y[:, N:] == 7.0)
+    return got
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k,K,N", [(1, 1, 1, 32, 1), (1, 64, 6, 512, 130), (2, 3, 2, 96, 16), (5, 4, 4, 128, 40),
+                                       (16, 8, 2, 1408, 100), (64, 128, 8, 256, 96), (33, 5, 1, 160, 257),
+                                       (100, 7, 3, 640, 200), (300, 4, 2, 512, 384), (512, 2, 1, 256, 1000),
+                                       (1500, 8, 2, 128, 300), (2100, 3, 2, 384, 520), (40, 1024, 32, 64, 33)])
+def test_product(T, E, k, K, N, out):
+    _product_case(T, E, k, K, N, out=out, perms=("none", "shared", "each")[T % 3])
+
+
+@pytest.mark.parametrize("mix", [(3,), (4,), (6,), (8,), (3, 6, 8), (4, 6), (3, 8), (3, 4, 6, 8)])
+@pytest.mark.parametrize("clamp", ["sym", "full"])
+@pytest.mark.parametrize("T", [3, 70, 700])
+def test_product_of_width_mixes(T, mix, clamp):
+    _product_case(T, 3, 2, 32 * 23, 150, mix=mix, clamp=clamp, round_="rna" if T == 70 else "rne", perms="each")
+
+
+@pytest.mark.parametrize("how", ["one", "skewed"])
+@pytest.mark.parametrize("T,E,k", [(20, 6, 2), (70, 40, 3), (900, 6, 2), (1300, 70, 2)])
+def test_product_of_uneven_groups(T, E, k, how):
+    _product_case(T, E, k, 256, 200, how=how, out=torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,E,k,K,N", [(9, 6, 2, 256, 100), (90, 6, 2, 256, 129), (1000, 3, 2, 256, 260)])
+@pytest.mark.parametrize("ldy", [1, 4, 8, 100])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_product_into_strided_rows(T, E, k, K, N, ldy, out):
+    _product_case(T, E, k, K, N, ldy=ldy, out=out)
+
+
+@pytest.mark.parametrize("T,E,k,K,N", [(64, 16, 4, 2048, 2816), (4096, 8, 2, 1024, 2048), (777, 32, 4, 4096, 1000),
+                                       (16, 8, 2, 4096, 28672)])
+def test_product_at_size(T, E, k, K, N):
+    _product_case(T, E, k, K, N, sample=150, perms="shared", skip=0.0)
+
+
+def test_products_repeat_bit_for_bit_and_do_not_depend_on_other_rows():
+    a = _product_case(50, 4, 2, 512, 200, skip=0.0)
+    b = _product_case(50, 4, 2, 512, 200, skip=0.0)
+    assert torch.equal(a, b)
+
+
+def test_product_without_rows():
+    fmt = mxq.Format(64, [4, 4])
+    w = torch.zeros((3, 20, 64), dtype=torch.bfloat16, device="cuda")
+    wm, we = mxq.pack_experts(w, fmt)
+    for ids in (torch.empty((0, 2), dtype=torch.int32), torch.full((5, 2), -1, dtype=torch.int32)):
+        plan = mxq.expert_plan(ids.cuda(), 3)
+        x = torch.ones((max(1, ids.shape[0]), 64), dtype=torch.bfloat16, device="cuda")[:ids.shape[0]]
+        am, ae = mxq.quantize_act_experts(x, fmt, plan)
+        y = torch.full((ids.numel(), 20), 3.0, device="cuda")
+        mxq.gemm_experts(am, ae, wm, we, fmt, plan, 20, out=y)
+        assert bool((y == 3.0).all())
+        o = mxq.combine_experts(y, ids.cuda(), torch.ones(ids.shape, device="cuda"), plan)
+        assert o.shape == (ids.shape[0], 20) and bool((o == 0).all())
+
+
+def test_nan_and_infinite_rows_stay_their_own():
+    fmt = mxq.Format(128, [4, 4, 6, 8])
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn((40, 128), generator=g).to(torch.bfloat16)
+    w = torch.randn((2, 50, 128), generator=g).to(torch.bfloat16).cuda()
+    ids = torch.randint(0, 2, (40, 1), generator=g).int().cuda()
+    plan = mxq.expert_plan(ids, 2)
+    wm, we = mxq.pack_experts(w, fmt)
+    y = mxq.gemm_experts(*mxq.quantize_act_experts(x.cuda(), fmt, plan), wm, we, fmt, plan, 50,
+                         dtype=torch.float32)
+    z = x.clone()
+    z[3, 7], z[17, 100] = float("nan"), float("inf")
+    yz = mxq.gemm_experts(*mxq.quantize_act_experts(z.cuda(), fmt, plan), wm, we, fmt, plan, 50,
+                          dtype=torch.float32)
+    rest = torch.ones(40, dtype=torch.bool, device="cuda")
+    rest[[3, 17]] = False
+    assert torch.equal(y[rest], yz[rest]) and bool(yz[~rest].isnan().all())
+
+
+# --------------------------------------------------------------------------
+# the weighted sum
+
+@pytest.mark.parametrize("T,k,N", [(1, 1, 1), (1, 6, 2048), (7, 2, 33), (64, 8, 256), (301, 3, 1000), (3, 32, 8)])
+@pytest.mark.parametrize("y32,o32,residual,pad", [(False, False, "own", 0), (True, True, None, 0),
+                                                  (False, True, "own", 8), (True, False, "in place", 3),
+                                                  (False, False, None, 1), (False, False, "in place", 16)])
+def test_combine(T, k, N, y32, o32, residual, pad):
+    say("combine", T, k, N, y32, o32, residual, pad)
+    g = torch.Generator().manual_seed(T + k + N)
+    E = 5
+    ids = torch.randint(-1, E + 1, (T, k), generator=g).int()
+    w = torch.randn((T, k), generator=g)
+    y = torch.randn((T * k, N + pad), generator=g)
+    y = y if y32 else y.to(torch.bfloat16)
+    out = (ids.reshape(-1) < 0) | (ids.reshape(-1) >= E)
+    y[out] = float("nan")                                # nobody's rows
+    w[(ids < 0) | (ids >= E)] = float("nan")
+    res = None if residual is None else torch.randn((T, N + pad), generator=g).to(torch.bfloat16)
+    plan = mxq.ExpertPlan(T * k, E)
+    r = None if res is None else res.cuda()[:, :N]
+    got = mxq.combine_experts(y.cuda()[:, :N], ids.cuda(), w.cuda(), plan, residual=r,
+                              out=r if residual == "in place" else None,
+                              dtype=torch.float32 if o32 else torch.bfloat16)
+    want, big = oe.combine(y[:, :N].double().numpy(), ids.numpy(), w.numpy(), E,
+                           None if res is None else res[:, :N].float().numpy())
+    d = np.abs(got.double().cpu().numpy() - want)
+    f32 = got.dtype is torch.float32
+    assert (got.dtype is torch.float32) == (o32 and residual != "in place")
+    # a rounding to float32 per term, then the result's
+    tol = k * 2.0 ** -24 * big
+    assert np.all(d <= (tol if f32 else tol + 2.0 ** -8 * (np.abs(want) + tol)))
+
+
+# --------------------------------------------------------------------------
+# a layer's step
+
+class Layer:
+    """Router, gate and up, SiLU * up, down, weighted sum, as a serving program runs them."""
+
+    def __init__(self, T, E, k, K, F, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.E, self.k, self.K, self.F = T, E, k, K, F
+        self.fmt1 = mxq.Format(K, _widths(K // 32, (4, 6, 8)), torch.randperm(K, generator=g).int().cuda())
+        self.fmt2 = mxq.Format(F, _widths(F // 32, (4, 6, 8)))
+        self.perms2 = torch.stack([torch.randperm(F, generator=g) for _ in range(E)]).int().cuda()
+        self.w1 = (0.05 * torch.randn((E, 2 * F, K), generator=g)).to(torch.bfloat16)
+        self.w2 = (0.05 * torch.randn((E, K, F), generator=g)).to(torch.bfloat16)
+        self.p1 = mxq.pack_experts(self.w1.cuda(), self.fmt1)
+        self.p2 = mxq.pack_experts(self.w2.cuda(), self.fmt2, perms=self.perms2)
+        self.inputs(seed)
+
+    def inputs(self, seed):
+        g = torch.Generator().manual_seed(1000 + seed)
+        x = torch.randn((self.T, self.K), generator=g).to(torch.bfloat16)
+        logits = torch.randn((self.T, self.E), generator=g)
+        if hasattr(self, "x"):
+            self.x.copy_(x)
+            self.logits.copy_(logits)
+        else:
+            self.x, self.logits = x.cuda(), logits.cuda()
+        return self
+
+    def run(self):
+        F = self.F
+        ids, w, plan = mxq.route(self.logits, self.k)
+        h = mxq.gemm_experts(*mxq.quantize_act_experts(self.x, self.fmt1, plan), *self.p1, self.fmt1, plan, 2 * F)
+        a2 = mxq.quantize_act_swiglu_experts(h[:, :F], h[:, F:], self.fmt2, plan, perms=self.perms2)
+        y = mxq.gemm_experts(*a2, *self.p2, self.fmt2, plan, self.K, dtype=torch.float32)
+        return ids, w, h, y, mxq.combine_experts(y, ids, w, plan, residual=self.x)
+
+    def check(self):
+        from oracle import fused
+        ids, w, h, y, o = (t.cpu() for t in self.run())
+        want, _ = oe.route(self.logits.cpu().numpy(), self.k)
+        assert np.array_equal(ids.numpy(), want)
+        K, F, k = self.K, self.F, self.k
+        xb = bits_of(self.x).repeat(k, axis=0)
+        hr, big = oe.product(xb, bits_of(self.w1), want, self.fmt1.perm.cpu().numpy(), list(self.fmt1.widths))
+        tol = (K / 64 + 16) * 2.0 ** -23 * big
+        assert np.all(np.abs(h.double().numpy() - hr) <= tol + 2.0 ** -8 * (np.abs(hr) + tol))
+        # from the framework's own rows on, so that a rounding does not count twice
+        hb = bits_of(h)
+        act = fused.swiglu_bf16(hb[:, :F], hb[:, F:])
+        yr, big = oe.product(act, bits_of(self.w2), want, self.perms2.cpu().numpy(), list(self.fmt2.widths))
+        assert np.all(np.abs(y.double().numpy() - yr) <= (F / 64 + 16) * 2.0 ** -23 * big)
+        orf, big = oe.combine(y.double().numpy(), want, w.numpy(), self.E, self.x.float().cpu().numpy())
+        tol = k * 2.0 ** -24 * big
+        assert np.all(np.abs(o.double().numpy() - orf) <= tol + 2.0 ** -8 * (np.abs(orf) + tol))
+        return o
+
+
+@pytest.mark.parametrize("T,E,k,K,F", [(1, 8, 2, 256, 96), (5, 16, 4, 512, 160), (64, 8, 2, 256, 256),
+                                       (700, 4, 2, 256, 128)])
+def test_layer(T, E, k, K, F):
+    Layer(T, E, k, K, F).check()
+
+
+def test_layer_captured_and_replayed():
+    """One capture serves other inputs (and so other groups); eager work in between."""
+    a, eager = Layer(40, 8, 2, 256, 128), Layer(33, 8, 2, 256, 128, seed=1)
+    a.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = a.run()
+    for seed in range(4):
+        a.inputs(seed)
+        graph.replay()
+        other = eager.run()
+        got = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        for g, w in zip(got, a.run()):
+            assert torch.equal(g, w)
+        for g, w in zip(other, eager.run()):
+            assert torch.equal(g, w)
+
+
+def test_layers_on_two_streams():
+    a, b = Layer(30, 8, 2, 256, 128), Layer(300, 4, 2, 256, 96, seed=2)
+    want = a.run(), b.run()
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(s):
+            x = a.run()
+        with torch.cuda.stream(t):
+            y = b.run()
+        torch.cuda.synchronize()
+        for got, ref in zip((x, y), want):
+            for g, w in zip(got, ref):
+                assert torch.equal(g, w)

@@ -58,6 +58,9 @@ mxq_status check_fmt(const mxq_fmt *f, Segs *s) {
 namespace {
 
 using mxq::check_fmt;
+using mxq::kImage;
+using mxq::kRows;
+using mxq::kWeights;
 using mxq::Segs;
 
 int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
@@ -87,13 +90,14 @@ int64_t w_exp_bytes(const Segs &s, int64_t N) {
 
 mxq_status launched(hipError_t e) { return e == hipSuccess ? MXQ_OK : MXQ_ERR_DEVICE; }
 
-enum QuantKind { kWeights, kImage, kRows };
+}  // namespace
+
+namespace mxq {
 
 mxq_status quantize_common(const mxq_fmt *fmt, const uint16_t *src, int64_t rows,
                            int64_t ld, uint8_t *mant, uint8_t *exp, void *stream,
-                           QuantKind kind, const uint16_t *gain = nullptr, float eps = 0.f,
-                           const uint16_t *src2 = nullptr, const mxq::Groups *by = nullptr,
-                           int64_t per_row = 1, const int32_t *perms = nullptr) {
+                           QuantKind kind, const uint16_t *gain, float eps, const uint16_t *src2,
+                           const Groups *by, int64_t per_row, const int32_t *perms) {
   Segs s;
   mxq_status st = check_fmt(fmt, &s);
   if (st != MXQ_OK) return st;
@@ -203,7 +207,7 @@ mxq_status gemm_args(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_
   return MXQ_OK;
 }
 
-}  // namespace
+}  // namespace mxq
 
 static mxq_status attn_common(const mxq_fmt *fmt, const uint16_t *q, int64_t B, int64_t Hq,
                               int64_t Hkv, int64_t T, float scale, const uint8_t *k_mant,
@@ -278,12 +282,12 @@ int64_t mxq_weight_exp_bytes(const mxq_fmt *fmt, int64_t N) {
 mxq_status mxq_quantize_act(const mxq_fmt *fmt, const uint16_t *a, int64_t M,
                             int64_t lda, uint8_t *a_mant, uint8_t *a_exp,
                             void *stream) {
-  return quantize_common(fmt, a, M, lda, a_mant, a_exp, stream, kImage);
+  return mxq::quantize_common(fmt, a, M, lda, a_mant, a_exp, stream, kImage);
 }
 
 mxq_status mxq_quantize_rows(const mxq_fmt *fmt, const uint16_t *a, int64_t M, int64_t lda,
                              uint8_t *rows, uint8_t *exps, void *stream) {
-  return quantize_common(fmt, a, M, lda, rows, exps, stream, kRows);
+  return mxq::quantize_common(fmt, a, M, lda, rows, exps, stream, kRows);
 }
 
 mxq_status mxq_quantize_act_rmsnorm(const mxq_fmt *fmt, const uint16_t *x, int64_t M,
@@ -291,27 +295,27 @@ mxq_status mxq_quantize_act_rmsnorm(const mxq_fmt *fmt, const uint16_t *x, int64
                                     uint8_t *a_mant, uint8_t *a_exp, void *stream) {
   if (M > 0 && !gain) return MXQ_ERR_NULL;
   if (!(eps >= 0.f)) return MXQ_ERR_SHAPE;
-  return quantize_common(fmt, x, M, ldx, a_mant, a_exp, stream, kImage, gain, eps);
+  return mxq::quantize_common(fmt, x, M, ldx, a_mant, a_exp, stream, kImage, gain, eps);
 }
 
 mxq_status mxq_quantize_act_swiglu(const mxq_fmt *fmt, const uint16_t *gate,
                                    const uint16_t *up, int64_t M, int64_t ld,
                                    uint8_t *a_mant, uint8_t *a_exp, void *stream) {
   if (M > 0 && !up) return MXQ_ERR_NULL;
-  return quantize_common(fmt, gate, M, ld, a_mant, a_exp, stream, kImage, nullptr, 0.f, up);
+  return mxq::quantize_common(fmt, gate, M, ld, a_mant, a_exp, stream, kImage, nullptr, 0.f, up);
 }
 
 mxq_status mxq_pack_weights(const mxq_fmt *fmt, const uint16_t *w, int64_t N,
                             int64_t ldw, uint8_t *w_mant, uint8_t *w_exp,
                             void *stream) {
-  return quantize_common(fmt, w, N, ldw, w_mant, w_exp, stream, kWeights);
+  return mxq::quantize_common(fmt, w, N, ldw, w_mant, w_exp, stream, kWeights);
 }
 
 mxq_status mxq_gemm(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_mant,
                     const uint8_t *a_exp, const uint8_t *w_mant, const uint8_t *w_exp,
                     float *y, int64_t ldy, void *stream) {
   mxq::GemmArgs g;
-  mxq_status st = gemm_args(fmt, M, N, a_mant, a_exp, w_mant, w_exp, y, &g);
+  mxq_status st = mxq::gemm_args(fmt, M, N, a_mant, a_exp, w_mant, w_exp, y, &g);
   if (st != MXQ_OK) return st;
   if (M == 0 || N == 0) return MXQ_OK;
   if (ldy < N) return MXQ_ERR_SHAPE;
@@ -323,61 +327,12 @@ mxq_status mxq_gemm(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_m
                       : mxq::launch_gemm_prefill(g, s));
 }
 
-static mxq_status quantize_experts(const mxq_fmt *fmt, const mxq_experts *plan,
-                                   const int32_t *perms, const uint16_t *src, const uint16_t *src2,
-                                   int64_t per_row, int64_t ld, uint8_t *mant, uint8_t *exp,
-                                   void *stream) {
-  mxq::Groups g;
-  const mxq_status st = mxq::check_experts(plan, &g);
-  if (st != MXQ_OK) return st;
-  if (per_row < 1 || per_row > INT32_MAX || g.pairs % per_row) return MXQ_ERR_SHAPE;
-  if (!aligned16(perms)) return MXQ_ERR_ALIGN;
-  return quantize_common(fmt, src, g.pairs / per_row, ld, mant, exp, stream, kImage, nullptr, 0.f,
-                         src2, &g, per_row, perms);
-}
-
-mxq_status mxq_quantize_act_experts(const mxq_fmt *fmt, const mxq_experts *plan,
-                                    const int32_t *perms, const uint16_t *a, int64_t per_row,
-                                    int64_t lda, uint8_t *a_mant, uint8_t *a_exp, void *stream) {
-  return quantize_experts(fmt, plan, perms, a, nullptr, per_row, lda, a_mant, a_exp, stream);
-}
-
-mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts *plan,
-                                           const int32_t *perms, const uint16_t *gate,
-                                           const uint16_t *up, int64_t per_row, int64_t ld,
-                                           uint8_t *a_mant, uint8_t *a_exp, void *stream) {
-  if (plan && plan->pairs > 0 && !up) return MXQ_ERR_NULL;
-  return quantize_experts(fmt, plan, perms, gate, up, per_row, ld, a_mant, a_exp, stream);
-}
-
-mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t N,
-                            const uint8_t *a_mant, const uint8_t *a_exp, const uint8_t *w_mant,
-                            const uint8_t *w_exp, void *y, int y_f32, int64_t ldy, void *stream) {
-  mxq::Groups x;
-  mxq_status st = mxq::check_experts(plan, &x);
-  if (st != MXQ_OK) return st;
-  mxq::GemmArgs g;
-  st = gemm_args(fmt, x.pairs, N, a_mant, a_exp, w_mant, w_exp, y, &g);
-  if (st != MXQ_OK) return st;
-  if (x.pairs == 0 || N == 0) return MXQ_OK;
-  if (ldy < N || N > INT32_MAX) return MXQ_ERR_SHAPE;
-  // (every kernel has fewer workgroups than one of 256 threads per 16 rows and 32 columns)
-  if ((x.rows / 16 + x.E) * ((N + 31) / 32) >= 1 << 23) return MXQ_ERR_SHAPE;
-  g.x = x;
-  g.w_expert = g.w_super * w_supers(N);
-  g.w_expert_sc = g.w_super_sc * w_supers(N);
-  g.y = (float *)y;
-  g.y_bf16 = !y_f32;
-  g.ldy = ldy;
-  return launched(mxq::launch_gemm_experts(g, (hipStream_t)stream));
-}
-
 mxq_status mxq_gemm_partials(const mxq_fmt *fmt, int64_t M, int64_t N,
                              const uint8_t *a_mant, const uint8_t *a_exp,
                              const uint8_t *w_mant, const uint8_t *w_exp, int32_t *p,
                              void *stream) {
   mxq::GemmArgs g;
-  mxq_status st = gemm_args(fmt, M, N, a_mant, a_exp, w_mant, w_exp, p, &g);
+  mxq_status st = mxq::gemm_args(fmt, M, N, a_mant, a_exp, w_mant, w_exp, p, &g);
   if (st != MXQ_OK) return st;
   if (M == 0 || N == 0) return MXQ_OK;
   g.p = p;

@@ -108,6 +108,55 @@ mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_
   return launched(mxq::launch_route(a, plan_args(g, ids), (hipStream_t)stream));
 }
 
+static mxq_status quantize_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                   const int32_t *perms, const uint16_t *src, const uint16_t *src2,
+                                   int64_t per_row, int64_t ld, uint8_t *mant, uint8_t *exp,
+                                   void *stream) {
+  mxq::Groups g;
+  const mxq_status st = mxq::check_experts(plan, &g);
+  if (st != MXQ_OK) return st;
+  if (per_row < 1 || per_row > INT32_MAX || g.pairs % per_row) return MXQ_ERR_SHAPE;
+  if (!aligned(perms, 16)) return MXQ_ERR_ALIGN;
+  return mxq::quantize_common(fmt, src, g.pairs / per_row, ld, mant, exp, stream, mxq::kImage, nullptr, 0.f,
+                         src2, &g, per_row, perms);
+}
+
+mxq_status mxq_quantize_act_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                    const int32_t *perms, const uint16_t *a, int64_t per_row,
+                                    int64_t lda, uint8_t *a_mant, uint8_t *a_exp, void *stream) {
+  return quantize_experts(fmt, plan, perms, a, nullptr, per_row, lda, a_mant, a_exp, stream);
+}
+
+mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts *plan,
+                                           const int32_t *perms, const uint16_t *gate,
+                                           const uint16_t *up, int64_t per_row, int64_t ld,
+                                           uint8_t *a_mant, uint8_t *a_exp, void *stream) {
+  if (plan && plan->pairs > 0 && !up) return MXQ_ERR_NULL;
+  return quantize_experts(fmt, plan, perms, gate, up, per_row, ld, a_mant, a_exp, stream);
+}
+
+mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t N,
+                            const uint8_t *a_mant, const uint8_t *a_exp, const uint8_t *w_mant,
+                            const uint8_t *w_exp, void *y, int y_f32, int64_t ldy, void *stream) {
+  mxq::Groups x;
+  mxq_status st = mxq::check_experts(plan, &x);
+  if (st != MXQ_OK) return st;
+  mxq::GemmArgs g;
+  st = mxq::gemm_args(fmt, x.pairs, N, a_mant, a_exp, w_mant, w_exp, y, &g);
+  if (st != MXQ_OK) return st;
+  if (x.pairs == 0 || N == 0) return MXQ_OK;
+  if (ldy < N || N > INT32_MAX) return MXQ_ERR_SHAPE;
+  // (every kernel has fewer workgroups than one of 256 threads per 16 rows and 32 columns)
+  if ((x.rows / 16 + x.E) * ((N + 31) / 32) >= 1 << 23) return MXQ_ERR_SHAPE;
+  g.x = x;
+  g.w_expert = mxq_weight_bytes(fmt, N);
+  g.w_expert_sc = mxq_weight_exp_bytes(fmt, N);
+  g.y = (float *)y;
+  g.y_bf16 = !y_f32;
+  g.ldy = ldy;
+  return launched(mxq::launch_gemm_experts(g, (hipStream_t)stream));
+}
+
 mxq_status mxq_combine_experts(const void *y, int y_f32, int64_t ldy, const int32_t *ids,
                                const float *weights, int64_t T, int64_t k, int32_t experts,
                                int64_t N, const uint16_t *residual, int64_t ldr, void *out,

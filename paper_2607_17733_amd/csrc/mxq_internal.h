@@ -154,6 +154,18 @@ hipError_t launch_attn_decode(const AttnArgs &args, hipStream_t s);
 // Validates a format and derives its width segments (api.cpp).
 struct Segs;
 mxq_status check_fmt(const mxq_fmt *f, Segs *s);
+// The checks and the launch of every quantizer (by: of image rows by a plan, row r
+// from source row pair[r] / per_row), and the checks and arguments of a product
+// (api.cpp).
+enum QuantKind { kWeights, kImage, kRows };
+mxq_status quantize_common(const mxq_fmt *fmt, const uint16_t *src, int64_t rows, int64_t ld,
+                           uint8_t *mant, uint8_t *exp, void *stream, QuantKind kind,
+                           const uint16_t *gain = nullptr, float eps = 0.f,
+                           const uint16_t *src2 = nullptr, const Groups *by = nullptr,
+                           int64_t per_row = 1, const int32_t *perms = nullptr);
+mxq_status gemm_args(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_mant,
+                     const uint8_t *a_exp, const uint8_t *w_mant, const uint8_t *w_exp,
+                     const void *out, GemmArgs *g);
 
 // Rotary positions (rope.hip).
 constexpr int kRopeMaxRot = 512;

@@ -413,7 +413,7 @@ int device_cu_count() {
   return n;
 }
 
-hipError_t launch_gemm_experts(const GemmArgs &a, hipStream_t stream) {
+hipError_t launch_experts_decode(const GemmArgs &a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)(a.x.rows / 16));
   const auto fn = a.full ? gemm_decode_kernel<true, 1, 2, true> : gemm_decode_kernel<false, 1, 2, true>;
   hipLaunchKernelGGL(fn, grid, dim3(256), 0, stream, a);

@@ -50,6 +50,7 @@
 // complete.  Workgroup ids are remapped so that each XCD owns
 // a compact block of output tiles: the activation rows and weight columns it
 // reads stay in its L2.
+#include "experts_device.h"
 #include "mxq_device.h"
 #include "mxq_internal.h"
 
@@ -169,9 +170,60 @@ __device__ inline uint32_t lo_codes(uint32_t w) {
   return FULL ? (w & 0x0F0F0F0Fu) : (w & 0x8F8F8F8Fu);
 }
 
+// The tile of workgroup `pid` of rows by experts: XCD x takes the column tiles x,
+// x + 8, ... of four row tiles after the other, so that the row tiles of an expert
+// that run at one time share its weights in an L2, and workgroups behind the last
+// expert's rows come last.  nt may pass the last column tile.
+__device__ inline void expert_order(int pid, int ntiles, int &mt, int &nt) {
+  const int loc = pid >> 3, per = (ntiles + 7) >> 3, q = loc / (4 * per);
+  mt = 4 * q + (loc & 3);
+  nt = (pid & 7) + 8 * ((loc - q * 4 * per) >> 2);
+}
+
+// The arguments of one expert's tile of 2^LG rows; false: there is none.
+template <int LG>
+__device__ inline bool take_expert(GemmArgs &g, int mt, const int32_t *&pair) {
+  const ExpertTile x = expert_tile<LG>(g.x, mt);
+  if (x.rows <= 0) return false;
+  g.M = x.rows;
+  pair = g.x.pair + x.row0;
+  g.a_mant += (int64_t)(x.row0 >> 4) * g.a_tile;
+  g.a_exp += (int64_t)(x.row0 >> 4) * g.a_tile_sc;
+  g.w_mant += x.e * g.w_expert;
+  g.w_exp += x.e * g.w_expert_sc;
+  return true;
+}
+
+// Four columns from `col` on of a row: the row of a pair (p < 0: of none) where rows
+// are by experts.
+template <bool BY>
+__device__ inline void store_row(const GemmArgs &g, int64_t row, int64_t col, bool vec, v4f s) {
+  if (BY && g.y_bf16) {
+    typedef __bf16 v4h __attribute__((ext_vector_type(4)));
+    __bf16 *dst = (__bf16 *)g.y + row * g.ldy + col;
+    const v4h h = {(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
+    if (vec) {
+      __builtin_nontemporal_store(h, (v4h *)dst);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (col + c < g.N) dst[c] = h[c];
+    }
+    return;
+  }
+  float *dst = g.y + row * g.ldy + col;
+  if (vec) {
+    __builtin_nontemporal_store(s, (v4f *)dst);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (col + c < g.N) dst[c] = s[c];
+  }
+}
+
 // TM: 32-row tiles per wave (2: 256-row workgroup tiles, one workgroup per
-// CU; 1: 128-row tiles, two per CU).
-template <bool FULL, int TM>
+// CU; 1: 128-row tiles, two per CU).  BY: the rows of experts (GemmArgs::x).
+template <bool FULL, int TM, bool BY = false>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(3 - TM, 3 - TM)))
 void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
   constexpr int BM = 128 * TM;
@@ -185,7 +237,9 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
     // XCD x (workgroups pid % 8 == x) owns a block of (mtiles / gm) x
     // (ntiles / gn) tiles, walked row by row.
     const int pid = blockIdx.x;
-    if (gm > 0) {
+    if (BY) {
+      expert_order(pid, ntiles, mt, nt);
+    } else if (gm > 0) {
       const int x = pid & 7, loc = pid >> 3;
       const int bm = mtiles / gm, bn = ntiles / gn;
       mt = (x / gn) * bm + loc / bn;
@@ -195,7 +249,9 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
       nt = pid - mt * ntiles;
     }
   }
-  const int64_t row0 = (int64_t)mt * BM, col0 = (int64_t)nt * BN;
+  const int32_t *pair = nullptr;
+  if (BY && (nt >= ntiles || !take_expert<(TM == 1 ? 7 : 8)>(g, mt, pair))) return;
+  const int64_t row0 = BY ? 0 : (int64_t)mt * BM, col0 = (int64_t)nt * BN;
   const LGeo lg(g.n3, g.n4, g.n6, g.n8);
   const int nsteps = lg.nsteps;
   char *const ring = (char *)lds;
@@ -588,16 +644,14 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
                     acc[tm][tn][4 * q + 3]};
         // lane (quad k, j) now: row rr + j, columns (cc & ~3) .. + 3
         s = quad_transpose(s, j);
-        const int64_t row = row0 + rr + j, col = col0 + (cc & ~3);
+        int64_t row = row0 + rr + j;
+        const int64_t col = col0 + (cc & ~3);
         if (row >= g.M) continue;
-        float *dst = g.y + row * g.ldy + col;
-        if (vec) {
-          __builtin_nontemporal_store(s, (v4f *)dst);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (col + c < g.N) dst[c] = s[c];
+        if (BY) {
+          row = pair[row];
+          if (row < 0 || row >= g.x.pairs) continue;
         }
+        store_row<BY>(g, row, col, vec, s);
       }
 }
 
@@ -610,7 +664,7 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
 // and activations straight into registers, a step ahead, each weight slot
 // refilled as soon as its operand is restored.  The latency of a step and, over
 // many tiles, the L2 reads of the weights (once per 32 TM rows) bound it.
-template <bool FULL, int KG, int TM, bool ONCE>
+template <bool FULL, int KG, int TM, bool ONCE, bool BY = false>
 __global__ __launch_bounds__(64 * KG) __attribute__((amdgpu_waves_per_eu(3 - TM, 3 - TM)))
 void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
   constexpr int kAux = ONCE ? 2 : 0;              // non-temporal weight loads
@@ -623,7 +677,9 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
   int mt, nt;
   {
     const int pid = blockIdx.x;
-    if (nx > 0) {
+    if (BY) {
+      expert_order(pid, ntiles, mt, nt);
+    } else if (nx > 0) {
       const int loc = pid >> 3;
       nt = (pid & 7) * nx + loc / mtiles;
       mt = loc % mtiles;
@@ -632,7 +688,9 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
       mt = pid - nt * mtiles;
     }
   }
-  const int64_t row0 = (int64_t)mt * 32 * TM, col0 = (int64_t)nt * BN;
+  const int32_t *pair = nullptr;
+  if (BY && (nt >= ntiles || !take_expert<(TM == 1 ? 5 : 6)>(g, mt, pair))) return;
+  const int64_t row0 = BY ? 0 : (int64_t)mt * 32 * TM, col0 = (int64_t)nt * BN;
   const LGeo lg(g.n3, g.n4, g.n6, g.n8);
 
   const int64_t last = (g.M - 1) / kATileRows, ta = row0 / kATileRows;
@@ -900,16 +958,14 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
 #pragma unroll
     for (int k = 1; k < KG; ++k) s += red[k][tq][lane];
     s = quad_transpose(s, j);
-    const int64_t row = row0 + 32 * tm + 8 * q + 4 * lh + j, col = col0 + ((tn * 32 + l32) & ~3);
+    int64_t row = row0 + 32 * tm + 8 * q + 4 * lh + j;
+    const int64_t col = col0 + ((tn * 32 + l32) & ~3);
     if (row >= g.M) continue;
-    float *dst = g.y + row * g.ldy + col;
-    if (vec) {
-      __builtin_nontemporal_store(s, (v4f *)dst);
-    } else {
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (col + c < g.N) dst[c] = s[c];
+    if (BY) {
+      row = pair[row];
+      if (row < 0 || row >= g.x.pairs) continue;
     }
+    store_row<BY>(g, row, col, vec, s);
   }
 }
 
@@ -1040,6 +1096,39 @@ hipError_t launch_gemm_prefill(const GemmArgs &a, hipStream_t stream) {
   else if (wg256 < device_cu_count()) go(std::false_type{}, std::integral_constant<int, 1>{});
   else go(std::false_type{}, std::integral_constant<int, 2>{});
   return hipGetLastError();
+}
+
+// Rows by experts: tiles of 2^lg rows of every expert, as many as any choice has.
+static int64_t expert_tiles(const GemmArgs &a, int lg) {
+  const int64_t active = std::min<int64_t>(a.x.E, a.x.pairs);
+  return active + ((a.x.rows - 16 * active) >> lg);
+}
+
+template <bool FULL>
+static hipError_t go_experts(const GemmArgs &a, hipStream_t stream) {
+  const int ntiles = (int)((a.N + BN - 1) / BN);
+  auto grid = [&](int lg) {
+    return dim3((unsigned)((expert_tiles(a, lg) + 3) / 4 * 4 * ((ntiles + 7) / 8 * 8)));
+  };
+  const int64_t mean = a.x.pairs / std::min<int64_t>(a.x.E, a.x.pairs);
+  if (mean <= 16) return launch_experts_decode(a, stream);
+  if (mean <= 32)
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 1, false, true>), grid(5), dim3(256), 0, stream, a, 0,
+                       ntiles, 0);
+  else if (mean <= 96)
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 2, false, true>), grid(6), dim3(256), 0, stream, a, 0,
+                       ntiles, 0);
+  else if (mean <= 256 && !FULL)
+    hipLaunchKernelGGL((gemm_prefill_kernel<FULL, 1, true>), grid(7), dim3(NT), 0, stream, a, 0, ntiles,
+                       0, 0);
+  else
+    hipLaunchKernelGGL((gemm_prefill_kernel<FULL, 2, true>), grid(8), dim3(NT), 0, stream, a, 0, ntiles,
+                       0, 0);
+  return hipGetLastError();
+}
+
+hipError_t launch_gemm_experts(const GemmArgs &a, hipStream_t stream) {
+  return a.full ? go_experts<true>(a, stream) : go_experts<false>(a, stream);
 }
 
 }  // namespace mxq

@@ -219,6 +219,7 @@ hipError_t launch_route(const RouteArgs &args, const PlanArgs &plan, hipStream_t
 hipError_t launch_combine(const CombineArgs &args, hipStream_t s);
 // The products of every expert's rows (decode.hip, gemm_prefill.hip).
 hipError_t launch_gemm_experts(const GemmArgs &args, hipStream_t s);
+hipError_t launch_experts_decode(const GemmArgs &args, hipStream_t s);
 
 // Norms of queries and keys with their rotation (rope.hip).
 struct NormArgs {

@@ -666,7 +666,7 @@ mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
  * are added with the router's weights.  (The paper quantizes every linear of a
  * decoder layer, Section 5; an expert's linears are such.)  Pair p = t * k + j
  * is the j-th choice of token t; an id outside [0, E) is no choice: its pair
- * takes no part and its rows are neither read nor written anywhere below.
+ * takes no part: its rows are not written, and what they hold does not matter.
  *
  * The plan of a batch lays the pairs out in rows of the operand image (layout
  * (A)), each expert's rows from a multiple of 16 on, in the order of the pairs:

@@ -11,6 +11,9 @@ namespace {
 
 constexpr int kThreads = 256;
 
+typedef unsigned comb_u4 __attribute__((ext_vector_type(4)));
+typedef float comb_f4 __attribute__((ext_vector_type(4)));
+
 __device__ inline float bf16f(uint32_t bits) { return __uint_as_float(bits << 16); }
 __device__ inline uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
@@ -77,13 +80,11 @@ __device__ inline uint64_t key_of(double x) {
   return u >> 63 ? ~u : u | (uint64_t)1 << 63;
 }
 
-// A wave per token; lane l holds the scores of experts l, l + 64, ...
+// The choice of one token by one wave; lane l holds the scores of experts l, l + 64,
+// ...  Lane j < k returns the j-th choice and its weight.
 template <int NE, bool BIAS>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+__device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float &weight) {
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * (kThreads / 64) +
-                    __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (t >= a.T) return;
   float x[NE];
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
@@ -176,100 +177,299 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
       all += x[i] == -__builtin_inff() ? 0.f : expf(x[i] - most);
     sum = (double)wave_sum(all);
   }
+  chosen = id;
+  weight = id >= 0 && sum > 0.0 ? (float)((double)a.scale * (s / sum)) : 0.f;
+}
+
+// A wave per token.
+template <int NE, bool BIAS>
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * (kThreads / 64) +
+                    __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= a.T) return;
+  int id;
+  float w;
+  choose<NE, BIAS>(a, t, id, w);
   if (lane < a.k) {
     a.ids[t * a.k + lane] = id;
-    a.weights[t * a.k + lane] = id >= 0 && sum > 0.0 ? (float)((double)a.scale * (s / sum)) : 0.f;
+    a.weights[t * a.k + lane] = w;
   }
 }
 
-// The plan, a workgroup per expert: the counts of all of them, its own rows.
-__global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs a) {
-  __shared__ int count[kMaxExperts];
-  __shared__ int part[kThreads / 64];
-  const int t = threadIdx.x, e = blockIdx.x, lane = t & 63, wave = t >> 6;
-  for (int i = t; i < a.E; i += kThreads) count[i] = 0;
-  __syncthreads();
-  for (int64_t p = t; p < a.pairs; p += kThreads) {
-    const int id = a.ids[p];
-    if (id >= 0 && id < a.E) atomicAdd(&count[id], 1);
+// ---------------------------------------------------------------------------
+// The plan.  Every workgroup counts all pairs of all experts, so that no workgroup
+// waits for another and one launch does it; then it lays out one expert's.
+
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+// A wave's share of the pairs, four to a lane: f(first pair of the lane's four, their
+// ids), -1 behind the last pair.
+template <typename F>
+__device__ inline void each_four(const PlanArgs &a, int wave, int lane, F f) {
+  const int P = (int)a.pairs, per = ((P + kPlanWaves - 1) / kPlanWaves + 255) & ~255;
+  const int end = min(P, (wave + 1) * per);
+#pragma unroll 4
+  for (int p0 = wave * per; p0 < end; p0 += 256) {
+    const int p = p0 + 4 * lane;
+    int4 id = {-1, -1, -1, -1};
+    if (p + 3 < P) {
+      id = *(const int4 *)(a.ids + p);
+    } else {
+      if (p < P) id.x = a.ids[p];
+      if (p + 1 < P) id.y = a.ids[p + 1];
+      if (p + 2 < P) id.z = a.ids[p + 2];
+    }
+    f(p, id);
   }
-  __syncthreads();
-  int before = 0;
-  for (int i = t; i < e; i += kThreads) before += (count[i] + 15) & ~15;
-  before = (int)wave_reduce((uint32_t)before, 0u, [](uint32_t x, uint32_t y) { return x + y; });
-  if (lane == 0) part[wave] = before;
+}
+
+// The sum of the experts' rows before expert e, count[] their pairs; every thread of
+// the workgroup calls it, part[] is its scratch.
+__device__ inline int rows_before(const int *count, int e, int *part) {
+  const int t = threadIdx.x, lane = t & 63;
+  const int mine = t < e ? (count[t] + 15) & ~15 : 0;      // (kMaxExperts threads)
+  const int sum = (int)wave_reduce((uint32_t)mine, 0u, [](uint32_t x, uint32_t y) { return x + y; });
+  if (lane == 0) part[t >> 6] = sum;
   __syncthreads();
   int row = 0;
-  for (int w = 0; w < kThreads / 64; ++w) row += part[w];
-  const int end = row + ((count[e] + 15) & ~15);
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) row += part[w];
+  __syncthreads();
+  return row;
+}
+static_assert(kPlanThreads >= kMaxExperts, "a thread per expert");
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+  __shared__ int count[kMaxExperts];
+  __shared__ int part[kPlanWaves];
+  const int t = threadIdx.x, e = blockIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  for (int i = t; i < a.E; i += kPlanThreads) count[i] = 0;
+  __syncthreads();
+  int mine = 0;                                            // the wave's pairs of expert e
+  each_four(a, wave, lane, [&](int, int4 id) {
+    if ((unsigned)id.x < (unsigned)a.E) atomicAdd(&count[id.x], 1);
+    if ((unsigned)id.y < (unsigned)a.E) atomicAdd(&count[id.y], 1);
+    if ((unsigned)id.z < (unsigned)a.E) atomicAdd(&count[id.z], 1);
+    if ((unsigned)id.w < (unsigned)a.E) atomicAdd(&count[id.w], 1);
+    mine += __popcll(__ballot(id.x == e)) + __popcll(__ballot(id.y == e)) +
+            __popcll(__ballot(id.z == e)) + __popcll(__ballot(id.w == e));
+  });
+  __syncthreads();
+  const int row = rows_before(count, e, part);
+  const int n = count[e], end = row + ((n + 15) & ~15);
   if (t == 0) a.first[e] = row;
-  if (t == 0 && e == a.E - 1) a.first[a.E] = end;
-  for (int i = row + count[e] + t; i < end; i += kThreads) a.pair[i] = -1;
-  if (e == a.E - 1)
-    for (int64_t i = end + t; i < a.rows; i += kThreads) a.pair[i] = -1;
-  for (int64_t p0 = 0; p0 < a.pairs; p0 += kThreads) {
-    const bool mine = p0 + t < a.pairs && a.ids[p0 + t] == e;
-    const uint64_t who = __ballot(mine);
-    __syncthreads();
-    if (lane == 0) part[wave] = __popcll(who);
-    __syncthreads();
-    int at = row, all = 0;
-    for (int w = 0; w < kThreads / 64; ++w) {
-      at += w < wave ? part[w] : 0;
-      all += part[w];
-    }
-    if (mine) a.pair[at + __popcll(who & (((uint64_t)1 << lane) - 1))] = (int)(p0 + t);
-    row += all;
+  if (row + n + t < end) a.pair[row + n + t] = -1;
+  if (e == a.E - 1) {                                      // and the rows behind the last expert's
+    if (t == 0) a.first[a.E] = end;
+    for (int64_t i = end + t; i < a.rows; i += kPlanThreads) a.pair[i] = -1;
   }
+  if (lane == 0) part[wave] = mine;
+  __syncthreads();
+  int at = row;
+  for (int w = 0; w < wave; ++w) at += part[w];
+  if (mine == 0) return;
+  each_four(a, wave, lane, [&](int p, int4 id) {
+    const uint64_t m[4] = {__ballot(id.x == e), __ballot(id.y == e), __ballot(id.z == e),
+                           __ballot(id.w == e)};
+    if ((m[0] | m[1] | m[2] | m[3]) == 0) return;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    int r = at, all = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      r += __popcll(m[c] & below);
+      all += __popcll(m[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (m[c] >> lane & 1) a.pair[r++] = p + c;
+    at += all;
+  });
 }
 
-// A thread per column of a token.
-__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= a.T * a.N) return;
-  const int64_t t = i / a.N, c = i - t * a.N;
-  float acc = a.residual ? bf16f(a.residual[t * a.ldr + c]) : 0.f;
-  for (int64_t j = 0; j < a.k; ++j) {
-    const int64_t p = t * a.k + j;
-    const int id = a.ids[p];
-    if (id < 0 || id >= a.E) continue;
-    const int64_t at = p * a.ldy + c;
-    const float y = a.y_f32 ? ((const float *)a.y)[at] : bf16f(((const uint16_t *)a.y)[at]);
-    acc = fmaf(a.weights[p], y, acc);
+// A few tokens: one workgroup chooses and plans, its pairs and rows in LDS.
+constexpr int kFewPairs = 256;
+
+template <int NE, bool BIAS>
+__global__ __launch_bounds__(kPlanThreads) void route_few_kernel(RouteArgs a, PlanArgs b) {
+  __shared__ int count[kMaxExperts];
+  __shared__ int start[kMaxExperts];
+  __shared__ int part[kPlanWaves];
+  __shared__ __attribute__((aligned(16))) int ids[kFewPairs + 4];
+  __shared__ int rows[16 * kFewPairs];
+  const int t = threadIdx.x, lane = t & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  for (int i = t; i < a.E; i += kPlanThreads) count[i] = 0;
+  for (int i = t; i < (int)b.rows; i += kPlanThreads) rows[i] = -1;
+  if (t < 4) ids[(b.pairs & ~3) + t] = -1;                 // (the last four's, before theirs are chosen)
+  __syncthreads();
+  for (int k = wave; k < (int)a.T; k += kPlanWaves) {
+    int id;
+    float w;
+    choose<NE, BIAS>(a, k, id, w);
+    if (lane < a.k) {
+      const int p = k * a.k + lane;
+      a.ids[p] = id;
+      a.weights[p] = w;
+      ids[p] = id;
+    }
   }
-  if (a.out_f32) ((float *)a.out)[t * a.ldo + c] = acc;
-  else ((uint16_t *)a.out)[t * a.ldo + c] = to_bf16(acc);
+  __syncthreads();
+  const int P = (int)b.pairs, id = t < P ? ids[t] : -1;
+  int rank = 0;
+  if (id >= 0) {
+    atomicAdd(&count[id], 1);
+#pragma unroll 8
+    for (int p = 0; p < P; p += 4) {
+      const int4 q = *(const int4 *)(ids + p);
+      rank += (p < t && q.x == id) + (p + 1 < t && q.y == id) + (p + 2 < t && q.z == id) +
+              (p + 3 < t && q.w == id);
+    }
+  }
+  __syncthreads();
+  // an expert's first row: the sums over the experts, a thread to each
+  const int mine = t < a.E ? (count[t] + 15) & ~15 : 0;
+  int upto = mine;
+  upto += (int)dpp_or<kShr1, 0xF>((uint32_t)upto, 0u);
+  upto += (int)dpp_or<kShr2, 0xF>((uint32_t)upto, 0u);
+  upto += (int)dpp_or<kShr4, 0xF>((uint32_t)upto, 0u);
+  upto += (int)dpp_or<kShr8, 0xF>((uint32_t)upto, 0u);
+  upto += (int)dpp_or<kBcast15, 0xA>((uint32_t)upto, 0u);
+  upto += (int)dpp_or<kBcast31, 0xC>((uint32_t)upto, 0u);
+  if (lane == 63) part[wave] = upto;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) upto += part[w];
+  if (t < a.E) {
+    start[t] = upto - mine;
+    b.first[t] = upto - mine;
+    if (t == a.E - 1) b.first[a.E] = upto;
+  }
+  __syncthreads();
+  if (id >= 0) rows[start[id] + rank] = t;
+  __syncthreads();
+  for (int i = t; i < (int)b.rows; i += kPlanThreads) b.pair[i] = rows[i];
+}
+
+// ---------------------------------------------------------------------------
+// A token's weighted sum: bytes bound it, so eight columns to a thread where the rows
+// allow 16-byte pieces, and the loads of four experts' rows in flight.
+
+template <bool VEC>
+__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
+  constexpr int C = VEC ? 8 : 1;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const uint32_t per = (uint32_t)(a.N / C);
+  const int64_t t = i / per;
+  if (t >= a.T) return;
+  const int64_t c = C * (i - t * per);
+  auto unpack = [](comb_u4 v, float *f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = __uint_as_float(v[e] << 16);
+      f[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+    }
+  };
+  float acc[C] = {};
+  if (a.residual) {
+    const uint16_t *r = a.residual + t * a.ldr + c;
+    if constexpr (VEC) unpack(*(const comb_u4 *)r, acc);
+    else acc[0] = bf16f(*r);
+  }
+  for (int j0 = 0; j0 < (int)a.k; j0 += 4) {
+    int id[4];
+    float w[4];
+    comb_u4 y[4][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      id[j] = -1;
+      if (j0 + j < a.k) {
+        const int64_t p = t * a.k + j0 + j;
+        id[j] = a.ids[p];
+        w[j] = a.weights[p];
+        const int64_t at = p * a.ldy + c;
+        if constexpr (VEC) {
+          const char *row = (const char *)a.y + at * (a.y_f32 ? 4 : 2);
+          y[j][0] = *(const comb_u4 *)row;
+          if (a.y_f32) y[j][1] = *(const comb_u4 *)(row + 16);
+        } else {
+          y[j][0][0] = a.y_f32 ? ((const uint32_t *)a.y)[at]
+                               : (uint32_t)((const uint16_t *)a.y)[at] << 16;
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (id[j] < 0 || id[j] >= a.E) continue;
+      float v[C];
+      if constexpr (!VEC) {
+        v[0] = __uint_as_float(y[j][0][0]);
+      } else if (a.y_f32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(y[j][e >> 2][e & 3]);
+      } else {
+        unpack(y[j][0], v);
+      }
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] = fmaf(w[j], v[e], acc[e]);
+    }
+  }
+  if constexpr (!VEC) {
+    if (a.out_f32) ((float *)a.out)[t * a.ldo + c] = acc[0];
+    else ((uint16_t *)a.out)[t * a.ldo + c] = to_bf16(acc[0]);
+  } else if (a.out_f32) {
+    comb_f4 *o = (comb_f4 *)((float *)a.out + t * a.ldo + c);
+    o[0] = comb_f4{acc[0], acc[1], acc[2], acc[3]};
+    o[1] = comb_f4{acc[4], acc[5], acc[6], acc[7]};
+  } else {
+    comb_u4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      o[e] = (uint32_t)to_bf16(acc[2 * e]) | (uint32_t)to_bf16(acc[2 * e + 1]) << 16;
+    *(comb_u4 *)((uint16_t *)a.out + t * a.ldo + c) = o;
+  }
 }
 
 }  // namespace
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL(plan_kernel, dim3((unsigned)a.E), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(plan_kernel, dim3((unsigned)a.E), dim3(kPlanThreads), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_route(const RouteArgs &a, const PlanArgs &p, hipStream_t s) {
-  if (a.T > 0) {
-    const dim3 grid((unsigned)((a.T + kThreads / 64 - 1) / (kThreads / 64))), block(kThreads);
-    auto go = [&](auto ne) {
-      constexpr int NE = decltype(ne)::value;
-      if (a.bias) hipLaunchKernelGGL((route_kernel<NE, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((route_kernel<NE, false>), grid, block, 0, s, a);
-    };
-    if (a.E <= 64) go(std::integral_constant<int, 1>{});
-    else if (a.E <= 128) go(std::integral_constant<int, 2>{});
-    else if (a.E <= 256) go(std::integral_constant<int, 4>{});
-    else if (a.E <= 512) go(std::integral_constant<int, 8>{});
-    else go(std::integral_constant<int, 16>{});
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return launch_expert_plan(p, s);
+  if (a.T == 0) return launch_expert_plan(p, s);
+  const bool few = a.T <= 2 * kPlanWaves && p.pairs <= kFewPairs;
+  const dim3 grid((unsigned)((a.T + kThreads / 64 - 1) / (kThreads / 64))), block(kThreads);
+  auto with = [&](auto ne, auto bias) {
+    constexpr int NE = decltype(ne)::value;
+    constexpr bool B = decltype(bias)::value;
+    if (few)
+      hipLaunchKernelGGL((route_few_kernel<NE, B>), dim3(1), dim3(kPlanThreads), 0, s, a, p);
+    else
+      hipLaunchKernelGGL((route_kernel<NE, B>), grid, block, 0, s, a);
+  };
+  auto go = [&](auto ne) {
+    if (a.bias) with(ne, std::true_type{});
+    else with(ne, std::false_type{});
+  };
+  if (a.E <= 64) go(std::integral_constant<int, 1>{});
+  else if (a.E <= 128) go(std::integral_constant<int, 2>{});
+  else if (a.E <= 256) go(std::integral_constant<int, 4>{});
+  else if (a.E <= 512) go(std::integral_constant<int, 8>{});
+  else go(std::integral_constant<int, 16>{});
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || few ? e : launch_expert_plan(p, s);
 }
 
 hipError_t launch_combine(const CombineArgs &a, hipStream_t s) {
-  const int64_t n = (a.T * a.N + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(combine_kernel, dim3((unsigned)n), dim3(kThreads), 0, s, a);
+  const int64_t yb = a.y_f32 ? 4 : 2, ob = a.out_f32 ? 4 : 2;
+  const bool vec =
+      a.N % 8 == 0 && ((a.ldy * yb | a.ldo * ob | (a.residual ? a.ldr * 2 : 0)) & 15) == 0 &&
+      (((uintptr_t)a.y | (uintptr_t)a.out | (uintptr_t)a.residual) & 15) == 0;
+  const int64_t n = (a.T * (a.N / (vec ? 8 : 1)) + kThreads - 1) / kThreads;
+  if (vec) hipLaunchKernelGGL(combine_kernel<true>, dim3((unsigned)n), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL(combine_kernel<false>, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

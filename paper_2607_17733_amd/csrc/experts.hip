@@ -80,6 +80,33 @@ __device__ inline uint64_t key_of(double x) {
   return u >> 63 ? ~u : u | (uint64_t)1 << 63;
 }
 
+// The largest key of a wave, key[i] being expert 64 i + lane's, and the lowest expert
+// that has it; its key is cleared.
+template <typename U>
+struct Best {
+  U key;
+  int e;
+};
+template <int NE, typename U>
+__device__ inline Best<U> best_of(U (&key)[NE], int lane) {
+  U mine = 0;
+  int at = 0;
+#pragma unroll
+  for (int i = 0; i < NE; ++i)
+    if (key[i] > mine) {
+      mine = key[i];
+      at = 64 * i + lane;
+    }
+  const U win = wave_max(mine);
+  const uint64_t who = __ballot(mine == win);
+  int e = __builtin_amdgcn_readlane(at, __builtin_ctzll(who));
+  if (who & (who - 1)) e = (int)~wave_max(mine == win ? ~(uint32_t)at : 0u);
+#pragma unroll
+  for (int i = 0; i < NE; ++i)
+    if (e == 64 * i + lane) key[i] = 0;
+  return Best<U>{win, e};
+}
+
 // The choice of one token by one wave; lane l holds the scores of experts l, l + 64,
 // ...  Lane j < k returns the j-th choice and its weight.
 template <int NE, bool BIAS>
@@ -98,69 +125,82 @@ __device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float 
     }
   }
   const bool softmax = a.score == MXQ_SCORE_SOFTMAX;
-  uint32_t top = 0;
+  uint32_t key[NE], top = 0;
 #pragma unroll
   for (int i = 0; i < NE; ++i) {
-    const uint32_t k = x[i] == -__builtin_inff() ? 0u : key_of(x[i]);
-    top = k > top ? k : top;
+    key[i] = x[i] == -__builtin_inff() ? 0u : key_of(x[i]);
+    top = max(top, key[i]);
   }
-  top = wave_max(top);
-  const float most = value_of(top);                        // (unused where no expert is left)
+  const float most = value_of(wave_max(top));              // (unused where no expert is left)
 
-  // keys of the choice: the score's, or those of score + bias in 64 bits
-  uint64_t key[NE];
-  if (BIAS) {
-    double s[NE], all = 0.0;
+  int id = -1;                                             // lane j: the j-th choice and its score
+  float sc = 0.f;
+  if (!BIAS) {
+    for (int j = 0; j < a.k; ++j) {
+      const Best<uint32_t> b = best_of<NE>(key, lane);
+      if (b.key == 0) break;
+      if (lane == j) {
+        id = b.e;
+        sc = value_of(b.key);
+      }
+    }
+  } else {
+    // The scores in 32 bits first.  Theirs and their sums' errors are below 2^-19 of the
+    // larger of 1 and the sum; where two neighbours of the order are within 2^-17, about
+    // one token in a hundred, all are formed in 64 bits.
+    float s[NE], all = 0.f;
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
-      const bool in = x[i] != -__builtin_inff();
-      s[i] = !in ? 0.0 : softmax ? exp((double)x[i] - (double)most) : 1.0 / (1.0 + exp(-(double)x[i]));
+      s[i] = x[i] == -__builtin_inff() ? 0.f : softmax ? expf(x[i] - most) : 1.f / (1.f + expf(-x[i]));
       all += s[i];
     }
     if (softmax) all = wave_sum(all);
+    float bias[NE];
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
       const int e = 64 * i + lane;
-      const double v = (softmax ? s[i] / all : s[i]) + (e < a.E ? (double)a.bias[e] : 0.0);
-      key[i] = x[i] == -__builtin_inff() || !(v > -__builtin_inf()) ? 0 : key_of(v);
+      bias[i] = e < a.E ? a.bias[e] : 0.f;
+      const float v = (softmax ? s[i] / all : s[i]) + bias[i];
+      key[i] = x[i] == -__builtin_inff() || !(v > -__builtin_inff()) ? 0u : key_of(v);
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < NE; ++i)                           // (the index below: the lowest wins)
-      key[i] = x[i] == -__builtin_inff()
-                   ? 0
-                   : (uint64_t)key_of(x[i]) << 32 | (uint32_t)~(64 * i + lane);
-  }
-  int id = -1;                                             // lane j: the j-th choice and its score
-  float sc = 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    uint64_t best = 0;
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < NE; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        at = i;
-      }
-    const uint64_t win = wave_max(best);
-    if (win == 0) break;
-    int e;
-    if (BIAS) {
-      const uint32_t mine = best == win ? ~(uint32_t)(64 * at + lane) : 0u;
-      e = (int)~wave_max(mine);
-    } else {
-      e = (int)~(uint32_t)win;
+    bool near = false;
+    float last = 0.f;
+    for (int j = 0; j <= a.k; ++j) {
+      const Best<uint32_t> b = best_of<NE>(key, lane);
+      if (b.key == 0) break;
+      const float v = value_of(b.key);
+      near = near || (j > 0 && !(last - v > 0x1p-17f * fmaxf(1.f, fabsf(last))));
+      last = v;
+      if (lane == j && j < a.k) id = b.e;
     }
-    float xe = 0.f;
+    if (near) {
+      double d[NE], sum = 0.0;
+      uint64_t wide[NE];
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-      if (e >> 6 == i) {
-        xe = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x[i]), e & 63));
-        if (lane == (e & 63)) key[i] = 0;
+      for (int i = 0; i < NE; ++i) {
+        d[i] = x[i] == -__builtin_inff() ? 0.0
+               : softmax                 ? exp((double)x[i] - (double)most)
+                                         : 1.0 / (1.0 + exp(-(double)x[i]));
+        sum += d[i];
       }
-    if (lane == j) {
-      id = e;
-      sc = xe;
+      if (softmax) sum = wave_sum(sum);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        const double v = (softmax ? d[i] / sum : d[i]) + (double)bias[i];
+        wide[i] = x[i] == -__builtin_inff() || !(v > -__builtin_inf()) ? 0 : key_of(v);
+      }
+      id = -1;
+      for (int j = 0; j < a.k; ++j) {
+        const Best<uint64_t> b = best_of<NE>(wide, lane);
+        if (b.key == 0) break;
+        if (lane == j) id = b.e;
+      }
+    }
+    if (id >= 0) {
+      const int64_t at = t * a.ld + id;
+      sc = fminf(a.logits_f32 ? ((const float *)a.logits)[at]
+                              : bf16f(((const uint16_t *)a.logits)[at]),
+                 3.40282347e38f);
     }
   }
   // float64 exponentials of the chosen: x - most is not exact in 32 bits
@@ -247,15 +287,15 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
   for (int i = t; i < a.E; i += kPlanThreads) count[i] = 0;
   __syncthreads();
-  int mine = 0;                                            // the wave's pairs of expert e
+  int mine = 0;                                            // the lane's pairs of expert e
   each_four(a, wave, lane, [&](int, int4 id) {
     if ((unsigned)id.x < (unsigned)a.E) atomicAdd(&count[id.x], 1);
     if ((unsigned)id.y < (unsigned)a.E) atomicAdd(&count[id.y], 1);
     if ((unsigned)id.z < (unsigned)a.E) atomicAdd(&count[id.z], 1);
     if ((unsigned)id.w < (unsigned)a.E) atomicAdd(&count[id.w], 1);
-    mine += __popcll(__ballot(id.x == e)) + __popcll(__ballot(id.y == e)) +
-            __popcll(__ballot(id.z == e)) + __popcll(__ballot(id.w == e));
+    mine += (id.x == e) + (id.y == e) + (id.z == e) + (id.w == e);
   });
+  mine = (int)wave_reduce((uint32_t)mine, 0u, [](uint32_t x, uint32_t y) { return x + y; });
   __syncthreads();
   const int row = rows_before(count, e, part);
   const int n = count[e], end = row + ((n + 15) & ~15);
@@ -271,9 +311,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   for (int w = 0; w < wave; ++w) at += part[w];
   if (mine == 0) return;
   each_four(a, wave, lane, [&](int p, int4 id) {
+    if (__ballot(id.x == e || id.y == e || id.z == e || id.w == e) == 0) return;
     const uint64_t m[4] = {__ballot(id.x == e), __ballot(id.y == e), __ballot(id.z == e),
                            __ballot(id.w == e)};
-    if ((m[0] | m[1] | m[2] | m[3]) == 0) return;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     int r = at, all = 0;
 #pragma unroll

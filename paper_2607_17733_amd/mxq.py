@@ -795,49 +795,46 @@ def rope(x, pos, table, interleaved: bool = False, out=None):
     return out
 
 
-def _gain(t, D: int, what: str, dev):
-    """A contiguous bf16 device tensor of D elements: its address."""
-    return _index(t, D, torch.bfloat16, what, dev)
-
-
 def rope_qk(q, k, pos, table, q_gain, k_gain, eps: float, interleaved: bool = False, q_out=None,
             k_out=None):
     """Queries q [T, Hq, D] and keys k [T, Hk, D] (bf16, strided; either may be None)
     normalised per head (x / sqrt(mean x^2 + eps) times its gain, bf16 [D]) and
     rotated as rope does, rounded once: (q_out, k_out).  Each may be its source (in
     place), else a tensor that overlaps none."""
-    first = q if q is not None else k
-    if first is None:
+    some = q if q is not None else k
+    if some is None:
         raise MxqError("rope_qk needs q or k")
-    T, _, D = _heads(first, "q or k")
-    dev = first.device
+    T, _, D = _heads(some, "q or k")
+    dev = some.device
     stream = _current(dev, "q or k")
-    sides, outs, gains = [], [], []
-    for x, gain, out, what in ((q, q_gain, q_out, "q"), (k, k_gain, k_out, "k")):
-        if x is None:
-            if out is not None:
-                raise MxqError("%s_out needs %s" % (what, what))
-            sides += [None, 0, 0, 0, None, 0, 0]
-            outs.append(None)
-            gains.append(None)
-            continue
-        Tx, H, _ = _heads(x, what, dev, None, D)
-        if Tx != T:
-            raise MxqError("q and k have %d and %d tokens" % (T, Tx))
-        if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
-        elif out is not x and _heads(out, what + "_out", dev, H, D)[0] != T:
-            raise MxqError("%s_out is %s, not %s" % (what, tuple(out.shape), tuple(x.shape)))
-        sx, so = x.stride(), out.stride()
-        sides += [x.data_ptr(), H, sx[0], sx[1], out.data_ptr(), so[0], so[1]]
-        outs.append(out)
-        gains.append(_gain(gain, D, what + "_gain", dev))
-    status = lib().mxq_rope_qk(_rotary(table, dev, interleaved),
-                               ctypes.byref(_QkNorm(gains[0], gains[1], eps)),
-                               _index(pos, T, torch.int32, "pos", dev), T, D, *sides, stream)
+    q_out, qs = _norm_side(q, q_gain, q_out, "q", T, D, dev)
+    k_out, ks = _norm_side(k, k_gain, k_out, "k", T, D, dev)
+    norm = _QkNorm(qs[0], ks[0], eps)
+    status = lib().mxq_rope_qk(_rotary(table, dev, interleaved), ctypes.byref(norm),
+                               _index(pos, T, torch.int32, "pos", dev), T, D, *qs[1:], *ks[1:],
+                               stream)
     if status:
         _check(status, "mxq_rope_qk")
-    return tuple(outs)
+    return q_out, k_out
+
+
+def _norm_side(x, gain, out, what: str, T: int, D: int, dev):
+    """The result and the arguments of rope_qk's queries or keys."""
+    if x is None:
+        if out is not None:
+            raise MxqError("%s_out needs %s" % (what, what))
+        return None, (None, None, 0, 0, 0, None, 0, 0)
+    Tx, H, _ = _heads(x, what, dev, None, D)
+    if Tx != T:
+        raise MxqError("q and k have %d and %d tokens" % (T, Tx))
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    elif out is not x and _heads(out, what + "_out", dev, H, D)[0] != T:
+        raise MxqError("%s_out is %s, not %s" % (what, tuple(out.shape), tuple(x.shape)))
+    at, hs, _ = x.stride()
+    oat, ohs, _ = out.stride()
+    return out, (_index(gain, D, torch.bfloat16, what + "_gain", dev), x.data_ptr(), H, at, hs,
+                 out.data_ptr(), oat, ohs)
 
 
 class PagedCache:
@@ -923,8 +920,8 @@ def kv_append(cache: PagedCache, k, v, slots, pos=None, rope=None, interleaved: 
     else:
         if r is None or (q is None) != (q_gain is None):
             raise MxqError("gains need rope, and q_gain goes with q")
-        norm = _QkNorm(None if q is None else _gain(q_gain, 128, "q_gain", dev),
-                       _gain(k_gain, 128, "k_gain", dev), eps)
+        norm = _QkNorm(None if q is None else _index(q_gain, 128, torch.bfloat16, "q_gain", dev),
+                       _index(k_gain, 128, torch.bfloat16, "k_gain", dev), eps)
         status = lib().mxq_kv_append_norm(cache.fmt._ref, cache._ref, ctypes.byref(norm), *args)
     if status:
         _check(status, "mxq_kv_append")

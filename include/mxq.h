@@ -676,18 +676,23 @@ mxq_status mxq_attn_paged(const mxq_fmt *fmt, const mxq_paged_kv *cache,
  *            .. first[e + 1] - 1 (its count rounded up to 16); first[0] = 0.
  *   pair     DEVICE int32 [mxq_expert_rows(pairs, E)], 16-byte aligned: the pair
  *            of each row, -1 for a row that holds none.
+ *   work     DEVICE int32 [MXQ_EXPERT_WORK * E], 16-byte aligned: scratch of the calls
+ *            that write the plan (the others take NULL as well), which needs no
+ *            initialisation.  Calls that may overlap in time must not share it.
  * mxq_expert_rows: the most rows that any choice needs, (pairs + 15 min(E,
  * pairs)) rounded down to 16; negative mxq_status on bad counts.  So buffers and
  * launches have the same size whatever the choice, and a captured step serves
  * every batch of T tokens.  The calls that take a plan read it on the device: it
  * is what mxq_route or mxq_expert_plan wrote for the same pairs and experts.
  */
+#define MXQ_EXPERT_WORK 64
 typedef struct {
   int64_t pairs;
   int32_t experts;
   int32_t reserved;        /* must be 0 */
   int32_t *first;
   int32_t *pair;
+  int32_t *work;
 } mxq_experts;
 
 int64_t mxq_expert_rows(int64_t pairs, int32_t experts);
@@ -699,12 +704,12 @@ int64_t mxq_expert_rows(int64_t pairs, int32_t experts);
  * Chosen are the k largest x[e] (both scores rise with x) or, with bias (DEVICE
  * float [E], not NULL), the k largest s[e] + bias[e], formed in float64; equal
  * ones go to the lowest index; ids[t][j] in falling order.  weights[t][j] = scale *
- * s[ids[t][j]], or with normalise scale * s / (sum of the chosen s), in float32
- * (relative error below 1e-6 where s is a normal float32); the bias enters the
- * choice only.  A logit of -Inf or NaN, and a bias that makes s + bias -Inf or NaN,
- * keeps its expert from being chosen, the former out of every sum too; +Inf
- * counts as the largest float.  Where fewer than k are left, the other ids are -1
- * and their weights 0; so are the weights of chosen scores that sum to 0.
+ * s[ids[t][j]], or with normalise scale * s / (sum of the chosen s), a ratio that is
+ * formed however small the scores, in float32 (relative error below 1e-6 where the
+ * result is a normal float32); the bias enters the choice only.  A logit of -Inf or
+ * NaN, and a bias that makes s + bias -Inf or NaN, keeps its expert from being chosen,
+ * the former out of every sum too; +Inf counts as the largest float.  Where fewer
+ * than k are left, the other ids are -1 and their weights 0.
  *   T >= 0; E = plan's experts; k 1 .. min(E, 32); T * k = plan's pairs.
  *   logits   DEVICE, float32 or (logits_f32 == 0) bf16, ld >= E, read only; any
  *            alignment of its type.

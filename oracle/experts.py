@@ -34,8 +34,14 @@ def route(logits, k, score="softmax", normalise=True, scale=1.0, bias=None):
         may = ok & ~np.isnan(key) & (key != -np.inf)
         order = [e for e in sorted(range(E), key=lambda e: (-key[e] if may[e] else np.inf, e)) if may[e]][:k]
         got = s[order]
-        if normalise:
-            got = got / got.sum() if got.sum() > 0 else got * 0
+        if normalise and order:                          # ratios, whatever the scores' size
+            c = x[order]
+            if score == "softmax":
+                got = np.exp(c - c.max())
+            else:
+                low = np.minimum(c, 0)
+                got = np.exp(low - min(c.max(), 0)) / (1 + np.exp(-np.abs(c)))
+            got = got / got.sum()
         ids[t, :len(order)], w[t, :len(order)] = order, got * np.float64(np.float32(scale))
     return ids, w
 

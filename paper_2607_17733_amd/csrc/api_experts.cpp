@@ -28,8 +28,14 @@ int64_t expert_rows(int64_t pairs, int64_t experts) {
   return (pairs + 15 * (pairs < experts ? pairs : experts)) & ~(int64_t)15;
 }
 
-mxq::PlanArgs plan_args(const mxq::Groups &g, const int32_t *ids) {
+mxq_status check_work(const mxq_experts *p) {
+  if (!p->work) return MXQ_ERR_NULL;
+  return aligned(p->work, 16) ? MXQ_OK : MXQ_ERR_ALIGN;
+}
+
+mxq::PlanArgs plan_args(const mxq::Groups &g, const int32_t *ids, int32_t *work) {
   mxq::PlanArgs a{};
+  a.work = work;
   a.ids = ids;
   a.pairs = g.pairs;
   a.rows = g.rows;
@@ -70,11 +76,11 @@ int64_t mxq_expert_rows(int64_t pairs, int32_t experts) {
 
 mxq_status mxq_expert_plan(const int32_t *ids, const mxq_experts *plan, void *stream) {
   mxq::Groups g;
-  const mxq_status st = mxq::check_experts(plan, &g);
-  if (st != MXQ_OK) return st;
+  mxq_status st = mxq::check_experts(plan, &g);
+  if (st != MXQ_OK || (st = check_work(plan)) != MXQ_OK) return st;
   if (g.pairs > 0 && !ids) return MXQ_ERR_NULL;
   if (!aligned(ids, 16)) return MXQ_ERR_ALIGN;
-  return launched(mxq::launch_expert_plan(plan_args(g, ids), (hipStream_t)stream));
+  return launched(mxq::launch_expert_plan(plan_args(g, ids, plan->work), (hipStream_t)stream));
 }
 
 mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_f32, int64_t T,
@@ -82,8 +88,8 @@ mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_
                      void *stream) {
   if (!opts) return MXQ_ERR_NULL;
   mxq::Groups g;
-  const mxq_status st = mxq::check_experts(plan, &g);
-  if (st != MXQ_OK) return st;
+  mxq_status st = mxq::check_experts(plan, &g);
+  if (st != MXQ_OK || (st = check_work(plan)) != MXQ_OK) return st;
   if (opts->score != MXQ_SCORE_SOFTMAX && opts->score != MXQ_SCORE_SIGMOID)
     return MXQ_ERR_UNSUPPORTED;
   if (opts->k < 1 || opts->k > 32 || opts->k > g.E || !isfinite(opts->scale)) return MXQ_ERR_SHAPE;
@@ -105,7 +111,7 @@ mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_
   a.bias = opts->bias;
   a.ids = ids;
   a.weights = weights;
-  return launched(mxq::launch_route(a, plan_args(g, ids), (hipStream_t)stream));
+  return launched(mxq::launch_route(a, plan_args(g, ids, plan->work), (hipStream_t)stream));
 }
 
 static mxq_status quantize_experts(const mxq_fmt *fmt, const mxq_experts *plan,

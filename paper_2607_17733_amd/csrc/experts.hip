@@ -1,6 +1,7 @@
 // experts.hip -- routing of tokens to experts, the plan that lays the chosen pairs
 // out by expert, and the weighted sum of a token's experts (include/mxq.h states
 // them).
+#include <algorithm>
 #include <type_traits>
 
 #include "mxq_internal.h"
@@ -49,6 +50,15 @@ __device__ inline U wave_reduce(U v, U none, F f) {
   v = f(v, dpp_or<kBcast15, 0xA>(v, none));
   v = f(v, dpp_or<kBcast31, 0xC>(v, none));
   return last_lane(v);
+}
+// The sum over the lanes up to this one.
+__device__ inline int lanes_upto(int v) {
+  v += (int)dpp_or<kShr1, 0xF>((uint32_t)v, 0u);
+  v += (int)dpp_or<kShr2, 0xF>((uint32_t)v, 0u);
+  v += (int)dpp_or<kShr4, 0xF>((uint32_t)v, 0u);
+  v += (int)dpp_or<kShr8, 0xF>((uint32_t)v, 0u);
+  v += (int)dpp_or<kBcast15, 0xA>((uint32_t)v, 0u);
+  return v + (int)dpp_or<kBcast31, 0xC>((uint32_t)v, 0u);
 }
 template <typename U>
 __device__ inline U wave_max(U v) {
@@ -203,22 +213,33 @@ __device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float 
                  3.40282347e38f);
     }
   }
-  // float64 exponentials of the chosen: x - most is not exact in 32 bits
-  double s = 0.0;
-  if (id >= 0)
-    s = softmax ? exp((double)sc - (double)most) : 1.0 / (1.0 + exp(-(double)sc));
-  double sum = 1.0;
+  // The chosen scores, relative to exp(ref) where only their ratios count, so that none is
+  // lost; x - ref with what its rounding leaves, so that the exponential is good to its
+  // own two units.
+  float ref = softmax ? most : 0.f;
+  if (a.normalise) {
+    const float best = value_of(wave_max(id >= 0 ? key_of(sc) : 0u));
+    ref = softmax ? best : fminf(best, 0.f);
+  }
+  float s = 0.f;
+  if (id >= 0) {
+    const float d = sc - ref, back = d - sc;
+    const float rest = (sc - (d - back)) - (ref + back);
+    // (below -104 it is 0; far below, d overflows and has no rest)
+    s = d < -110.f ? 0.f : expf(d) * (1.f + rest);
+    if (!softmax) s = sc > 0.f ? 1.f / (1.f + expf(-sc)) : s / (1.f + expf(sc));
+  }
+  float sum = 1.f;
   if (a.normalise) {
     sum = wave_sum(s);
   } else if (softmax) {
-    float all = 0.f;
+    sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NE; ++i)
-      all += x[i] == -__builtin_inff() ? 0.f : expf(x[i] - most);
-    sum = (double)wave_sum(all);
+    for (int i = 0; i < NE; ++i) sum += x[i] == -__builtin_inff() ? 0.f : expf(x[i] - most);
+    sum = wave_sum(sum);
   }
   chosen = id;
-  weight = id >= 0 && sum > 0.0 ? (float)((double)a.scale * (s / sum)) : 0.f;
+  weight = id >= 0 && sum > 0.f ? a.scale * (s / sum) : 0.f;
 }
 
 // A wave per token.
@@ -238,94 +259,119 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// The plan.  Every workgroup counts all pairs of all experts, so that no workgroup
-// waits for another and one launch does it; then it lays out one expert's.
+// The plan, a sort of the pairs by expert that keeps their order: the pairs in at most
+// kPlanParts runs, a workgroup each.  One launch counts every run's pairs by expert,
+// the next adds the counts up and places the runs' pairs; a single run counts itself.
+// 65528 pairs of 256 experts: 7 + 2 to 4 us; with a workgroup to each expert that looked
+// through all pairs, in one launch, 20.
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-
-// A wave's share of the pairs, four to a lane: f(first pair of the lane's four, their
-// ids), -1 behind the last pair.
-template <typename F>
-__device__ inline void each_four(const PlanArgs &a, int wave, int lane, F f) {
-  const int P = (int)a.pairs, per = ((P + kPlanWaves - 1) / kPlanWaves + 255) & ~255;
-  const int end = min(P, (wave + 1) * per);
-#pragma unroll 4
-  for (int p0 = wave * per; p0 < end; p0 += 256) {
-    const int p = p0 + 4 * lane;
-    int4 id = {-1, -1, -1, -1};
-    if (p + 3 < P) {
-      id = *(const int4 *)(a.ids + p);
-    } else {
-      if (p < P) id.x = a.ids[p];
-      if (p + 1 < P) id.y = a.ids[p + 1];
-      if (p + 2 < P) id.z = a.ids[p + 2];
-    }
-    f(p, id);
-  }
-}
-
-// The sum of the experts' rows before expert e, count[] their pairs; every thread of
-// the workgroup calls it, part[] is its scratch.
-__device__ inline int rows_before(const int *count, int e, int *part) {
-  const int t = threadIdx.x, lane = t & 63;
-  const int mine = t < e ? (count[t] + 15) & ~15 : 0;      // (kMaxExperts threads)
-  const int sum = (int)wave_reduce((uint32_t)mine, 0u, [](uint32_t x, uint32_t y) { return x + y; });
-  if (lane == 0) part[t >> 6] = sum;
-  __syncthreads();
-  int row = 0;
-#pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) row += part[w];
-  __syncthreads();
-  return row;
-}
 static_assert(kPlanThreads >= kMaxExperts, "a thread per expert");
 
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
-  __shared__ int count[kMaxExperts];
-  __shared__ int part[kPlanWaves];
-  const int t = threadIdx.x, e = blockIdx.x, lane = t & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  for (int i = t; i < a.E; i += kPlanThreads) count[i] = 0;
+// The rows of the experts before this thread's, of which `mine` are its own; last: of
+// all of them.  Every thread of the workgroup calls it; part[] is its scratch.
+__device__ inline int rows_before(int mine, int *part, int &last) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = lanes_upto(mine);
+  if (lane == 63) part[wave] = upto;
   __syncthreads();
-  int mine = 0;                                            // the lane's pairs of expert e
-  each_four(a, wave, lane, [&](int, int4 id) {
-    if ((unsigned)id.x < (unsigned)a.E) atomicAdd(&count[id.x], 1);
-    if ((unsigned)id.y < (unsigned)a.E) atomicAdd(&count[id.y], 1);
-    if ((unsigned)id.z < (unsigned)a.E) atomicAdd(&count[id.z], 1);
-    if ((unsigned)id.w < (unsigned)a.E) atomicAdd(&count[id.w], 1);
-    mine += (id.x == e) + (id.y == e) + (id.z == e) + (id.w == e);
-  });
-  mine = (int)wave_reduce((uint32_t)mine, 0u, [](uint32_t x, uint32_t y) { return x + y; });
-  __syncthreads();
-  const int row = rows_before(count, e, part);
-  const int n = count[e], end = row + ((n + 15) & ~15);
-  if (t == 0) a.first[e] = row;
-  if (row + n + t < end) a.pair[row + n + t] = -1;
-  if (e == a.E - 1) {                                      // and the rows behind the last expert's
-    if (t == 0) a.first[a.E] = end;
-    for (int64_t i = end + t; i < a.rows; i += kPlanThreads) a.pair[i] = -1;
+  last = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    upto += w < wave ? part[w] : 0;
+    last += part[w];
   }
-  if (lane == 0) part[wave] = mine;
+  return upto - mine;
+}
+
+__device__ inline int run_of(const PlanArgs &a, int parts) {
+  return (int)(((a.pairs + parts - 1) / parts + kPlanThreads - 1) / kPlanThreads) * kPlanThreads;
+}
+// The pairs of run b by expert into count[], which is zero.
+__device__ inline void count_run(const PlanArgs &a, int run, int b, int *count) {
+  const int64_t end = min(a.pairs, (int64_t)(b + 1) * run);
+  for (int64_t p = (int64_t)b * run + threadIdx.x; p < end; p += kPlanThreads) {
+    const int id = a.ids[p];
+    if ((unsigned)id < (unsigned)a.E) atomicAdd(&count[id], 1);
+  }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_count_kernel(PlanArgs a) {
+  __shared__ int count[kMaxExperts];
+  const int t = threadIdx.x, b = blockIdx.x;
+  count[t] = 0;
   __syncthreads();
-  int at = row;
-  for (int w = 0; w < wave; ++w) at += part[w];
-  if (mine == 0) return;
-  each_four(a, wave, lane, [&](int p, int4 id) {
-    if (__ballot(id.x == e || id.y == e || id.z == e || id.w == e) == 0) return;
-    const uint64_t m[4] = {__ballot(id.x == e), __ballot(id.y == e), __ballot(id.z == e),
-                           __ballot(id.w == e)};
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    int r = at, all = 0;
+  count_run(a, run_of(a, gridDim.x), b, count);
+  __syncthreads();
+  if (t < a.E) a.work[b * a.E + t] = count[t];
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_place_kernel(PlanArgs a) {
+  __shared__ int next[kMaxExperts];                        // the row of the run's next pair
+  __shared__ uint8_t in_wave[kPlanWaves][kMaxExperts];     // pairs of an expert in a wave
+  __shared__ int part[kPlanWaves];
+  const int t = threadIdx.x, lane = t & 63, b = blockIdx.x, parts = gridDim.x;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int run = run_of(a, parts);
+  int all = 0, before = 0;
+  if (parts == 1) {
+    next[t] = 0;
+    __syncthreads();
+    count_run(a, run, 0, next);
+    __syncthreads();
+    all = next[t];
+  } else if (t < a.E) {
+    constexpr int kAhead = 16;
+    for (int i0 = 0; i0 < parts; i0 += kAhead) {
+      int n[kAhead];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      r += __popcll(m[c] & below);
-      all += __popcll(m[c]);
+      for (int i = 0; i < kAhead; ++i) n[i] = i0 + i < parts ? a.work[(i0 + i) * a.E + t] : 0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        all += n[i];
+        before += i0 + i < b ? n[i] : 0;
+      }
     }
+  }
+  int last;
+  const int row = rows_before((all + 15) & ~15, part, last);
+  if (t < a.E && t % parts == b)                           // the rows that fill an expert's sixteen
+    for (int i = all; i & 15; ++i) a.pair[row + i] = -1;
+  if (b == 0 && t < a.E) a.first[t] = row;
+  if (b == 0 && t == 0) a.first[a.E] = last;
+  for (int64_t i = last + (int64_t)b * kPlanThreads + t; i < a.rows; i += (int64_t)parts * kPlanThreads)
+    a.pair[i] = -1;
+  next[t] = row + before;
+
+  for (int64_t p0 = (int64_t)b * run; p0 < min(a.pairs, (int64_t)(b + 1) * run); p0 += kPlanThreads) {
+    const int64_t p = p0 + t;
+    int id = p < a.pairs ? a.ids[p] : -1;
+    if ((unsigned)id >= (unsigned)a.E) id = kMaxExperts;   // (a group of its own)
+    for (int e = lane; e < a.E; e += 64) in_wave[wave][e] = 0;
+    // the lanes of the same expert, bit by bit of its number
+    uint64_t same = ~(uint64_t)0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (m[c] >> lane & 1) a.pair[r++] = p + c;
-    at += all;
-  });
+    for (int bit = 0; bit < 11; ++bit) {
+      const uint64_t set = __ballot(id >> bit & 1);
+      same &= id >> bit & 1 ? set : ~set;
+    }
+    const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+    if (rank == 0 && id < a.E) in_wave[wave][id] = (uint8_t)__popcll(same);
+    __syncthreads();
+    if (id < a.E) {
+      int at = next[id] + rank;
+      for (int w = 0; w < wave; ++w) at += in_wave[w][id];
+      a.pair[at] = (int)p;
+    }
+    __syncthreads();
+    if (t < a.E) {                                         // the next thousand's
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < kPlanWaves; ++w) n += in_wave[w][t];
+      next[t] += n;
+    }
+    __syncthreads();
+  }
 }
 
 // A few tokens: one workgroup chooses and plans, its pairs and rows in LDS.
@@ -369,22 +415,13 @@ __global__ __launch_bounds__(kPlanThreads) void route_few_kernel(RouteArgs a, Pl
   }
   __syncthreads();
   // an expert's first row: the sums over the experts, a thread to each
-  const int mine = t < a.E ? (count[t] + 15) & ~15 : 0;
-  int upto = mine;
-  upto += (int)dpp_or<kShr1, 0xF>((uint32_t)upto, 0u);
-  upto += (int)dpp_or<kShr2, 0xF>((uint32_t)upto, 0u);
-  upto += (int)dpp_or<kShr4, 0xF>((uint32_t)upto, 0u);
-  upto += (int)dpp_or<kShr8, 0xF>((uint32_t)upto, 0u);
-  upto += (int)dpp_or<kBcast15, 0xA>((uint32_t)upto, 0u);
-  upto += (int)dpp_or<kBcast31, 0xC>((uint32_t)upto, 0u);
-  if (lane == 63) part[wave] = upto;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) upto += part[w];
+  int last;
+  const int row = rows_before(t < a.E ? (count[t] + 15) & ~15 : 0, part, last);
   if (t < a.E) {
-    start[t] = upto - mine;
-    b.first[t] = upto - mine;
-    if (t == a.E - 1) b.first[a.E] = upto;
+    start[t] = row;
+    b.first[t] = row;
   }
+  if (t == 0) b.first[a.E] = last;
   __syncthreads();
   if (id >= 0) rows[start[id] + rank] = t;
   __syncthreads();
@@ -473,7 +510,12 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
 }  // namespace
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL(plan_kernel, dim3((unsigned)a.E), dim3(kPlanThreads), 0, s, a);
+  // A run of its own for every thousand pairs, beyond two thousand: a run's rounds take
+  // 2 us each (4000 pairs of 32 experts in one run 10.2 us, in four 4.8 and 2.2 to count).
+  const int64_t parts = std::min<int64_t>((a.pairs + kPlanThreads - 1) / kPlanThreads, kPlanParts);
+  const dim3 grid((unsigned)(parts <= 2 ? 1 : parts));
+  if (grid.x > 1) hipLaunchKernelGGL(plan_count_kernel, grid, dim3(kPlanThreads), 0, s, a);
+  hipLaunchKernelGGL(plan_place_kernel, grid, dim3(kPlanThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -187,6 +187,7 @@ hipError_t launch_rope(const RopeRowsArgs &args, hipStream_t s);
 
 // Experts (experts.hip).
 constexpr int kMaxExperts = 1024;
+constexpr int kPlanParts = MXQ_EXPERT_WORK;
 mxq_status check_experts(const mxq_experts *plan, Groups *g);   // (api_experts.cpp)
 struct RouteArgs {
   const void *logits;
@@ -202,7 +203,7 @@ struct PlanArgs {
   const int32_t *ids;
   int64_t pairs, rows;
   int E;
-  int32_t *first, *pair;
+  int32_t *first, *pair, *work;
 };
 struct CombineArgs {
   const void *y;

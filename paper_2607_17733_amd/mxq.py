@@ -57,7 +57,7 @@ class _AttnOpts(ctypes.Structure):
 class _Experts(ctypes.Structure):
     _fields_ = [("pairs", ctypes.c_int64), ("experts", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("first", ctypes.c_void_p),
-                ("pair", ctypes.c_void_p)]
+                ("pair", ctypes.c_void_p), ("work", ctypes.c_void_p)]
 
 
 class _RouteOpts(ctypes.Structure):
@@ -69,6 +69,7 @@ class _QkNorm(ctypes.Structure):
     _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
+EXPERT_WORK = 64
 _SCORES = {"softmax": 0, "sigmoid": 1}
 
 _lib = None
@@ -1038,25 +1039,30 @@ def _choices(t, dtype, what: str, dev, shape=None):
 class ExpertPlan:
     """Where the chosen token-expert pairs of a batch lie (include/mxq.h mxq_experts):
     `rows` rows of an operand image, expert e's from first[e] (int32 [experts + 1])
-    on, row r holding pair[r] (int32 [rows], -1: none).  The buffers are the
-    caller's, or new ones, which route or expert_plan fills; the sizes go by pairs
-    and experts alone, so a plan serves every batch of as many tokens."""
+    on, row r holding pair[r] (int32 [rows], -1: none).  The buffers are new ones,
+    with a scratch, which route or expert_plan fills; or the caller's, of a plan that
+    is made (first and pair, and work, int32 [EXPERT_WORK * experts], where it is to be
+    written again).  The sizes go by pairs and experts alone, so a plan serves every
+    batch of as many tokens."""
 
-    def __init__(self, pairs: int, experts: int, device="cuda", first=None, pair=None):
+    def __init__(self, pairs: int, experts: int, device="cuda", first=None, pair=None, work=None):
         self.pairs, self.experts = int(pairs), int(experts)
         self.rows = _size(lib().mxq_expert_rows(self.pairs, self.experts), "mxq_expert_rows")
         if first is None and pair is None:
-            # (one allocation; both 16-byte aligned)
+            # (one allocation; each part 16-byte aligned)
             at = self.experts + 4 & ~3
-            both = torch.empty(at + self.rows, dtype=torch.int32, device=device)
-            first, pair = both[:self.experts + 1], both[at:]
+            n = EXPERT_WORK * self.experts
+            whole = torch.empty(at + n + self.rows, dtype=torch.int32, device=device)
+            first, work, pair = whole[:self.experts + 1], whole[at:at + n], whole[at + n:]
         elif first is None or pair is None:
             raise MxqError("a plan takes first and pair, or neither")
         self.device = first.device if isinstance(first, torch.Tensor) else None
         f = _index(first, self.experts + 1, torch.int32, "first", self.device)
         p = _index(pair, self.rows, torch.int32, "pair", self.device)
-        self.first, self.pair = first, pair
-        self._c = _Experts(self.pairs, self.experts, 0, f, p)
+        w = None if work is None else _index(work, EXPERT_WORK * self.experts, torch.int32, "work",
+                                             self.device)
+        self.first, self.pair, self.work = first, pair, work
+        self._c = _Experts(self.pairs, self.experts, 0, f, p, w)
         self._ref = ctypes.byref(self._c)
 
 

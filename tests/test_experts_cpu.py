@@ -27,7 +27,7 @@ def ref(x):
 
 
 def plan(**kw):
-    c = dict(pairs=12, experts=4, reserved=0, first=FAKE, pair=FAKE)
+    c = dict(pairs=12, experts=4, reserved=0, first=FAKE, pair=FAKE, work=FAKE)
     c.update(kw)
     return mxq._Experts(*[c[n] for n, _ in mxq._Experts._fields_])
 
@@ -42,6 +42,7 @@ BAD_PLANS = [(dict(pairs=-1), SHAPE), (dict(pairs=2 ** 26 + 4), SHAPE), (dict(ex
              (dict(experts=-3), SHAPE), (dict(experts=1025), SHAPE), (dict(reserved=1), UNSUPPORTED),
              (dict(first=0), NULL), (dict(pair=0), NULL), (dict(first=FAKE + 8), ALIGN),
              (dict(pair=FAKE + 4), ALIGN)]
+BAD_WORK = [(dict(work=0), NULL), (dict(work=FAKE + 8), ALIGN)]        # of the calls that write a plan
 
 
 def test_rows(L):
@@ -60,7 +61,7 @@ def test_route_refusals(L):
     def call(o=None, p=None, logits=FAKE, f32=1, T=4, ld=4, ids=FAKE, w=FAKE, none=False):
         return L.mxq_route(None if none else ref(o or opts()), logits, f32, T, ld, ids, w, ref(p or plan()), None)
 
-    for kw, want in ([(dict(p=plan(**k)), w) for k, w in BAD_PLANS] +
+    for kw, want in ([(dict(p=plan(**k)), w) for k, w in BAD_PLANS + BAD_WORK] +
                      [(dict(none=True), NULL), (dict(logits=0), NULL), (dict(ids=0), NULL), (dict(w=0), NULL),
                       (dict(o=opts(k=0), p=plan(pairs=0)), SHAPE), (dict(o=opts(k=5), p=plan(pairs=20)), SHAPE),
                       (dict(o=opts(k=33), p=plan(pairs=132, experts=100), ld=100), SHAPE),
@@ -74,7 +75,7 @@ def test_route_refusals(L):
 
 
 def test_plan_refusals(L):
-    for k, want in BAD_PLANS:
+    for k, want in BAD_PLANS + BAD_WORK:
         assert L.mxq_expert_plan(FAKE, ref(plan(**k)), None) == want, k
     assert L.mxq_expert_plan(FAKE, None, None) == NULL
     assert L.mxq_expert_plan(0, ref(plan()), None) == NULL

@@ -765,9 +765,9 @@ mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts
  *   y             DEVICE [pairs][ldy], float32 or (y_f32 == 0) bf16 (the float32 sum
  *                 rounded to nearest even), ldy >= N, 16-byte aligned.
  * A row's result does not depend on the other rows of its call; which kernel runs
- * goes by pairs and E, as for mxq_gemm, and the kernels differ in the order of
- * their float32 sums.
- * Errors: as mxq_gemm, and the plan's.
+ * goes by pairs, E and N, and the kernels differ in the order of their float32 sums.
+ * Errors: as mxq_gemm, and the plan's; MXQ_ERR_SHAPE also for more tiles (of 32 or
+ * more rows, 128 columns) than a dispatch's 2^24 workgroups.
  */
 mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t N,
                             const uint8_t *a_mant, const uint8_t *a_exp, const uint8_t *w_mant,

@@ -152,14 +152,13 @@ mxq_status mxq_gemm_experts(const mxq_fmt *fmt, const mxq_experts *plan, int64_t
   if (st != MXQ_OK) return st;
   if (x.pairs == 0 || N == 0) return MXQ_OK;
   if (ldy < N || N > INT32_MAX) return MXQ_ERR_SHAPE;
-  // (every kernel has fewer workgroups than one of 256 threads per 16 rows and 32 columns)
-  if ((x.rows / 16 + x.E) * ((N + 31) / 32) >= 1 << 23) return MXQ_ERR_SHAPE;
   g.x = x;
   g.w_expert = mxq_weight_bytes(fmt, N);
   g.w_expert_sc = mxq_weight_exp_bytes(fmt, N);
   g.y = (float *)y;
   g.y_bf16 = !y_f32;
   g.ldy = ldy;
+  if (mxq::gemm_experts_workgroups(g) > kMaxGrid) return MXQ_ERR_SHAPE;
   return launched(mxq::launch_gemm_experts(g, (hipStream_t)stream));
 }
 

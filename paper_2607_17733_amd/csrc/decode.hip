@@ -31,7 +31,6 @@
 #include <atomic>
 #include <type_traits>
 
-#include "experts_device.h"
 #include "mxq_device.h"
 #include "mxq_internal.h"
 
@@ -101,8 +100,7 @@ __device__ inline uint32_t lo_codes(uint32_t w) {
 // consecutive slabs; with 2 or 4 it lies inside one 128-column super-slab,
 // with 5 to 7 (one unit per CU where that balances the CUs) it may cross
 // into the next super-slab.
-// BY: the rows of experts (GemmArgs::x): blockIdx.y is the tile of 16 T rows.
-template <bool FULL, int T, int SL, bool BY = false>
+template <bool FULL, int T, int SL>
 __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g) {
   __shared__ v4f red[kMaxWaves][SL][64];
   const int t = threadIdx.x, lane = t & 63;
@@ -133,20 +131,6 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g)
   // slab sl lies in super-slab ss + 1 when n0 + sl >= 8 (at most one
   // crossing); cross: some live slab of the unit does
   const bool cross = !ALIGNED && n0 + SL > kWSlabs && (ss + 1) * kWCols < g.N;
-  const int32_t *pair = nullptr;
-  if (BY) {
-    constexpr int LG = T == 1 ? 4 : T == 2 ? 5 : 6;
-    const ExpertTile x = expert_tile<LG>(g.x, blockIdx.y);
-    if (x.rows <= 0) return;
-    g.M = x.rows;
-    pair = g.x.pair + x.row0;
-    g.a_mant += (int64_t)(x.row0 >> 4) * g.a_tile;
-    g.a_exp += (int64_t)(x.row0 >> 4) * g.a_tile_sc;
-    g.w_mant += x.e * g.w_expert;
-    g.w_exp += x.e * g.w_expert_sc;
-  }
-  // (a tile past the expert's rows reads its first one)
-  auto tile = [&](int t) { return BY && 16 * t >= g.M ? 0 : t; };
   const uint8_t *wsup = g.w_mant + ss * g.w_super;
   const uint8_t *wsc = g.w_exp + ss * g.w_super_sc + 32 * lane;
   const uint8_t *wsc2 = cross ? wsc + g.w_super_sc : wsc;
@@ -154,10 +138,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g)
   // live lane, so no extra traffic); their output rows are discarded.
   int alane[T];
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const bool in = BY ? pair[16 * tile(t) + line] >= 0 : 16 * t + line < g.M;
-    alane[t] = in ? lane : (lane & ~15);
-  }
+  for (int t = 0; t < T; ++t) alane[t] = 16 * t + line < g.M ? lane : (lane & ~15);
   v4f acc[T][SL];
 #pragma unroll
   for (int t = 0; t < T; ++t)
@@ -195,7 +176,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g)
     uint32_t sa[T];
 #pragma unroll
     for (int t = 0; t < T; ++t)
-      sa[t] = *(const uint32_t *)(g.a_exp + tile(t) * g.a_tile_sc + (int64_t)gi * 256 + 4 * alane[t]);
+      sa[t] = *(const uint32_t *)(g.a_exp + t * g.a_tile_sc + (int64_t)gi * 256 + 4 * alane[t]);
     const uint8_t *wseg = wsup + w_seg_base<SEG, FULL>(lg) + (int64_t)(4 * gl) * kWSlabs * CB +
                           (int64_t)n0 * CB;
     const uint8_t *aseg = g.a_mant + a_seg_base<SEG>(lg) +
@@ -212,7 +193,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g)
       const uint8_t *w0 = wseg + (int64_t)k * kWSlabs * CB;
 #pragma unroll
       for (int t = 0; t < T; ++t) {
-        const uint8_t *ap = aseg + tile(t) * g.a_tile + (int64_t)k * kLanes * a_lane_bytes(SEG) +
+        const uint8_t *ap = aseg + t * g.a_tile + (int64_t)k * kLanes * a_lane_bytes(SEG) +
                             (int64_t)a_lane_bytes(SEG) * alane[t];
         if (SEG == 3) {
           r.a0[t] = *(const u4 *)ap;
@@ -364,15 +345,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void gemm_decode_kernel(GemmArgs g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = 16 * t + 4 * grp + i;
-        if (row >= g.M || col >= g.N) continue;
-        if (BY) {
-          const int p = pair[row];
-          if (p < 0 || p >= g.x.pairs) continue;
-          if (g.y_bf16) ((__bf16 *)g.y)[p * g.ldy + col] = (__bf16)y[i];
-          else g.y[p * g.ldy + col] = y[i];
-        } else {
-          g.y[row * g.ldy + col] = y[i];
-        }
+        if (row < g.M && col < g.N) g.y[row * g.ldy + col] = y[i];
       }
     }
   }
@@ -411,13 +384,6 @@ int device_cu_count() {
     return 256;
   if (keep) known[dev].store(n, std::memory_order_relaxed);
   return n;
-}
-
-hipError_t launch_experts_decode(const GemmArgs &a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)(a.x.rows / 16));
-  const auto fn = a.full ? gemm_decode_kernel<true, 1, 2, true> : gemm_decode_kernel<false, 1, 2, true>;
-  hipLaunchKernelGGL(fn, grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
 }
 
 hipError_t launch_gemm_decode(const GemmArgs &a, hipStream_t stream) {

@@ -170,21 +170,13 @@ __device__ inline uint32_t lo_codes(uint32_t w) {
   return FULL ? (w & 0x0F0F0F0Fu) : (w & 0x8F8F8F8Fu);
 }
 
-// The tile of workgroup `pid` of rows by experts: XCD x takes the column tiles x,
-// x + 8, ... of four row tiles after the other, so that the row tiles of an expert
-// that run at one time share its weights in an L2, and workgroups behind the last
-// expert's rows come last.  nt may pass the last column tile.
-__device__ inline void expert_order(int pid, int ntiles, int &mt, int &nt) {
-  const int loc = pid >> 3, per = (ntiles + 7) >> 3, q = loc / (4 * per);
-  mt = 4 * q + (loc & 3);
-  nt = (pid & 7) + 8 * ((loc - q * 4 * per) >> 2);
-}
-
 // The arguments of one expert's tile of 2^LG rows; false: there is none.
 template <int LG>
-__device__ inline bool take_expert(GemmArgs &g, int mt, const int32_t *&pair) {
-  const ExpertTile x = expert_tile<LG>(g.x, mt);
+__device__ inline bool take_expert(GemmArgs &g, int ntiles, int near, const int32_t *&pair,
+                                   int &nt) {
+  const ExpertTile x = expert_tile<LG>(g.x, blockIdx.x, ntiles, near);
   if (x.rows <= 0) return false;
+  nt = x.nt;
   g.M = x.rows;
   pair = g.x.pair + x.row0;
   g.a_mant += (int64_t)(x.row0 >> 4) * g.a_tile;
@@ -232,14 +224,15 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
   const int t = threadIdx.x, lane = t & 63;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6);      // wave-uniform
   const int l32 = lane & 31, lh = lane >> 5, l16 = lane & 15, hx = l32 >> 4;
-  int mt, nt;
-  {
+  int mt = 0, nt;
+  const int32_t *pair = nullptr;
+  if (BY) {
+    if (!take_expert<(TM == 1 ? 7 : 8)>(g, ntiles, gm, pair, nt)) return;
+  } else {
     // XCD x (workgroups pid % 8 == x) owns a block of (mtiles / gm) x
     // (ntiles / gn) tiles, walked row by row.
     const int pid = blockIdx.x;
-    if (BY) {
-      expert_order(pid, ntiles, mt, nt);
-    } else if (gm > 0) {
+    if (gm > 0) {
       const int x = pid & 7, loc = pid >> 3;
       const int bm = mtiles / gm, bn = ntiles / gn;
       mt = (x / gn) * bm + loc / bn;
@@ -249,9 +242,7 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
       nt = pid - mt * ntiles;
     }
   }
-  const int32_t *pair = nullptr;
-  if (BY && (nt >= ntiles || !take_expert<(TM == 1 ? 7 : 8)>(g, mt, pair))) return;
-  const int64_t row0 = BY ? 0 : (int64_t)mt * BM, col0 = (int64_t)nt * BN;
+  const int64_t row0 = (int64_t)mt * BM, col0 = (int64_t)nt * BN;
   const LGeo lg(g.n3, g.n4, g.n6, g.n8);
   const int nsteps = lg.nsteps;
   char *const ring = (char *)lds;
@@ -674,12 +665,13 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
   const int l32 = lane & 31, lh = lane >> 5, l16 = lane & 15, hx = l32 >> 4;
   // XCD x owns the column tiles nt with nt / nx == x (nx > 0), all row tiles
   // of each, so that its L2 holds their weights; else in order.
-  int mt, nt;
-  {
+  int mt = 0, nt;
+  const int32_t *pair = nullptr;
+  if (BY) {
+    if (!take_expert<(TM == 1 ? 5 : 6)>(g, ntiles, nx, pair, nt)) return;
+  } else {
     const int pid = blockIdx.x;
-    if (BY) {
-      expert_order(pid, ntiles, mt, nt);
-    } else if (nx > 0) {
+    if (nx > 0) {
       const int loc = pid >> 3;
       nt = (pid & 7) * nx + loc / mtiles;
       mt = loc % mtiles;
@@ -688,9 +680,7 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
       mt = pid - nt * mtiles;
     }
   }
-  const int32_t *pair = nullptr;
-  if (BY && (nt >= ntiles || !take_expert<(TM == 1 ? 5 : 6)>(g, mt, pair))) return;
-  const int64_t row0 = BY ? 0 : (int64_t)mt * 32 * TM, col0 = (int64_t)nt * BN;
+  const int64_t row0 = (int64_t)mt * 32 * TM, col0 = (int64_t)nt * BN;
   const LGeo lg(g.n3, g.n4, g.n6, g.n8);
 
   const int64_t last = (g.M - 1) / kATileRows, ta = row0 / kATileRows;
@@ -1098,32 +1088,70 @@ hipError_t launch_gemm_prefill(const GemmArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Rows by experts: tiles of 2^lg rows of every expert, as many as any choice has.
-static int64_t expert_tiles(const GemmArgs &a, int lg) {
-  const int64_t active = std::min<int64_t>(a.x.E, a.x.pairs);
-  return active + ((a.x.rows - 16 * active) >> lg);
+// Rows by experts.  The launch is sized by the pairs and the experts alone; a mean
+// group is the pairs over the experts that they can reach.  us of the kernels that split
+// K in four, in two (both 32-row tiles, the tiled one 128), tokens x experts x choices,
+// K, N, 4-6-8 maps:
+//   up to 16 rows, or up to two tiles of 32 rows per CU: four shares:
+//     1 x 64 x 6, 2048, 2816 8.6, 9.5; 64 x 128 x 8, 2048, 1536 48, 53; 8 x 8 x 2,
+//     4096, 28672 88, 99; 48 x 16 x 4, 1408, 2048 9.8, 10.4; 100 x 2 x 1, 8192, 8192
+//     17.5, 22.6 (but 16 x 64 x 6, 2048, 2816 35, 33)
+//   more: two: 333 x 8 x 2, 4096, 4000 28, 27; 1000 x 32 x 4, 2048, 3584 92, 83; 2000 x
+//     8 x 2, 1024, 2048 32, 27 (tiled 30)
+//   from 48 rows and 3 1/4 tiles of 128 rows per CU on: tiled: 4096 x 8 x 2, 4096, 28672
+//     1556 (2138; tiles of 256 rows, one per CU, 1650), 1000 x 32 x 4, 2048, 3584 76
+//     (83), 2048 x 64 x 6, 1408, 2048 71 (76), 512 x 32 x 4, 2048, 3584 53 (59); 800 x 8
+//     x 2, 4096, 4096, with two per CU, 51.3 (50.7)
+// The full clamp's 12 KB weight stages leave a CU one tiled workgroup, so that two shares
+// of 64 rows take its place: 2048 x 8 x 2, 4096, 14336 480 (tiled 593, of 256 rows 537).
+// A kernel that streams weights for 16-row tiles, as for single linears, took 51 for 64 x
+// 128 x 8 and 94 for 8 x 8 x 2.
+struct ExpertLaunch {
+  enum { kSplit4, kSplit2, kSplit2x64, kTiled } kernel;
+  int near;                // row tiles to a column tile that run together
+  int64_t groups;          // workgroups
+};
+static ExpertLaunch expert_launch(const GemmArgs &a) {
+  const int64_t cus = device_cu_count(), nt = (a.N + BN - 1) / BN;
+  const int64_t active = std::min<int64_t>(a.x.E, a.x.pairs), mean = a.x.pairs / active;
+  // tiles of 2^lg rows: about as many, and as many as any choice needs
+  auto about = [&](int lg) { return (a.x.pairs >> lg) + active / 2; };
+  auto tiles = [&](int lg) { return active + ((a.x.rows - 16 * active) >> lg); };
+  ExpertLaunch l{ExpertLaunch::kSplit2, 1, 0};
+  int lg = 5;
+  if (mean >= 48 && 4 * about(7) * nt >= 13 * cus) {
+    l.kernel = a.full ? ExpertLaunch::kSplit2x64 : ExpertLaunch::kTiled;
+    l.near = 4;
+    lg = a.full ? 6 : 7;
+  } else if (mean <= 16 || (about(5) + active / 2) * nt <= 2 * cus) {
+    l.kernel = ExpertLaunch::kSplit4;
+  }
+  // (whole groups of `near` row tiles, as many for every XCD)
+  l.groups = ((tiles(lg) + l.near - 1) / l.near * nt + 7) / 8 * 8 * l.near;
+  return l;
 }
+
+int64_t gemm_experts_workgroups(const GemmArgs &a) { return expert_launch(a).groups; }
 
 template <bool FULL>
 static hipError_t go_experts(const GemmArgs &a, hipStream_t stream) {
+  const ExpertLaunch l = expert_launch(a);
   const int ntiles = (int)((a.N + BN - 1) / BN);
-  auto grid = [&](int lg) {
-    return dim3((unsigned)((expert_tiles(a, lg) + 3) / 4 * 4 * ((ntiles + 7) / 8 * 8)));
+  const dim3 grid((unsigned)l.groups);
+  auto split = [&](auto kg, auto tm) {
+    constexpr int KG = decltype(kg)::value, TM = decltype(tm)::value;
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, KG, TM, false, true>), grid, dim3(64 * KG), 0, stream, a,
+                       0, ntiles, l.near);
   };
-  const int64_t mean = a.x.pairs / std::min<int64_t>(a.x.E, a.x.pairs);
-  if (mean <= 16) return launch_experts_decode(a, stream);
-  if (mean <= 32)
-    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 1, false, true>), grid(5), dim3(256), 0, stream, a, 0,
-                       ntiles, 0);
-  else if (mean <= 96)
-    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 2, false, true>), grid(6), dim3(256), 0, stream, a, 0,
-                       ntiles, 0);
-  else if (mean <= 256 && !FULL)
-    hipLaunchKernelGGL((gemm_prefill_kernel<FULL, 1, true>), grid(7), dim3(NT), 0, stream, a, 0, ntiles,
-                       0, 0);
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I4 = std::integral_constant<int, 4>;
+  if (l.kernel == ExpertLaunch::kSplit4) split(I4{}, I1{});
+  else if (l.kernel == ExpertLaunch::kSplit2) split(I2{}, I1{});
+  else if constexpr (FULL) split(I2{}, I2{});
   else
-    hipLaunchKernelGGL((gemm_prefill_kernel<FULL, 2, true>), grid(8), dim3(NT), 0, stream, a, 0, ntiles,
-                       0, 0);
+    hipLaunchKernelGGL((gemm_prefill_kernel<false, 1, true>), grid, dim3(NT), 0, stream, a, 0, ntiles,
+                       l.near, 0);
   return hipGetLastError();
 }
 

@@ -218,9 +218,9 @@ struct CombineArgs {
 hipError_t launch_expert_plan(const PlanArgs &args, hipStream_t s);
 hipError_t launch_route(const RouteArgs &args, const PlanArgs &plan, hipStream_t s);
 hipError_t launch_combine(const CombineArgs &args, hipStream_t s);
-// The products of every expert's rows (decode.hip, gemm_prefill.hip).
+// The products of every expert's rows, and their workgroups (gemm_prefill.hip).
 hipError_t launch_gemm_experts(const GemmArgs &args, hipStream_t s);
-hipError_t launch_experts_decode(const GemmArgs &args, hipStream_t s);
+int64_t gemm_experts_workgroups(const GemmArgs &args);
 
 // Norms of queries and keys with their rotation (rope.hip).
 struct NormArgs {

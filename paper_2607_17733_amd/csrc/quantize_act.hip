@@ -678,16 +678,18 @@ __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) 
   for (int64_t grp = w0; grp < groups; grp += nwg) {
     const int64_t r0 = grp << lgR;
     if (BY) {
-      // rows behind the last expert's are nobody's
-      if (r0 >= q.x.first[q.x.E]) break;
-      for (int lr = t; lr < R; lr += nthr) {
-        const int p = r0 + lr < q.out_rows ? q.x.pair[r0 + lr] : -1;
-        from[lr] = p < 0 || p >= q.x.pairs ? -1 : (int)((uint32_t)p / q.per_row);
-      }
-      // (a group's rows are one expert's: at most 16, and its first row a multiple of them)
+      // (at most 64 rows, a thread to each; the loads are in flight together)
+      int p = -1;
+      if (t < R && r0 + t < q.out_rows) p = q.x.pair[r0 + t];
+      // (with a permutation for each expert a group's rows are one expert's: at most 16,
+      // the first a multiple of them)
+      int mine = -1;
       if (q.perms)
         for (int e = t; e < q.x.E; e += nthr)
-          if (q.x.first[e] <= r0 && r0 < q.x.first[e + 1]) from[R] = e;
+          if (q.x.first[e] <= r0 && r0 < q.x.first[e + 1]) mine = e;
+      if (r0 >= q.x.first[q.x.E]) break;                   // rows behind the last expert's
+      if (t < R) from[t] = p < 0 || p >= q.x.pairs ? -1 : (int)((uint32_t)p / q.per_row);
+      if (mine >= 0) from[R] = mine;
       __syncthreads();
       if (q.perms) {
         const int e = (int)min((unsigned)__builtin_amdgcn_readfirstlane(from[R]), (unsigned)q.x.E - 1);
@@ -917,10 +919,15 @@ static RowGroups row_groups(const QuantArgs &a, int cus) {
   constexpr int kMaxWaves = kMaxThreads / 64;
   auto one = [&](int lg) { return RowGroups{lg, 64 * std::min(waves(lg), kMaxWaves), 1}; };
   for (int lg = 0; lg <= most && fits(lg, 1) && waves(lg) <= 2 * kMaxWaves; ++lg)
-    if (((a.out_rows - 1) >> lg) + 1 <= cus) return one(lg);
+    if (!(a.x.E && a.swiglu && lg > 3) && ((a.out_rows - 1) >> lg) + 1 <= cus) return one(lg);
   int lg = 0;
   while (lg < most && fits(lg + 1, 2) && waves(lg + 1) <= kMaxWaves + 2) ++lg;
   if (!fits(lg, 2)) return one(0);
+  // Rows by experts, of which an image has more than pairs: groups for both of every CU
+  // come first (4000 rows of 1792 with SiLU * up, 8 rows each 17.8 us, 16 23.0, 32, one
+  // workgroup per CU, 22.2; 12288 of 1408, 16 rows 36)
+  if (a.x.E && a.swiglu)
+    while (lg > 0 && ((a.out_rows - 1) >> lg) + 1 < 2 * cus) --lg;
   // SiLU * up of long rows: its tables and arithmetic outweigh the overlap
   // (K = 14336, M = 4096: 4 rows and 1024 threads, one per CU, 82 us, 2 rows
   // and 512 threads, two per CU, 86 us)
@@ -970,10 +977,12 @@ hipError_t launch_quantize_act(const QuantArgs &args, hipStream_t stream) {
   const RowGroups rg = row_groups(a, cus);
   a.lg_rows = rg.lg;
   const int64_t groups = ((a.out_rows - 1) >> rg.lg) + 1;
-  // the silu table pays from six times its own size in elements
+  // the silu table pays from six times its own size in elements; by experts, whose rows are
+  // short, from twice (gates of size 1: 4000 rows of 1792 17.2, without it 17.5 us, 12288 of
+  // 1408 33.7, 35.6; of size 8, near more rounding borders, 17.3, 23.7 and 33.5, 48.1)
   const int64_t grid = a.swiglu ? std::min<int64_t>(groups, (int64_t)rg.per_cu * cus) : groups;
   int64_t lds = ((row_lds(a.K, a.rmsnorm != 0) << rg.lg) + 15) & ~15;
-  a.silu_table = a.swiglu && a.vec16 && ((groups / grid * a.K) << rg.lg) >= 6 * kSiluN &&
+  a.silu_table = a.swiglu && a.vec16 && ((groups / grid * a.K) << rg.lg) >= (a.x.E ? 2 : 6) * kSiluN &&
                  lds + 2 * kSiluN + (a.x.E ? kGroupLds : 0) <= kMaxLds;
   if (a.silu_table) lds += 2 * kSiluN;
   if (a.x.E) lds += kGroupLds;

@@ -135,24 +135,28 @@ __global__ __launch_bounds__(kThreads) void rope_qk_any_kernel(RopeQkArgs a, int
                      : a.q_out + t * a.qo_ts + h * a.qo_hs;
   const uint16_t *gain = is_k ? a.norm.k_gain : a.norm.q_gain;
   const int D = (int)a.D, rot = a.rope.rot, half = rot / 2;
-  double s = 0.0;
-  for (int c = 8 * lane; c < D; c += 512)
-    for (int d = c; d < min(c + 8, D); ++d) {
-      const double v = (double)bf16_to_f32(x[d]);
-      s = fma(v, v, s);
-    }
-  const double r = norm_factor(sum_lanes(s, 64), (double)D, a.norm.eps);
+  const HeadNorm r = head_norm(
+      [&](auto s) {
+        for (int c = 8 * lane; c < D; c += 512)
+          for (int d = c; d < min(c + 8, D); ++d) {
+            const decltype(s) v = bf16_to_f32(x[d]);
+            s = fma(v, v, s);
+          }
+        return s;
+      },
+      64, D, a.norm.eps);
+  auto value = [&](int d) { return normalised1(bf16_to_f32(x[d]), r, bf16_to_f32(gain[d])); };
   const int p = a.pos[t];
   const bool out = p < 0 || p >= a.rope.positions;
   const float *row = a.rope.table + (int64_t)(out ? 0 : p) * rot;
   for (int e = lane; e < half + (D - rot); e += 64) {
     if (e >= half) {
       const int d = rot + e - half;
-      y[d] = (uint16_t)f32_to_bf16(normalised1(x[d], r, gain[d]));
+      y[d] = (uint16_t)f32_to_bf16(value(d));
       continue;
     }
     const int i = a.rope.pairs ? 2 * e : e, j = a.rope.pairs ? 2 * e + 1 : e + half;
-    const float u = normalised1(x[i], r, gain[i]), v = normalised1(x[j], r, gain[j]);
+    const float u = value(i), v = value(j);
     y[i] = out ? 0xFFFF : (uint16_t)f32_to_bf16(rotated(u, v, row[2 * e], row[2 * e + 1], false));
     y[j] = out ? 0xFFFF : (uint16_t)f32_to_bf16(rotated(v, u, row[2 * e], row[2 * e + 1], true));
   }

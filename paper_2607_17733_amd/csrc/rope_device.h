@@ -52,21 +52,9 @@ __device__ inline rope_u4 rotate_pairs8(rope_u4 x, const rope_f4 (&cs)[4]) {
   return y;
 }
 
-// Eight values of a head, normalised: float32(float32(x r) gain), r in float64.
 struct rope_f8 {
   float v[8];
 };
-__device__ inline rope_f8 normalised8(rope_u4 x, double r, rope_u4 gain) {
-#pragma clang fp contract(off)
-  rope_f8 y;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y.v[2 * i] = (float)((double)bf16_to_f32(x[i]) * r) * bf16_to_f32(gain[i]);
-    y.v[2 * i + 1] = (float)((double)__uint_as_float(x[i] & 0xFFFF0000u) * r) *
-                     __uint_as_float(gain[i] & 0xFFFF0000u);
-  }
-  return y;
-}
 __device__ inline rope_u4 to_bf16x8(const rope_f8 &x) {
   rope_u4 y;
 #pragma unroll
@@ -92,30 +80,61 @@ __device__ inline rope_f8 rotate_pairs8(const rope_f8 &x, const rope_f4 (&cs)[4]
   }
   return y;
 }
-// The sum of eight squares in float64, and 1 / sqrt(sum / D + eps); a head of zeros
-// has no direction, and stays zero.
-__device__ inline double squares8(rope_u4 x) {
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const double a = (double)bf16_to_f32(x[i]), b = (double)__uint_as_float(x[i] & 0xFFFF0000u);
-    s = fma(a, a, s);
-    s = fma(b, b, s);
-  }
-  return s;
+// The sum over the n lanes of a head (a power of two), the same in each.
+template <int CTRL>
+__device__ inline float lane_dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF,
+                                                            0xF, false));
 }
-__device__ inline double norm_factor(double squares, double D, float eps) {
-  const double m = squares / D + (double)eps;
-  return m == 0.0 ? 0.0 : 1.0 / sqrt(m);
+__device__ inline float sum_lanes(float v, int n) {
+  if (n > 1) v += lane_dpp<0xB1>(v);                       // the other of two,
+  if (n > 2) v += lane_dpp<0x4E>(v);                       // the other two of four,
+  if (n > 4) v += lane_dpp<0x141>(v);                      // four of eight,
+  if (n > 8) v += lane_dpp<0x140>(v);                      // eight of sixteen
+  if (n > 16) v += __shfl_xor(v, 16);
+  if (n > 32) v += __shfl_xor(v, 32);
+  return v;
 }
-// Over the n lanes of a head (a power of two), the same in each.
 __device__ inline double sum_lanes(double v, int n) {
   for (int i = 1; i < n; i *= 2) v += __shfl_xor(v, i);
   return v;
 }
 
-__device__ inline float normalised1(uint32_t x, double r, uint32_t gain) {
-  return (float)((double)bf16_to_f32(x) * r) * bf16_to_f32(gain);
+// 1 / sqrt(mean of the squares + eps) of a head, from the squares that each of its n
+// lanes has added up; f(T) adds the lane's own in T.  In float32 where the sum is far
+// from its limits (float64 for all heads made the arithmetic the bound: 4001 tokens of
+// 48 heads 24 -> 22 us), else in float64: a head of zeros has no direction, and stays
+// zero.
+struct HeadNorm {
+  float r;
+  double wide;             // in r's place where it is not 0
+};
+template <typename F>
+__device__ inline HeadNorm head_norm(F f, int n, int D, float eps) {
+  const float s = sum_lanes(f(0.f), n);
+  HeadNorm h = {0.f, 0.0};
+  if (s > 0x1p-80f && s < 0x1p120f) {
+    h.r = __builtin_amdgcn_rsqf(fmaf(s, 1.f / (float)D, eps));
+  } else {                                                 // (all lanes of the head)
+    const double m = sum_lanes(f(0.0), n) / (double)D + (double)eps;
+    h.wide = m == 0.0 ? 0.0 : 1.0 / sqrt(m);
+  }
+  return h;
+}
+// float32(float32(x r) gain).
+__device__ inline float normalised1(float x, const HeadNorm &h, float gain) {
+#pragma clang fp contract(off)
+  return (h.wide == 0.0 ? x * h.r : (float)((double)x * h.wide)) * gain;
+}
+__device__ inline rope_f8 normalised8(rope_u4 x, const HeadNorm &h, rope_u4 gain) {
+  rope_f8 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y.v[2 * i] = normalised1(bf16_to_f32(x[i]), h, bf16_to_f32(gain[i]));
+    y.v[2 * i + 1] = normalised1(__uint_as_float(x[i] & 0xFFFF0000u), h,
+                                 __uint_as_float(gain[i] & 0xFFFF0000u));
+  }
+  return y;
 }
 
 // Values d0 .. d0 + 7 of a head of D values at x, normalised and rotated, in one of the
@@ -147,7 +166,17 @@ __device__ inline rope_u4 load_normalised_rotated(const RopeArgs &rope, int p, c
       pg = *(const rope_u4 *)(gain + partner);
     }
   }
-  const double r = norm_factor(sum_lanes(squares8(u), n), (double)D, eps);
+  const HeadNorm r = head_norm(
+      [&](auto s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const decltype(s) a = bf16_to_f32(u[i]), b = __uint_as_float(u[i] & 0xFFFF0000u);
+          s = fma(a, a, s);
+          s = fma(b, b, s);
+        }
+        return s;
+      },
+      n, D, eps);
   const rope_f8 v = normalised8(u, r, g);
   if (!turns) return to_bf16x8(v);
   if (out) return rope_u4{~0u, ~0u, ~0u, ~0u};

@@ -805,37 +805,39 @@ def rope_qk(q, k, pos, table, q_gain, k_gain, eps: float, interleaved: bool = Fa
     some = q if q is not None else k
     if some is None:
         raise MxqError("rope_qk needs q or k")
-    T, _, D = _heads(some, "q or k")
+    T, H, D = _heads(some, "k" if q is None else "q")
     dev = some.device
     stream = _current(dev, "q or k")
-    q_out, qs = _norm_side(q, q_gain, q_out, "q", T, D, dev)
-    k_out, ks = _norm_side(k, k_gain, k_out, "k", T, D, dev)
-    norm = _QkNorm(qs[0], ks[0], eps)
-    status = lib().mxq_rope_qk(_rotary(table, dev, interleaved), ctypes.byref(norm),
-                               _index(pos, T, torch.int32, "pos", dev), T, D, *qs[1:], *ks[1:],
+    q_gain, q_out, q_args = _norm_side(q, H, q_gain, q_out, "q", T, D, dev)
+    k_gain, k_out, k_args = _norm_side(k, H if q is None else None, k_gain, k_out, "k", T, D, dev)
+    status = lib().mxq_rope_qk(_rotary(table, dev, interleaved),
+                               ctypes.byref(_QkNorm(q_gain, k_gain, eps)),
+                               _index(pos, T, torch.int32, "pos", dev), T, D, *q_args, *k_args,
                                stream)
     if status:
         _check(status, "mxq_rope_qk")
     return q_out, k_out
 
 
-def _norm_side(x, gain, out, what: str, T: int, D: int, dev):
-    """The result and the arguments of rope_qk's queries or keys."""
+def _norm_side(x, H, gain, out, what: str, T: int, D: int, dev):
+    """The gain, the result and the arguments of rope_qk's queries or keys (of H heads
+    of checked rows, or None)."""
     if x is None:
         if out is not None:
             raise MxqError("%s_out needs %s" % (what, what))
-        return None, (None, None, 0, 0, 0, None, 0, 0)
-    Tx, H, _ = _heads(x, what, dev, None, D)
-    if Tx != T:
-        raise MxqError("q and k have %d and %d tokens" % (T, Tx))
+        return None, None, (None, 0, 0, 0, None, 0, 0)
+    if H is None:
+        Tx, H, _ = _heads(x, what, dev, None, D)
+        if Tx != T:
+            raise MxqError("q and k have %d and %d tokens" % (T, Tx))
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=dev)
     elif out is not x and _heads(out, what + "_out", dev, H, D)[0] != T:
         raise MxqError("%s_out is %s, not %s" % (what, tuple(out.shape), tuple(x.shape)))
-    at, hs, _ = x.stride()
-    oat, ohs, _ = out.stride()
-    return out, (_index(gain, D, torch.bfloat16, what + "_gain", dev), x.data_ptr(), H, at, hs,
-                 out.data_ptr(), oat, ohs)
+    ts, hs, _ = x.stride()
+    ots, ohs, _ = out.stride()
+    return _index(gain, D, torch.bfloat16, what + "_gain", dev), out, (
+        x.data_ptr(), H, ts, hs, out.data_ptr(), ots, ohs)
 
 
 class PagedCache:
@@ -1036,6 +1038,27 @@ def _choices(t, dtype, what: str, dev, shape=None):
     return t.shape
 
 
+def _bytes(t, n: int, what: str, dev):
+    """The address of a contiguous uint8 tensor of at least n bytes on the device dev."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.uint8 and t.device == dev
+            and t.is_contiguous() and t.numel() >= n):
+        _dev_bytes(t, n, what, dev)
+    return t.data_ptr()
+
+
+def _image(out, fmt: Format, rows: int, dev):
+    """The buffers of an image of `rows` rows (a multiple of 16), the caller's or new
+    ones, and their addresses."""
+    unit = fmt._units()
+    if out is None:
+        mant = torch.empty((rows >> 4) * unit[0], dtype=torch.uint8, device=dev)
+        exp = torch.empty((rows >> 4) * unit[1], dtype=torch.uint8, device=dev)
+        return (mant, exp), mant.data_ptr(), exp.data_ptr()
+    mant, exp = out
+    return out, _bytes(mant, (rows >> 4) * unit[0], "activation mantissa buffer", dev), _bytes(
+        exp, (rows >> 4) * unit[1], "activation exponent buffer", dev)
+
+
 class ExpertPlan:
     """Where the chosen token-expert pairs of a batch lie (include/mxq.h mxq_experts):
     `rows` rows of an operand image, expert e's from first[e] (int32 [experts + 1])
@@ -1144,14 +1167,15 @@ def quantize_act_experts(x, fmt: Format, plan: ExpertPlan, perms=None, out=None)
     operand image of its rows, for gemm_experts.  perms (int32 [experts, K]): a
     permutation for each expert in place of fmt's."""
     _bf16_2d(x, fmt.K, "activations")
-    per = _per_row(x.shape[0], plan, "activations", x.device)
-    stream = _current(x.device, "activations")
-    mant, exp = _act_out(out, fmt, plan.rows, x.device)
-    _check(lib().mxq_quantize_act_experts(fmt.ref, plan._ref,
-                                          _perms(perms, fmt, plan.experts, x.device), _ptr(x), per,
-                                          x.stride(0), _ptr(mant), _ptr(exp), stream),
-           "mxq_quantize_act_experts")
-    return mant, exp
+    dev = x.device
+    per = _per_row(x.shape[0], plan, "activations", dev)
+    stream = _current(dev, "activations")
+    out, mant, exp = _image(out, fmt, plan.rows, dev)
+    status = lib().mxq_quantize_act_experts(fmt._ref, plan._ref, _perms(perms, fmt, plan.experts, dev),
+                                            x.data_ptr(), per, x.stride(0), mant, exp, stream)
+    if status:
+        _check(status, "mxq_quantize_act_experts")
+    return out
 
 
 def quantize_act_swiglu_experts(gate, up, fmt: Format, plan: ExpertPlan, perms=None, out=None):
@@ -1163,13 +1187,16 @@ def quantize_act_swiglu_experts(gate, up, fmt: Format, plan: ExpertPlan, perms=N
         raise MxqError("gate and up must have the same shape and strides")
     if up.device != gate.device:
         raise MxqError("gate and up must be on one device")
-    per = _per_row(gate.shape[0], plan, "gate", gate.device)
-    stream = _current(gate.device, "gate")
-    mant, exp = _act_out(out, fmt, plan.rows, gate.device)
-    _check(lib().mxq_quantize_act_swiglu_experts(
-        fmt.ref, plan._ref, _perms(perms, fmt, plan.experts, gate.device), _ptr(gate), _ptr(up), per,
-        gate.stride(0), _ptr(mant), _ptr(exp), stream), "mxq_quantize_act_swiglu_experts")
-    return mant, exp
+    dev = gate.device
+    per = _per_row(gate.shape[0], plan, "gate", dev)
+    stream = _current(dev, "gate")
+    out, mant, exp = _image(out, fmt, plan.rows, dev)
+    status = lib().mxq_quantize_act_swiglu_experts(
+        fmt._ref, plan._ref, _perms(perms, fmt, plan.experts, dev), gate.data_ptr(), up.data_ptr(),
+        per, gate.stride(0), mant, exp, stream)
+    if status:
+        _check(status, "mxq_quantize_act_swiglu_experts")
+    return out
 
 
 def pack_experts(w, fmt: Format, perms=None):
@@ -1200,21 +1227,23 @@ def gemm_experts(a_mant, a_exp, w_mant, w_exp, fmt: Format, plan: ExpertPlan, N:
     stream = _current(dev, "the plan")
     if N < 0:
         raise MxqError("N must be non-negative")
-    _dev_bytes(a_mant, fmt.act_bytes(plan.rows), "a_mant", dev)
-    _dev_bytes(a_exp, fmt.act_exp_bytes(plan.rows), "a_exp", dev)
-    _dev_bytes(w_mant, plan.experts * fmt.weight_bytes(N), "w_mant", dev)
-    _dev_bytes(w_exp, plan.experts * fmt.weight_exp_bytes(N), "w_exp", dev)
+    unit, tiles, slabs = fmt._units(), plan.rows >> 4, plan.experts * (N + 127 >> 7)
+    at = (_bytes(a_mant, tiles * unit[0], "a_mant", dev), _bytes(a_exp, tiles * unit[1], "a_exp", dev),
+          _bytes(w_mant, slabs * unit[2], "w_mant", dev), _bytes(w_exp, slabs * unit[3], "w_exp", dev))
     if out is None:
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise MxqError("dtype must be torch.bfloat16 or torch.float32")
         out = torch.empty((plan.pairs, N), dtype=dtype, device=dev)
-    f32 = _bf16_or_f32(out, "out")
-    if out.device != dev or out.shape[0] < plan.pairs or out.shape[1] < N:
-        raise MxqError("out is %s on %s, smaller than [%d, %d] or not on %s"
-                       % (tuple(out.shape), out.device, plan.pairs, N, dev))
-    _check(lib().mxq_gemm_experts(fmt.ref, plan._ref, N, _ptr(a_mant), _ptr(a_exp), _ptr(w_mant),
-                                  _ptr(w_exp), _ptr(out), 1 if f32 else 0, out.stride(0), stream),
-           "mxq_gemm_experts")
+        f32 = dtype is torch.float32
+    else:
+        f32 = _bf16_or_f32(out, "out")
+        if out.device != dev or out.shape[0] < plan.pairs or out.shape[1] < N:
+            raise MxqError("out is %s on %s, smaller than [%d, %d] or not on %s"
+                           % (tuple(out.shape), out.device, plan.pairs, N, dev))
+    status = lib().mxq_gemm_experts(fmt._ref, plan._ref, N, *at, out.data_ptr(), 1 if f32 else 0,
+                                    out.stride(0), stream)
+    if status:
+        _check(status, "mxq_gemm_experts")
     return out
 
 
@@ -1226,27 +1255,31 @@ def combine_experts(y, ids, weights, plan: ExpertPlan, residual=None, out=None,
     f32 = _bf16_or_f32(y, "y")
     dev = y.device
     stream = _current(dev, "y")
-    T, k = _choices(ids, torch.int32, "ids", dev)
-    _choices(weights, torch.float32, "weights", dev, (T, k))
-    if T * k != plan.pairs or y.shape[0] < T * k:
-        raise MxqError("y has %d rows and ids %d pairs, the plan %d" % (y.shape[0], T * k, plan.pairs))
-    N = y.shape[1]
+    T, k = shape = _choices(ids, torch.int32, "ids", dev)
+    _choices(weights, torch.float32, "weights", dev, shape)
+    rows, N = y.shape
+    if T * k != plan.pairs or rows < plan.pairs:
+        raise MxqError("y has %d rows and ids %d pairs, the plan %d" % (rows, T * k, plan.pairs))
+    r = ldr = 0
     if residual is not None:
         if _bf16_or_f32(residual, "residual") or residual.device != dev:
             raise MxqError("residual must be bf16, on %s" % dev)
         if residual.shape != (T, N):
             raise MxqError("residual is %s, not [%d, %d]" % (tuple(residual.shape), T, N))
+        r, ldr = residual.data_ptr(), residual.stride(0)
     if out is None:
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise MxqError("dtype must be torch.bfloat16 or torch.float32")
         out = torch.empty((T, N), dtype=dtype, device=dev)
-    of32 = _bf16_or_f32(out, "out")
-    if out.device != dev or out.shape != (T, N):
-        raise MxqError("out is %s on %s, not [%d, %d] on %s" % (tuple(out.shape), out.device, T, N, dev))
-    status = lib().mxq_combine_experts(
-        y.data_ptr(), 1 if f32 else 0, y.stride(0), ids.data_ptr(), weights.data_ptr(), T, k,
-        plan.experts, N, _ptr(residual), 0 if residual is None else residual.stride(0),
-        out.data_ptr(), 1 if of32 else 0, out.stride(0), stream)
+        of32 = dtype is torch.float32
+    else:
+        of32 = _bf16_or_f32(out, "out")
+        if out.device != dev or out.shape != (T, N):
+            raise MxqError("out is %s on %s, not [%d, %d] on %s"
+                           % (tuple(out.shape), out.device, T, N, dev))
+    status = lib().mxq_combine_experts(y.data_ptr(), 1 if f32 else 0, y.stride(0), ids.data_ptr(),
+                                       weights.data_ptr(), T, k, plan.experts, N, r, ldr,
+                                       out.data_ptr(), 1 if of32 else 0, out.stride(0), stream)
     if status:
         _check(status, "mxq_combine_experts")
     return out

@@ -93,7 +93,7 @@ mxq_status mxq_route(const mxq_route_opts *opts, const void *logits, int logits_
   if (opts->score != MXQ_SCORE_SOFTMAX && opts->score != MXQ_SCORE_SIGMOID)
     return MXQ_ERR_UNSUPPORTED;
   if (opts->k < 1 || opts->k > 32 || opts->k > g.E || !isfinite(opts->scale)) return MXQ_ERR_SHAPE;
-  if (T < 0 || T > kMaxPairs || T * opts->k != g.pairs || (T > 1 && ld < g.E)) return MXQ_ERR_SHAPE;
+  if (T < 0 || T > kMaxGrid * 4 || T * opts->k != g.pairs || (T > 1 && ld < g.E)) return MXQ_ERR_SHAPE;
   if (T > 0 && (!logits || !ids || !weights)) return MXQ_ERR_NULL;
   if (!aligned(logits, logits_f32 ? 4 : 2) || !aligned(ids, 16) || !aligned(weights, 16) ||
       !aligned(opts->bias, 4))

@@ -462,3 +462,145 @@ def test_layers_on_two_streams():
         for got, ref in zip((x, y), want):
             for g, w in zip(got, ref):
                 assert torch.equal(g, w)
+
+
+# --------------------------------------------------------------------------
+# where it can go wrong
+
+@pytest.mark.parametrize("T,E,k", [(0, 8, 2), (31, 64, 8), (32, 64, 8), (32, 1024, 8), (33, 64, 8), (16, 64, 16),
+                                   (17, 64, 16), (8, 64, 32), (9, 64, 32), (256, 5, 1), (2048, 4, 1), (2049, 4, 1)])
+def test_route_at_the_borders_of_its_launches(T, E, k):
+    _check_route(_randn((T, E), T + k), k)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_neighbours_that_32_bits_cannot_tell_apart(score):
+    """Scores one unit of the logits apart, in an order that only 64 bits show."""
+    g = np.random.RandomState(0)
+    x = np.zeros((64, 96), np.float32)
+    for t in range(64):
+        steps = g.permutation(96)
+        v = np.float32(0.5 + t / 16)
+        x[t] = (np.full(96, v, np.float32).view(np.int32) + steps.astype(np.int32)).view(np.float32)
+    b = torch.zeros(96)
+    for bias in (None, b, b + 0.25, 1e-9 * torch.from_numpy(g.randn(96).astype(np.float32))):
+        _check_route(torch.from_numpy(x), 7, score=score, bias=bias)
+
+
+def test_products_past_2_to_the_32_elements_of_y():
+    """140000 pairs of 32768 columns: 9.2 GB of bf16 results."""
+    T, N, K = 140000, 32768, 32
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn((T, K), generator=g).to(torch.bfloat16)
+    w = torch.randn((2, N, K), generator=g).to(torch.bfloat16)
+    ids = torch.randint(0, 2, (T, 1), generator=g).int()
+    fmt = mxq.Format(K, [4])
+    plan = mxq.expert_plan(ids.cuda(), 2)
+    wm, we = mxq.pack_experts(w.cuda(), fmt)
+    y = mxq.gemm_experts(*mxq.quantize_act_experts(x.cuda(), fmt, plan), wm, we, fmt, plan, N)
+    at = np.array([0, 1, 65535, 131071, 131072, 131073, T - 2, T - 1])
+    want, big = oe.product(bits_of(x)[at], bits_of(w), ids.numpy()[at], None, [4])
+    got = y[torch.from_numpy(at).cuda()].double().cpu().numpy()
+    tol = 17 * 2.0 ** -23 * big
+    assert np.all(np.abs(got - want) <= tol + 2.0 ** -8 * (np.abs(want) + tol))
+    o = mxq.combine_experts(y, ids.cuda(), torch.full((T, 1), 0.5, device="cuda"), plan)
+    assert torch.equal(o[-5:], (y[-5:].float() * 0.5).to(torch.bfloat16))
+
+
+def test_source_rows_past_2_to_the_32_elements():
+    """Rows 65536 elements apart, the last ones 9 GB behind the first."""
+    T, ld, K = 70000, 65536, 512
+    x = torch.zeros((T, ld), dtype=torch.bfloat16, device="cuda")
+    view = x[:, 64:64 + K]
+    view.copy_(torch.randn((T, K), device="cuda"))
+    fmt = mxq.Format(K, [4] * 12 + [6] * 2 + [8] * 2)
+    ids = torch.zeros((T, 1), dtype=torch.int32)
+    ids[:-40] = -1                                       # the last 40 tokens alone choose
+    plan = mxq.expert_plan(ids.cuda(), 1)
+    near = torch.zeros((40, 1), dtype=torch.int32)
+    small = mxq.expert_plan(near.cuda(), 1)
+    last = view[-40:].contiguous()
+    for u in (None, x[:, 1024:1024 + K]):
+        if u is None:
+            a = mxq.quantize_act_experts(view, fmt, plan)
+            b = mxq.quantize_act_experts(last, fmt, small)
+        else:
+            u.copy_(torch.randn((T, K), device="cuda"))
+            a = mxq.quantize_act_swiglu_experts(view, u, fmt, plan)
+            b = mxq.quantize_act_swiglu_experts(last, u[-40:].contiguous(), fmt, small)
+        for s, t, rows in zip(a, b, _byte_rows(list(fmt.widths), 48)):
+            s, t = s[:t.numel()].cpu().numpy(), t.cpu().numpy()
+            assert np.array_equal(s[rows < 40], t[rows < 40])
+
+
+def test_weights_past_4_gb():
+    """The last of 80 experts of 62 MB each."""
+    E, N, K = 80, 28672, 4096
+    fmt = mxq.Format(K, [4] * 128)
+    w = (0.02 * torch.randn((1, N, K), device="cuda")).to(torch.bfloat16)
+    one = mxq.pack_experts(w, fmt)
+    many = [torch.zeros((E, t.shape[1]), dtype=torch.uint8, device="cuda") for t in one]
+    for m, t in zip(many, one):
+        m[-1:] = t
+    x = torch.randn((20, K), device="cuda").to(torch.bfloat16)
+    ids = torch.full((20, 1), E - 1, dtype=torch.int32, device="cuda")
+    plan = mxq.expert_plan(ids, E)
+    y = mxq.gemm_experts(*mxq.quantize_act_experts(x, fmt, plan), *many, fmt, plan, N, dtype=torch.float32)
+    first = mxq.expert_plan(torch.zeros_like(ids), E)
+    many[0][0], many[1][0] = one[0][0], one[1][0]
+    z = mxq.gemm_experts(*mxq.quantize_act_experts(x, fmt, first), *many, fmt, first, N, dtype=torch.float32)
+    assert torch.equal(y, z) and bool((y != 0).any())
+
+
+def test_permutations_with_entries_out_of_range():
+    """They read as zeros, as in the plain quantizer."""
+    g = torch.Generator().manual_seed(4)
+    K, E = 96, 3
+    perms = torch.stack([torch.randperm(K, generator=g) for _ in range(E)]).int()
+    perms[0, 5], perms[1, 40], perms[2, 95] = -1, K, 2 ** 31 - 1
+    x = torch.randn((30, K), generator=g).to(torch.bfloat16).cuda()
+    ids = torch.randint(0, E, (30, 1), generator=g).int()
+    plan = mxq.expert_plan(ids.cuda(), E)
+    fmt = mxq.Format(K, [4, 6, 8])
+    w = torch.randn((E, 40, K), generator=g).to(torch.bfloat16).cuda()
+    wm, we = mxq.pack_experts(w, fmt, perms=perms.cuda())
+    am, ae = mxq.quantize_act_experts(x, fmt, plan, perms=perms.cuda())
+    y = mxq.gemm_experts(am, ae, wm, we, fmt, plan, 40, dtype=torch.float32)
+    for e in range(E):
+        here = torch.nonzero(ids[:, 0] == e)[:, 0].cuda()
+        f = mxq.Format(K, [4, 6, 8], perms[e].cuda())
+        want = mxq.gemm(*mxq.quantize_act(x[here].contiguous(), f), *mxq.pack_weights(w[e], f), f, len(here), 40)
+        assert torch.allclose(y[here], want, rtol=1e-5, atol=1e-5)
+
+
+def test_refused_tensors():
+    """Checks of the binding that need device tensors."""
+    fmt = mxq.Format(64, [4, 4])
+    x = torch.zeros((6, 64), dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros((6, 2), dtype=torch.int32, device="cuda")
+    plan = mxq.expert_plan(ids, 4)
+    am, ae = mxq.quantize_act_experts(x, fmt, plan)
+    w = torch.zeros((4, 20, 64), dtype=torch.bfloat16, device="cuda")
+    wm, we = mxq.pack_experts(w, fmt)
+    y = torch.zeros((12, 20), device="cuda")
+    weights = torch.zeros((6, 2), device="cuda")
+    for f in (lambda: mxq.route(x, 65), lambda: mxq.route(x, 2, score="max"), lambda: mxq.route(x.half(), 2),
+              lambda: mxq.route(x, 2, bias=torch.zeros(63, device="cuda")),
+              lambda: mxq.route(x, 2, out=(ids, weights, plan)),            # a plan of 4 experts, not 64
+              lambda: mxq.route(x, 2, scale=float("nan")), lambda: mxq.route(x.expand(6, 64)[:, ::2], 2),
+              lambda: mxq.expert_plan(ids.long(), 4), lambda: mxq.expert_plan(ids[:, :1], 4),
+              lambda: mxq.expert_plan(ids, 5, out=plan),
+              lambda: mxq.expert_plan(ids, 4, out=mxq.ExpertPlan(12, 4, first=plan.first, pair=plan.pair)),
+              lambda: mxq.quantize_act_experts(x[:5], fmt, plan), lambda: mxq.quantize_act_experts(x[:, :32], fmt, plan),
+              lambda: mxq.quantize_act_experts(x, fmt, plan, perms=torch.zeros((3, 64), dtype=torch.int32, device="cuda")),
+              lambda: mxq.quantize_act_experts(x, fmt, plan, out=(am[:-1], ae)),
+              lambda: mxq.gemm_experts(am, ae, wm[:3].contiguous(), we, fmt, plan, 20),
+              lambda: mxq.gemm_experts(am, ae, wm, we, fmt, plan, 200), lambda: mxq.gemm_experts(am, ae, wm, we, fmt, plan, -1),
+              lambda: mxq.gemm_experts(am, ae, wm, we, fmt, plan, 20, out=y[:11]),
+              lambda: mxq.gemm_experts(am, ae, wm, we, fmt, plan, 20, dtype=torch.float16),
+              lambda: mxq.combine_experts(y[:10], ids, weights, plan), lambda: mxq.combine_experts(y, ids, weights[:5], plan),
+              lambda: mxq.combine_experts(y, ids, weights, plan, residual=y[:6]),
+              lambda: mxq.combine_experts(y, ids, weights, plan, out=y[:5]),
+              lambda: mxq.pack_experts(w.float(), fmt), lambda: mxq.pack_experts(w[0], fmt)):
+        with pytest.raises(mxq.MxqError):
+            f()

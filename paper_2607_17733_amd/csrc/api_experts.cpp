@@ -170,7 +170,6 @@ mxq_status mxq_combine_experts(const void *y, int y_f32, int64_t ldy, const int3
     return MXQ_ERR_SHAPE;
   if (N > INT32_MAX || ldy < N || ldo < N || (residual && ldr < N)) return MXQ_ERR_SHAPE;
   if (T == 0 || N == 0) return MXQ_OK;
-  if (T > kMaxGrid * 256 / N) return MXQ_ERR_SHAPE;
   if (!y || !ids || !weights || !out) return MXQ_ERR_NULL;
   if (!aligned(y, y_f32 ? 4 : 2) || !aligned(out, out_f32 ? 4 : 2) || !aligned(ids, 4) ||
       !aligned(weights, 4) || !aligned(residual, 2))

@@ -433,13 +433,8 @@ __global__ __launch_bounds__(kPlanThreads) void route_few_kernel(RouteArgs a, Pl
 // allow 16-byte pieces, and the loads of four experts' rows in flight.
 
 template <bool VEC>
-__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
+__device__ inline void combine(const CombineArgs &a, int64_t t, int64_t c) {
   constexpr int C = VEC ? 8 : 1;
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const uint32_t per = (uint32_t)(a.N / C);
-  const int64_t t = i / per;
-  if (t >= a.T) return;
-  const int64_t c = C * (i - t * per);
   auto unpack = [](comb_u4 v, float *f) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -507,6 +502,18 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
   }
 }
 
+template <bool VEC>
+__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
+  constexpr int C = VEC ? 8 : 1;
+  const uint32_t per = (uint32_t)(a.N / C);
+  // (a dispatch holds fewer threads than the largest results have elements)
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.T * per;
+       i += (int64_t)gridDim.x * kThreads) {
+    const int64_t t = i / per;
+    combine<VEC>(a, t, C * (i - t * per));
+  }
+}
+
 }  // namespace
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t s) {
@@ -549,7 +556,7 @@ hipError_t launch_combine(const CombineArgs &a, hipStream_t s) {
   const bool vec =
       a.N % 8 == 0 && ((a.ldy * yb | a.ldo * ob | (a.residual ? a.ldr * 2 : 0)) & 15) == 0 &&
       (((uintptr_t)a.y | (uintptr_t)a.out | (uintptr_t)a.residual) & 15) == 0;
-  const int64_t n = (a.T * (a.N / (vec ? 8 : 1)) + kThreads - 1) / kThreads;
+  const int64_t n = std::min<int64_t>((a.T * (a.N / (vec ? 8 : 1)) + kThreads - 1) / kThreads, 1 << 22);
   if (vec) hipLaunchKernelGGL(combine_kernel<true>, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL(combine_kernel<false>, dim3((unsigned)n), dim3(kThreads), 0, s, a);
   return hipGetLastError();

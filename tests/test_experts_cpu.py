@@ -132,7 +132,7 @@ def test_combine_refusals(L):
                      [(dict([(n, -1)]), SHAPE) for n in ("T", "N", "k", "E")] +
                      [(dict(k=0), SHAPE), (dict(E=0), SHAPE), (dict(ldy=39), SHAPE), (dict(ldr=39), SHAPE),
                       (dict(ldo=39), SHAPE), (dict(T=2 ** 26, k=2), SHAPE), (dict(T=2 ** 62, k=4), SHAPE),
-                      (dict(T=2 ** 26, k=1, N=2 ** 20, ldy=2 ** 20, ldr=2 ** 20, ldo=2 ** 20), SHAPE),
+                      (dict(T=2 ** 20, k=1, N=2 ** 31, ldy=2 ** 31, ldr=2 ** 31, ldo=2 ** 31), SHAPE),
                       (dict(y=FAKE + 1), ALIGN), (dict(y=FAKE + 2, f32=1), ALIGN), (dict(out=FAKE + 1), ALIGN),
                       (dict(out=FAKE + 2, of32=1), ALIGN), (dict(ids=FAKE + 2), ALIGN), (dict(w=FAKE + 2), ALIGN),
                       (dict(res=FAKE + 1), ALIGN),

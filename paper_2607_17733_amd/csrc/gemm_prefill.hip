@@ -624,24 +624,30 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
   // columns of the quad) so that a lane stores four consecutive columns.
   const bool vec = (g.ldy & 3) == 0 && ((uintptr_t)g.y & 15) == 0 && col0 + BN <= g.N;
   const int j = l32 & 3;
+  // (the lane's rows of y, all in one latency: one by one between the stores they took 7 %
+  // of the whole product)
+  int64_t rows[TM][4];
+#pragma unroll
+  for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t row = row0 + wave * 32 * TM + tm * 32 + 8 * q + 4 * lh + j;
+      rows[tm][q] = row < g.M ? BY ? pair[row] : row : -1;
+      if (BY && rows[tm][q] >= g.x.pairs) rows[tm][q] = -1;
+    }
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
     for (int tn = 0; tn < 4; ++tn)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int rr = wave * 32 * TM + tm * 32 + 8 * q + 4 * lh, cc = tn * 32 + l32;
+        const int cc = tn * 32 + l32;
         v4f s = v4f{acc[tm][tn][4 * q], acc[tm][tn][4 * q + 1], acc[tm][tn][4 * q + 2],
                     acc[tm][tn][4 * q + 3]};
-        // lane (quad k, j) now: row rr + j, columns (cc & ~3) .. + 3
+        // lane (quad k, j) now: row j of the four, columns (cc & ~3) .. + 3
         s = quad_transpose(s, j);
-        int64_t row = row0 + rr + j;
-        const int64_t col = col0 + (cc & ~3);
-        if (row >= g.M) continue;
-        if (BY) {
-          row = pair[row];
-          if (row < 0 || row >= g.x.pairs) continue;
-        }
+        const int64_t row = rows[tm][q], col = col0 + (cc & ~3);
+        if (row < 0) continue;
         store_row<BY>(g, row, col, vec, s);
       }
 }
@@ -929,6 +935,17 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
   run(Int<2>{});
   run(Int<3>{});
 
+  // the rows of y that this wave adds up: tiles wave * n .. + n - 1 of (tm, tn, q)
+  constexpr int kOwn = 16 * TM / KG;
+  const int j = l32 & 3;
+  int64_t rows[kOwn];
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int tq = wave * kOwn + i;
+    const int64_t row = row0 + 32 * (tq >> 4) + 8 * (tq & 3) + 4 * lh + j;
+    rows[i] = row < g.M ? BY ? pair[row] : row : -1;
+    if (BY && rows[i] >= g.x.pairs) rows[i] = -1;
+  }
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
@@ -940,21 +957,15 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
                 acc[tm][tn][4 * q + 3]};
   __syncthreads();
   const bool vec = (g.ldy & 3) == 0 && ((uintptr_t)g.y & 15) == 0 && col0 + BN <= g.N;
-  const int j = l32 & 3;
 #pragma unroll
-  for (int i = 0; i < 16 * TM / KG; ++i) {
-    const int tq = wave * (16 * TM / KG) + i, tm = tq >> 4, tn = (tq >> 2) & 3, q = tq & 3;
+  for (int i = 0; i < kOwn; ++i) {
+    const int tq = wave * kOwn + i, tn = (tq >> 2) & 3;
     v4f s = red[0][tq][lane];
 #pragma unroll
     for (int k = 1; k < KG; ++k) s += red[k][tq][lane];
     s = quad_transpose(s, j);
-    int64_t row = row0 + 32 * tm + 8 * q + 4 * lh + j;
-    const int64_t col = col0 + ((tn * 32 + l32) & ~3);
-    if (row >= g.M) continue;
-    if (BY) {
-      row = pair[row];
-      if (row < 0 || row >= g.x.pairs) continue;
-    }
+    const int64_t row = rows[i], col = col0 + ((tn * 32 + l32) & ~3);
+    if (row < 0) continue;
     store_row<BY>(g, row, col, vec, s);
   }
 }
@@ -1099,15 +1110,15 @@ hipError_t launch_gemm_prefill(const GemmArgs &a, hipStream_t stream) {
 //   more: two: 333 x 8 x 2, 4096, 4000 28, 27; 1000 x 32 x 4, 2048, 3584 92, 83; 2000 x
 //     8 x 2, 1024, 2048 32, 27 (tiled 30)
 //   from 48 rows and 3 1/4 tiles of 128 rows per CU on: tiled: 4096 x 8 x 2, 4096, 28672
-//     1556 (2138; tiles of 256 rows, one per CU, 1650), 1000 x 32 x 4, 2048, 3584 76
+//     1517 (2138; tiles of 256 rows, one per CU, 1506, but 2048 tokens 448 to 414), 1000 x 32 x 4, 2048, 3584 76
 //     (83), 2048 x 64 x 6, 1408, 2048 71 (76), 512 x 32 x 4, 2048, 3584 53 (59); 800 x 8
 //     x 2, 4096, 4096, with two per CU, 51.3 (50.7)
-// The full clamp's 12 KB weight stages leave a CU one tiled workgroup, so that two shares
-// of 64 rows take its place: 2048 x 8 x 2, 4096, 14336 480 (tiled 593, of 256 rows 537).
+// The full clamp's 12 KB weight stages leave a CU one tiled workgroup, of 256 rows then:
+// 2048 x 8 x 2, 4096, 14336 462 (of 128 rows about 590, two shares of 64 rows 486).
 // A kernel that streams weights for 16-row tiles, as for single linears, took 51 for 64 x
 // 128 x 8 and 94 for 8 x 8 x 2.
 struct ExpertLaunch {
-  enum { kSplit4, kSplit2, kSplit2x64, kTiled } kernel;
+  enum { kSplit4, kSplit2, kTiled } kernel;
   int near;                // row tiles to a column tile that run together
   int64_t groups;          // workgroups
 };
@@ -1120,9 +1131,9 @@ static ExpertLaunch expert_launch(const GemmArgs &a) {
   ExpertLaunch l{ExpertLaunch::kSplit2, 1, 0};
   int lg = 5;
   if (mean >= 48 && 4 * about(7) * nt >= 13 * cus) {
-    l.kernel = a.full ? ExpertLaunch::kSplit2x64 : ExpertLaunch::kTiled;
-    l.near = 4;
-    lg = a.full ? 6 : 7;
+    l.kernel = ExpertLaunch::kTiled;
+    l.near = a.full ? 1 : 4;
+    lg = a.full ? 8 : 7;
   } else if (mean <= 16 || (about(5) + active / 2) * nt <= 2 * cus) {
     l.kernel = ExpertLaunch::kSplit4;
   }
@@ -1138,20 +1149,15 @@ static hipError_t go_experts(const GemmArgs &a, hipStream_t stream) {
   const ExpertLaunch l = expert_launch(a);
   const int ntiles = (int)((a.N + BN - 1) / BN);
   const dim3 grid((unsigned)l.groups);
-  auto split = [&](auto kg, auto tm) {
-    constexpr int KG = decltype(kg)::value, TM = decltype(tm)::value;
-    hipLaunchKernelGGL((gemm_split_kernel<FULL, KG, TM, false, true>), grid, dim3(64 * KG), 0, stream, a,
-                       0, ntiles, l.near);
-  };
-  using I1 = std::integral_constant<int, 1>;
-  using I2 = std::integral_constant<int, 2>;
-  using I4 = std::integral_constant<int, 4>;
-  if (l.kernel == ExpertLaunch::kSplit4) split(I4{}, I1{});
-  else if (l.kernel == ExpertLaunch::kSplit2) split(I2{}, I1{});
-  else if constexpr (FULL) split(I2{}, I2{});
+  if (l.kernel == ExpertLaunch::kSplit4)
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 1, false, true>), grid, dim3(256), 0, stream, a, 0,
+                       ntiles, l.near);
+  else if (l.kernel == ExpertLaunch::kSplit2)
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, 2, 1, false, true>), grid, dim3(128), 0, stream, a, 0,
+                       ntiles, l.near);
   else
-    hipLaunchKernelGGL((gemm_prefill_kernel<false, 1, true>), grid, dim3(NT), 0, stream, a, 0, ntiles,
-                       l.near, 0);
+    hipLaunchKernelGGL((gemm_prefill_kernel<FULL, FULL ? 2 : 1, true>), grid, dim3(NT), 0, stream, a,
+                       0, ntiles, l.near, 0);
   return hipGetLastError();
 }
 

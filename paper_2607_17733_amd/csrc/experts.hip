@@ -1,6 +1,20 @@
 // experts.hip -- routing of tokens to experts, the plan that lays the chosen pairs
 // out by expert, and the weighted sum of a token's experts (include/mxq.h states
 // them).
+//
+// Routing.  Both scores rise with the logits, so the choice needs no exponential, only
+// an order: a wave holds a token's logits as integer keys, a few to a lane, and takes
+// the largest k times by a reduction over the lanes.  The exponentials of the k chosen
+// are taken relative to the largest (of the chosen, where only their ratios count).
+// With a bias the order is that of score + bias, whose neighbours 32 bits cannot always
+// tell apart; 64 bits decide then.  Vector instructions bound it: 8191 tokens among 256
+// experts, 8 chosen, with a bias 14 us, without 8 (bytes: 2); one token, with its plan
+// by the same workgroup, 3.5, most of it the launch.
+//
+// Plan.  A counting sort, stable, whole numbers only: 65528 pairs 7 + 2 to 4 us, latency
+// (0.5 MB).  Image rows come in sixteens, so an expert wastes 8 rows on average.
+//
+// Weighted sum.  Bytes: 2048 tokens of 6 experts, 2048 columns, 67 MB 13 us (5.2 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -93,7 +107,7 @@ __device__ inline uint64_t key_of(double x) {
 // The keys of a wave's experts, lane l's being those of l, l + 64, ...; take() gives the
 // largest that is left and the lowest expert that has it.  Up to four a lane are put in
 // order once, so that a round looks at one of each lane (a round that looked through four
-// took 100 instructions: 8191 tokens among 256 experts 15.5 us, ordered ROUTE).
+// took 100 instructions: 8191 tokens among 256 experts 15.5 us, ordered 14).
 template <int NE, typename U>
 struct Keys {
   static constexpr bool kOrdered = NE <= 4;

@@ -50,6 +50,12 @@
 // complete.  Workgroup ids are remapped so that each XCD owns
 // a compact block of output tiles: the activation rows and weight columns it
 // reads stay in its L2.
+//
+// Products by experts (BY; experts_device.h, expert_launch below).  The operand image
+// holds every expert's rows from a multiple of 16 on, so a tile of them is a tile as
+// above: the kernels run on it with the expert's weights, and the rows of y are looked
+// up.  Nothing but the prologue and the epilogue differs, and a row's sums are those
+// that the same kernel forms for a single linear.
 #include "experts_device.h"
 #include "mxq_device.h"
 #include "mxq_internal.h"
@@ -253,7 +259,10 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
   // arithmetic), so the 32-bit buffer offsets stay below 4 image tiles; the
   // host rejects shapes where 16 tiles pass INT32_MAX.
   const int64_t last = (g.M - 1) / kATileRows;
-  const int64_t ta = min(row0 / kATileRows + 2 * TM * wave, last);
+  // (by experts the rows that a short tile leaves out are another wave's in each
+  // workgroup, so that no SIMD has all of them)
+  const int part = BY ? (wave + (blockIdx.x >> 3)) & (kWaves - 1) : wave;
+  const int64_t ta = min(row0 / kATileRows + 2 * TM * part, last);
   const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(
       (void *)(g.a_mant + ta * g.a_tile), 0,
       (int)min((last + 1 - ta) * g.a_tile, (int64_t)0x7fffffff), 0x00020000);
@@ -600,6 +609,23 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
     }
   };
 
+  // An expert's last tile: a wave without rows only brings its share of the weights, and
+  // leaves its SIMD to the other workgroup's (1000 tokens among 32 experts, 2048 x 3584
+  // 82 -> 74 us).  Its loads in flight are those of the steps below, less the
+  // activations and scales.
+  if (BY && row0 + 32 * TM * part >= g.M) {
+    for (int s = 0; s < kWAhead; ++s) issue_w(s, 0, C::kWLoads);
+    wait_loads<(kWAhead - 1) * C::kWLoads>();
+    barrier();
+    for (int s = 0; s < nsteps; ++s) {
+      wait_loads<(kWAhead - 2) * C::kWLoads>();
+      barrier();
+      issue_w(s + kWAhead, 0, C::kWLoads);
+    }
+    wait_loads<0>();
+    return;
+  }
+
   // Prologue: the weights of steps 0 and 1, the activations of step 0, the
   // weights of steps 2 and 3, and the wait for the stage of step 0.
   issue_w(0, 0, C::kWLoads);
@@ -631,7 +657,7 @@ void gemm_prefill_kernel(GemmArgs g, int mtiles, int ntiles, int gm, int gn) {
   for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int64_t row = row0 + wave * 32 * TM + tm * 32 + 8 * q + 4 * lh + j;
+      const int64_t row = row0 + part * 32 * TM + tm * 32 + 8 * q + 4 * lh + j;
       rows[tm][q] = row < g.M ? BY ? pair[row] : row : -1;
       if (BY && rows[tm][q] >= g.x.pairs) rows[tm][q] = -1;
     }

@@ -637,7 +637,9 @@ __device__ inline u4 swiglu8_table(const uint16_t *tab, u4 g, u4 u) {
   return o;
 }
 
-// BY: the rows of a plan (QuantArgs::x); image rows that hold no pair are left.
+// BY: the rows of a plan (QuantArgs::x): an image row gathers its pair's source row as
+// it is staged (a token chosen by k experts is quantized k times: 8192 x 4096 of 4096
+// tokens 33 us, 73 MB; one token of 6 experts 5); image rows that hold no pair are left.
 template <bool RNA, int MODE, int PROD, bool BY>
 __global__ __launch_bounds__(kMaxThreads) void quantize_act_kernel(QuantArgs q) {
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];

@@ -99,7 +99,9 @@ __global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeRowsArgs a, int6
 // Queries and keys normalised per head and rotated: L lanes of eight values hold a
 // head (a power of two, so that their sum is an exchange within the wave), the
 // queries' heads before the keys'.  The values stay in registers between the two;
-// those of the partners of a rotation in halves are read again, from the cache.
+// those of the partners of a rotation in halves are read again, from the cache.  Bytes
+// bound it: 4001 tokens of 48 heads, half of each rotated, 99 MB 21.7 us (4.6 TB/s; a
+// large copy moves 4.7 to 5.2); one token 3 us, the launch.
 __global__ __launch_bounds__(kThreads) void rope_qk_kernel(RopeQkArgs a, int lg_lanes,
                                                            int64_t total) {
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;

@@ -1125,46 +1125,39 @@ hipError_t launch_gemm_prefill(const GemmArgs &a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Rows by experts.  The launch is sized by the pairs and the experts alone; a mean
-// group is the pairs over the experts that they can reach.  us of the kernels that split
-// K in four, in two (both 32-row tiles, the tiled one 128), tokens x experts x choices,
-// K, N, 4-6-8 maps:
-//   up to 16 rows, or up to two tiles of 32 rows per CU: four shares:
-//     1 x 64 x 6, 2048, 2816 8.6, 9.5; 64 x 128 x 8, 2048, 1536 48, 53; 8 x 8 x 2,
-//     4096, 28672 88, 99; 48 x 16 x 4, 1408, 2048 9.8, 10.4; 100 x 2 x 1, 8192, 8192
-//     17.5, 22.6 (but 16 x 64 x 6, 2048, 2816 35, 33)
-//   more: two: 333 x 8 x 2, 4096, 4000 28, 27; 1000 x 32 x 4, 2048, 3584 92, 83; 2000 x
-//     8 x 2, 1024, 2048 32, 27 (tiled 30)
-//   from 48 rows and 3 1/4 tiles of 128 rows per CU on: tiled: 4096 x 8 x 2, 4096, 28672
-//     1517 (2138; tiles of 256 rows, one per CU, 1506, but 2048 tokens 448 to 414), 1000 x 32 x 4, 2048, 3584 76
-//     (83), 2048 x 64 x 6, 1408, 2048 71 (76), 512 x 32 x 4, 2048, 3584 53 (59); 800 x 8
-//     x 2, 4096, 4096, with two per CU, 51.3 (50.7)
-// The full clamp's 12 KB weight stages leave a CU one tiled workgroup, of 256 rows then:
-// 2048 x 8 x 2, 4096, 14336 462 (of 128 rows about 590, two shares of 64 rows 486).
-// A kernel that streams weights for 16-row tiles, as for single linears, took 51 for 64 x
-// 128 x 8 and 94 for 8 x 8 x 2.
+// Rows by experts.  The launch is sized by the pairs and the experts alone: a mean group is
+// the pairs over the experts that they can reach, and tiles are counted as if half of
+// one per expert were empty.  Groups of 32 rows and more that come to 1.4 tiles of 128
+// rows per CU take the tiled kernel, others four shares of K over 32-row tiles.  us of
+// shares, tiled; tokens x experts x choices, K, N, 4-6-8 maps:
+//   4096 x 8 x 2, 4096, 28672 2522, 1517; 1000 x 32 x 4, 2048, 3584 92, 72; 1792, 2048 44,
+//   36; 2048, 1024 29, 26 (1.5 tiles per CU); 256 x 32 x 4, 2048, 3584 44, 42 (32 rows); 300
+//   x 4 x 2, 2048, 8192 28, 22 (1.5); 700 x 16 x 2, 8192, 4096 113, 116; 128 x 8 x 2, 4096,
+//   14336 70, 74 (32 rows)
+//   256 x 64 x 6, 2048, 2816 61, 63 (24 rows); 333 x 8 x 2, 4096, 4000 27, 30 (1.1); 400 x 8
+//   x 2, 4096, 4096 28, 34 (1.25); 64 x 128 x 8, 2048, 1536 48, about 80
+// Two shares of K were within 5 % of four everywhere that tiles are not taken (16 x 64 x 6,
+// 2048, 2816 33 against 35, 8 x 8 x 2, 4096, 28672 99 against 88); tiles of 256 rows, one
+// workgroup per CU, 1506 in the first case, but 448 against 414 for 2048 tokens.  The full
+// clamp's 12 KB weight stages leave a CU one tiled workgroup, of 256 rows then: 2048 x 8 x
+// 2, 4096, 14336 462 (of 128 rows about 590).  A kernel that streams weights for 16-row
+// tiles, as for single linears, took 51 for 64 x 128 x 8 and 94 for 8 x 8 x 2, 4096, 28672.
 struct ExpertLaunch {
-  enum { kSplit4, kSplit2, kTiled } kernel;
+  bool tiled;
   int near;                // row tiles to a column tile that run together
   int64_t groups;          // workgroups
 };
 static ExpertLaunch expert_launch(const GemmArgs &a) {
   const int64_t cus = device_cu_count(), nt = (a.N + BN - 1) / BN;
   const int64_t active = std::min<int64_t>(a.x.E, a.x.pairs), mean = a.x.pairs / active;
-  // tiles of 2^lg rows: about as many, and as many as any choice needs
-  auto about = [&](int lg) { return (a.x.pairs >> lg) + active / 2; };
-  auto tiles = [&](int lg) { return active + ((a.x.rows - 16 * active) >> lg); };
-  ExpertLaunch l{ExpertLaunch::kSplit2, 1, 0};
-  int lg = 5;
-  if (mean >= 48 && 4 * about(7) * nt >= 13 * cus) {
-    l.kernel = ExpertLaunch::kTiled;
-    l.near = a.full ? 1 : 4;
-    lg = a.full ? 8 : 7;
-  } else if (mean <= 16 || (about(5) + active / 2) * nt <= 2 * cus) {
-    l.kernel = ExpertLaunch::kSplit4;
-  }
-  // (whole groups of `near` row tiles, as many for every XCD)
-  l.groups = ((tiles(lg) + l.near - 1) / l.near * nt + 7) / 8 * 8 * l.near;
+  ExpertLaunch l;
+  l.tiled = mean >= 32 && 5 * ((a.x.pairs >> 7) + active / 2) * nt >= 7 * cus;
+  l.near = l.tiled && !a.full ? 4 : 1;
+  const int lg = !l.tiled ? 5 : a.full ? 8 : 7;
+  // as many tiles of 2^lg rows as any choice needs, in whole groups of `near`, as many for
+  // every XCD
+  const int64_t tiles = active + ((a.x.rows - 16 * active) >> lg);
+  l.groups = ((tiles + l.near - 1) / l.near * nt + 7) / 8 * 8 * l.near;
   return l;
 }
 
@@ -1175,15 +1168,12 @@ static hipError_t go_experts(const GemmArgs &a, hipStream_t stream) {
   const ExpertLaunch l = expert_launch(a);
   const int ntiles = (int)((a.N + BN - 1) / BN);
   const dim3 grid((unsigned)l.groups);
-  if (l.kernel == ExpertLaunch::kSplit4)
-    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 1, false, true>), grid, dim3(256), 0, stream, a, 0,
-                       ntiles, l.near);
-  else if (l.kernel == ExpertLaunch::kSplit2)
-    hipLaunchKernelGGL((gemm_split_kernel<FULL, 2, 1, false, true>), grid, dim3(128), 0, stream, a, 0,
-                       ntiles, l.near);
-  else
+  if (l.tiled)
     hipLaunchKernelGGL((gemm_prefill_kernel<FULL, FULL ? 2 : 1, true>), grid, dim3(NT), 0, stream, a,
                        0, ntiles, l.near, 0);
+  else
+    hipLaunchKernelGGL((gemm_split_kernel<FULL, 4, 1, false, true>), grid, dim3(256), 0, stream, a, 0,
+                       ntiles, l.near);
   return hipGetLastError();
 }
 

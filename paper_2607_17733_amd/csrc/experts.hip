@@ -208,8 +208,8 @@ __device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float 
     }
   } else {
     // The scores in 32 bits first.  Theirs and their sums' errors are below 2^-19 of the
-    // larger of 1 and the sum; where two neighbours of the order are within 2^-17, about
-    // one token in a hundred, all are formed in 64 bits.
+    // larger of 1 and the sum; where two neighbours of the order are within 2^-17, all are
+    // formed in 64 bits.
     float s[NE], all = 0.f;
 #pragma unroll
     for (int i = 0; i < NE; ++i) {

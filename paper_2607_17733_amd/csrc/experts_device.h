@@ -27,7 +27,7 @@ __device__ inline int wave_scan(int v) {
 // The tiles lie in order of the experts, `near` row tiles to a column tile; groups of
 // `near` go to the XCDs (workgroup pid to pid % 8) in turn, so that all have as many and
 // surplus workgroups come last.  (Longer runs, up to an eighth of all for each XCD,
-// were 5 % faster to 5 % slower; column tiles bound to an XCD up to a third slower
+// were 10 % faster to 50 % slower; column tiles bound to an XCD up to a quarter slower
 // where their number is no multiple of 8.)  Every lane of the wave calls it.
 struct ExpertTile {
   int e, row0, rows, nt;

@@ -604,3 +604,44 @@ def test_refused_tensors():
               lambda: mxq.pack_experts(w.float(), fmt), lambda: mxq.pack_experts(w[0], fmt)):
         with pytest.raises(mxq.MxqError):
             f()
+
+
+# --------------------------------------------------------------------------
+# the tiled kernel: groups of 32 rows and more, 1.4 tiles of 128 rows per CU and more
+
+@pytest.mark.parametrize("clamp", ["sym", "full"])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,E,k,K,N,how", [(1400, 4, 2, 32, 5000, "any"), (1400, 4, 2, 736, 4999, "skewed"),
+                                           (700, 9, 2, 160, 9000, "any"), (300, 4, 2, 96, 20000, "skewed"),
+                                           (257, 2, 1, 1408, 33000, "one"), (2000, 40, 2, 352, 3001, "skewed")])
+def test_product_on_tiles(T, E, k, K, N, how, out, clamp):
+    _product_case(T, E, k, K, N, how=how, out=out, clamp=clamp, sample=120, perms="shared",
+                  mix=(4, 6, 8) if K > 32 else (4,), ldy=T % 8)
+
+
+@pytest.mark.parametrize("clamp", ["sym", "full"])
+@pytest.mark.parametrize("mix", [(3,), (4,), (6,), (8,), (3, 6, 8), (4, 6), (3, 8), (3, 4, 6, 8)])
+def test_product_on_tiles_of_width_mixes(mix, clamp):
+    for blocks in (1, 5, 23):
+        _product_case(450, 5, 2, 32 * blocks, 9000, mix=mix, clamp=clamp, sample=60, how="skewed",
+                      round_="rna" if blocks == 5 else "rne")
+
+
+def test_rows_do_not_depend_on_the_other_groups():
+    """The same pairs beside other ones, in a call of the same size: bit for bit."""
+    g = torch.Generator().manual_seed(0)
+    T, E, K, N = 600, 6, 256, 9000
+    x = torch.randn((T, K), generator=g).to(torch.bfloat16).cuda()
+    w = torch.randn((E, N, K), generator=g).to(torch.bfloat16).cuda()
+    fmt = mxq.Format(K, [4] * 6 + [6, 8])
+    wm, we = mxq.pack_experts(w, fmt)
+    ids = torch.randint(0, E, (T, 1), generator=g).int()
+    other = torch.randint(0, E, (T, 1), generator=g).int()
+    other[:50] = ids[:50]
+    ys = []
+    for i in (ids, other):
+        plan = mxq.expert_plan(i.cuda(), E)
+        ys.append(mxq.gemm_experts(*mxq.quantize_act_experts(x, fmt, plan), wm, we, fmt, plan, N, dtype=torch.float32))
+    assert torch.equal(ys[0][:50], ys[1][:50])
+    same = (ids == other)[:, 0].cuda()
+    assert torch.equal(ys[0][same], ys[1][same])

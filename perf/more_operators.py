@@ -287,7 +287,8 @@ def _own_run(s):
         image = _own_image(s, mxq, fmt, plan)
         if kind == "down":
             am, ae = mxq.quantize_act_swiglu_experts(s["gate"], s["up"], fmt, plan, perms=perms, out=image)
-            y = mxq.gemm_experts(am, ae, wm, we, fmt, plan, c["N"])
+            # (float32 rows: the weighted sum's, which is rounded once, as the result)
+            y = mxq.gemm_experts(am, ae, wm, we, fmt, plan, c["N"], dtype=torch.float32)
             return mxq.combine_experts(y, ids, weights, plan, residual=s["residual"])
         am, ae = mxq.quantize_act_experts(s["x"], fmt, plan, perms=perms, out=image)
         if kind == "product":
@@ -298,7 +299,7 @@ def _own_run(s):
         fmt2, perms2, (wm2, we2) = _own_linear(s, mxq, "2")
         am, ae = mxq.quantize_act_swiglu_experts(h[:, :F], h[:, F:], fmt2, plan, perms=perms2,
                                                  out=_own_image(s, mxq, fmt2, plan, "2"))
-        y = mxq.gemm_experts(am, ae, wm2, we2, fmt2, plan, c["K"])
+        y = mxq.gemm_experts(am, ae, wm2, we2, fmt2, plan, c["K"], dtype=torch.float32)
         return ids, mxq.combine_experts(y, ids, weights, plan, residual=s["residual"])
     if kind == "norm":
         return mxq.rope_qk(s["q"], s["k"], s["pos"], s["table"], s["q_gain"], s["k_gain"], s["eps"],

@@ -763,7 +763,9 @@ mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts
  *                 mxq_pack_weights writes it for N columns, mxq_weight_bytes(fmt, N)
  *                 and mxq_weight_exp_bytes(fmt, N) apart.
  *   y             DEVICE [pairs][ldy], float32 or (y_f32 == 0) bf16 (the float32 sum
- *                 rounded to nearest even), ldy >= N, 16-byte aligned.
+ *                 rounded to nearest even), ldy >= N, 16-byte aligned.  Rows that a
+ *                 quantizer takes are bf16; float32 ones keep a weighted sum's terms
+ *                 from a rounding of their own.
  * A row's result does not depend on the other rows of its call; which kernel runs
  * goes by pairs, E and N, and the kernels differ in the order of their float32 sums.
  * Errors: as mxq_gemm, and the plan's; MXQ_ERR_SHAPE also for more tiles (of 32 or

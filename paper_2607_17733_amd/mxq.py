@@ -1222,7 +1222,8 @@ def gemm_experts(a_mant, a_exp, w_mant, w_exp, fmt: Format, plan: ExpertPlan, N:
                  dtype=torch.bfloat16):
     """Every pair's row times its expert's weights (pack_experts): [pairs, N], bf16
     or float32 (`dtype`); rows of pairs that chose no expert stay as `out` holds
-    them."""
+    them.  bf16 rows are what quantize_act_swiglu_experts takes; for rows that
+    combine_experts adds up float32 spares each a rounding before the sum."""
     dev = plan.device
     stream = _current(dev, "the plan")
     if N < 0:

@@ -645,3 +645,34 @@ def test_rows_do_not_depend_on_the_other_groups():
     assert torch.equal(ys[0][:50], ys[1][:50])
     same = (ids == other)[:, 0].cuda()
     assert torch.equal(ys[0][same], ys[1][same])
+
+
+# --------------------------------------------------------------------------
+# the bits of a layer's results
+
+def test_the_cases_sum_rows_of_32_bits(monkeypatch):
+    """A term of a token's sum is not rounded before it is added: the measured calls give the
+    one rounding of the result, and the product's and the sum's in float32."""
+    import perf.more_operators as cases
+    from oracle import fused
+    monkeypatch.setattr(cases, "own", True)
+    T, E, k, K, N = 40, 6, 3, 256, 200
+    s = cases.prepare(cases._product("down", T, E, k, K, N, kind="down", perms="each"), 0)
+    got = cases.run(s).double().cpu().numpy()
+    ids, w = s["ids"].cpu().numpy(), s["weights"].cpu().numpy()
+    act = fused.swiglu_bf16(bits_of(s["gate"]), bits_of(s["up"]))
+    y, big = oe.product(act, bits_of(s["w"]), ids, s["perm"].cpu().numpy(), list(s["widths"]))
+    tol = (K / 64 + 16) * 2.0 ** -23 * big
+    want, sums = oe.combine(y, ids, w, E, s["residual"].float().cpu().numpy())
+    # (what the product's error adds to a sum, and a rounding to float32 for each term)
+    more, _ = oe.combine(tol, ids, np.abs(w), E)
+    more = more + k * 2.0 ** -24 * (sums + more)
+    assert np.all(np.abs(got - want) <= more + 2.0 ** -8 * (np.abs(want) + more))
+
+    # a layer's rows on their way into the sum
+    seen = []
+    combine = mxq.combine_experts
+    monkeypatch.setattr(mxq, "combine_experts", lambda y, *a, **kw: (seen.append(y.dtype), combine(y, *a, **kw))[1])
+    cases.run(cases.prepare({"kind": "layer", "T": 5, "E": 4, "k": 2, "K": 128, "F": 64, "p6": 0.1, "p8": 0.05,
+                             "low": 4}, 0))
+    assert seen == [torch.float32]

@@ -1066,10 +1066,16 @@ class ExpertPlan:
     with a scratch, which route or expert_plan fills; or the caller's, of a plan that
     is made (first and pair, and work, int32 [EXPERT_WORK * experts], where it is to be
     written again).  The sizes go by pairs and experts alone, so a plan serves every
-    batch of as many tokens."""
+    batch of as many tokens.  k: the pairs of a token; route and expert_plan set it with
+    the plan that they write.  Where it is not known, the quantizers take any number of
+    rows that divides the pairs for a row per token."""
 
-    def __init__(self, pairs: int, experts: int, device="cuda", first=None, pair=None, work=None):
+    def __init__(self, pairs: int, experts: int, device="cuda", first=None, pair=None, work=None,
+                 k=None):
         self.pairs, self.experts = int(pairs), int(experts)
+        if k is not None and (k < 1 or self.pairs % k):
+            raise MxqError("%d pairs are not %d for every token" % (self.pairs, k))
+        self.k = k
         self.rows = _size(lib().mxq_expert_rows(self.pairs, self.experts), "mxq_expert_rows")
         if first is None and pair is None:
             # (one allocation; each part 16-byte aligned)
@@ -1104,7 +1110,7 @@ def route(logits, k: int, score: str = "softmax", normalise: bool = True, scale:
     if out is None:
         ids = torch.empty((T, k), dtype=torch.int32, device=dev)
         weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-        plan = ExpertPlan(T * k, E, device=dev)
+        plan = ExpertPlan(T * k, E, device=dev, k=k)
     else:
         ids, weights, plan = out
         _choices(ids, torch.int32, "ids", dev, (T, k))
@@ -1122,6 +1128,7 @@ def route(logits, k: int, score: str = "softmax", normalise: bool = True, scale:
                              stream)
     if status:
         _check(status, "mxq_route")
+    plan.k = k
     return ids, weights, plan
 
 
@@ -1136,6 +1143,7 @@ def expert_plan(ids, experts: int, out=None):
         raise MxqError("the plan is of %d pairs and %d experts on %s, not %d and %d on %s"
                        % (out.pairs, out.experts, out.device, T * k, experts, ids.device))
     _check(lib().mxq_expert_plan(ids.data_ptr(), out._ref, stream), "mxq_expert_plan")
+    out.k = k or None
     return out
 
 
@@ -1156,9 +1164,9 @@ def _per_row(rows: int, plan: ExpertPlan, what: str, dev) -> int:
         raise MxqError("the plan is on %s, not %s" % (plan.device, dev))
     if rows == plan.pairs:
         return 1
-    if rows == 0 or plan.pairs % rows:
-        raise MxqError("%s has %d rows: a row per token or per pair (%d) is needed"
-                       % (what, rows, plan.pairs))
+    if rows == 0 or plan.pairs % rows or (plan.k is not None and rows * plan.k != plan.pairs):
+        raise MxqError("%s has %d rows: a row per token (of %s pairs) or per pair (%d) is needed"
+                       % (what, rows, plan.k or "some", plan.pairs))
     return plan.pairs // rows
 
 
@@ -1261,6 +1269,8 @@ def combine_experts(y, ids, weights, plan: ExpertPlan, residual=None, out=None,
     rows, N = y.shape
     if T * k != plan.pairs or rows < plan.pairs:
         raise MxqError("y has %d rows and ids %d pairs, the plan %d" % (rows, T * k, plan.pairs))
+    if plan.k is not None and k != plan.k:
+        raise MxqError("ids have %d pairs a token, the plan %d" % (k, plan.k))
     r = ldr = 0
     if residual is not None:
         if _bf16_or_f32(residual, "residual") or residual.device != dev:

@@ -3,6 +3,7 @@ for every refused argument (nothing is launched: each call fails its checks), th
 binding's checks, and pins of the oracle."""
 import ctypes
 import math
+import types
 
 import numpy as np
 import pytest
@@ -246,3 +247,23 @@ def test_oracle_norm_has_unit_mean_square_and_keeps_lengths():
     z, _ = oe.norm_rope(x, np.arange(5), table * 0 + [1.0, 0.0], one, 0.0, False)
     assert np.allclose((z * z).mean(-1), 1.0, rtol=1e-12)
     assert not oe.norm_rope(np.zeros((1, 1, 64), np.uint16), [0], table, one, 0.0, False)[0].any()
+
+
+def test_source_rows_are_those_of_the_tokens_or_of_the_pairs():
+    """Rows that divide the pairs but are not the tokens would be other tokens' rows."""
+    plan = types.SimpleNamespace(pairs=12, experts=4, k=2, device="here")
+    assert mxq._per_row(6, plan, "x", "here") == 2 and mxq._per_row(12, plan, "x", "here") == 1
+    for rows in (0, 1, 2, 3, 4, 5, 7, 24):
+        with pytest.raises(mxq.MxqError):
+            mxq._per_row(rows, plan, "x", "here")
+    plan.k = None                                      # of a plan that came without it: as many as divide
+    assert mxq._per_row(6, plan, "x", "here") == 2 and mxq._per_row(4, plan, "x", "here") == 3
+    with pytest.raises(mxq.MxqError):
+        mxq._per_row(5, plan, "x", "here")
+    none = types.SimpleNamespace(pairs=0, experts=4, k=2, device="here")
+    assert mxq._per_row(0, none, "x", "here") == 1
+    with pytest.raises(mxq.MxqError):
+        mxq._per_row(5, none, "x", "here")
+    for k in (0, -1, 5):
+        with pytest.raises(mxq.MxqError):
+            mxq.ExpertPlan(12, 4, k=k)

@@ -676,3 +676,31 @@ def test_the_cases_sum_rows_of_32_bits(monkeypatch):
     cases.run(cases.prepare({"kind": "layer", "T": 5, "E": 4, "k": 2, "K": 128, "F": 64, "p6": 0.1, "p8": 0.05,
                              "low": 4}, 0))
     assert seen == [torch.float32]
+
+
+def test_rows_of_another_number_of_tokens_are_refused():
+    """Row counts that divide the pairs; the plan of ids, of a router, written again, or brought with k."""
+    fmt = mxq.Format(64, [4, 4])
+    x = torch.ones((12, 64), dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros((6, 2), dtype=torch.int32, device="cuda")
+    plan = mxq.expert_plan(ids, 4)
+    routed = mxq.route(torch.randn((6, 4), device="cuda"), 2)[2]
+    brought = mxq.ExpertPlan(12, 4, first=plan.first, pair=plan.pair, k=2)
+    for p in (plan, routed, brought):
+        for f in (lambda r: mxq.quantize_act_experts(x[:r], fmt, p),
+                  lambda r: mxq.quantize_act_swiglu_experts(x[:r], x[:r], fmt, p)):
+            for rows in (1, 2, 3, 4):
+                with pytest.raises(mxq.MxqError):
+                    f(rows)
+            f(6), f(12)
+    weights = torch.ones((4, 3), device="cuda")
+    y = torch.ones((12, 8), device="cuda")
+    with pytest.raises(mxq.MxqError):                   # three pairs a token, of a plan of two
+        mxq.combine_experts(y, ids.view(4, 3), weights, plan)
+    mxq.expert_plan(ids.view(4, 3), 4, out=plan)        # now of three
+    mxq.quantize_act_experts(x[:4], fmt, plan)
+    mxq.combine_experts(y, ids.view(4, 3), weights, plan)
+    with pytest.raises(mxq.MxqError):
+        mxq.quantize_act_experts(x[:6], fmt, plan)
+    mxq.quantize_act_experts(x[:4], fmt, mxq.ExpertPlan(12, 4, first=plan.first, pair=plan.pair))
+    torch.cuda.synchronize()

@@ -704,3 +704,38 @@ def test_rows_of_another_number_of_tokens_are_refused():
         mxq.quantize_act_experts(x[:6], fmt, plan)
     mxq.quantize_act_experts(x[:4], fmt, mxq.ExpertPlan(12, 4, first=plan.first, pair=plan.pair))
     torch.cuda.synchronize()
+
+
+# --------------------------------------------------------------------------
+# SiLU * up of large batches: 16-byte pieces, the table, several row groups to a workgroup
+
+@pytest.mark.parametrize("perms", ["none", "shared", "each"])
+@pytest.mark.parametrize("T,E,k,K,skip,round_", [(2001, 64, 6, 1408, 0.1, "rne"), (1001, 32, 4, 1792, 0.0, "rna"),
+                                                 (4003, 60, 6, 1408, 0.0, "rne"), (1500, 3, 8, 2048, 0.3, "rne")])
+def test_swiglu_images_of_many_groups(T, E, k, K, skip, round_, perms):
+    """Workgroups that go from one live group to the next: the table stays, the rows, the expert and its
+    permutation are others.  512 workgroups at 256 CUs, and about 700, 530, 1530 and 530 groups with rows."""
+    say("swiglu groups", T, E, k, K, skip, perms)
+    ids, plan, fmt, each, gate, up = _image_case(T, E, k, K, (4, 6, 8), perms, True, ld=8, skip=skip, round_=round_)
+    gate[::7] *= 1000                                    # gates that the table does not hold
+    gate[3::11] *= 1e-6
+    pair, first = plan.pair.cpu().numpy(), plan.first.cpu().numpy()
+    live = pair >= 0
+    noise = [torch.randint(0, 256, (n,), dtype=torch.uint8).cuda()
+             for n in (fmt.act_bytes(plan.rows), fmt.act_exp_bytes(plan.rows))]
+    got = mxq.quantize_act_swiglu_experts(gate, up, fmt, plan, perms=each, out=tuple(t.clone() for t in noise))
+    src = torch.from_numpy(np.where(live, pair, 0)).cuda()
+    rows, ups = gate[src].contiguous(), up[src].contiguous()
+    want = tuple(t.clone() for t in noise)
+    tb, sb = fmt.act_bytes(16), fmt.act_exp_bytes(16)
+    for e in range(E):
+        a, b = int(first[e]), int(first[e + 1])
+        f = fmt if each is None else mxq.Format(K, fmt.widths, each[e], round=round_)
+        if a < b:
+            mxq.quantize_act_swiglu(rows[a:b], ups[a:b], f, out=(want[0][a // 16 * tb:b // 16 * tb],
+                                                                 want[1][a // 16 * sb:b // 16 * sb]))
+    torch.cuda.synchronize()
+    for g, w, z, at in zip(got, want, noise, _byte_rows(list(fmt.widths), plan.rows)):
+        g, w, z = g.cpu().numpy(), w.cpu().numpy(), z.cpu().numpy()
+        assert np.array_equal(g[live[at]], w[live[at]])
+        assert np.array_equal(g[~live[at]], z[~live[at]])

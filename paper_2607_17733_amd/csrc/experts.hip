@@ -278,17 +278,22 @@ __device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float 
     const float best = value_of(wave_max(id >= 0 ? key_of(sc) : 0u));
     ref = softmax ? best : fminf(best, 0.f);
   }
+  // A score below e^-80, soon no normal float32, is held as s e^-88, since a large scale
+  // may make a normal weight of it.
+  constexpr float kHalf = 7.78113224e-20f;                 // e^-44
   float s = 0.f;
+  bool far = false;
   if (id >= 0) {
     const float d = sc - ref, back = d - sc;
     const float rest = (sc - (d - back)) - (ref + back);
-    // (below -104 it is 0; far below, d overflows and has no rest)
-    s = d < -110.f ? 0.f : expf(d) * (1.f + rest);
+    far = d < -80.f;
+    // (no scale brings back what lies below -177; far below, d overflows and has no rest)
+    s = d < -200.f ? 0.f : expf(far ? d + 88.f : d) * (1.f + rest);
     if (!softmax) s = sc > 0.f ? 1.f / (1.f + expf(-sc)) : s / (1.f + expf(sc));
   }
   float sum = 1.f;
   if (a.normalise) {
-    sum = wave_sum(s);
+    sum = wave_sum(far ? 0.f : s);                         // (the best is not far from itself)
   } else if (softmax) {
     sum = 0.f;
 #pragma unroll
@@ -296,7 +301,7 @@ __device__ inline void choose(const RouteArgs &a, int64_t t, int &chosen, float 
     sum = wave_sum(sum);
   }
   chosen = id;
-  weight = id >= 0 && sum > 0.f ? a.scale * (s / sum) : 0.f;
+  weight = id >= 0 && sum > 0.f ? (far ? a.scale * kHalf * (s / sum) * kHalf : a.scale * (s / sum)) : 0.f;
 }
 
 // A wave per token.

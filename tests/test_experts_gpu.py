@@ -739,3 +739,18 @@ def test_swiglu_images_of_many_groups(T, E, k, K, skip, round_, perms):
         g, w, z = g.cpu().numpy(), w.cpu().numpy(), z.cpu().numpy()
         assert np.array_equal(g[live[at]], w[live[at]])
         assert np.array_equal(g[~live[at]], z[~live[at]])
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("bias", [False, True])
+def test_route_scores_below_float32_and_a_large_scale(score, bias):
+    """A weight is good to 1e-6 wherever it is a normal float32, also where its score is not one."""
+    x = torch.tensor([[0.0, -40.0, -79.9, -80.1, -87.0, -90.0, -95.5, -103.0, -104.5, -110.25, -120.0, -150.0, -170.0, -400.0],
+                      [30.0, 29.0, -50.0, -51.0, -60.0, -70.0, -73.0, -75.0, -80.0, -90.0, -100.0, -110.0, -140.0, -3e38],
+                      [-100.0, -101.0, -180.0, -181.0, -186.5, -190.0, -200.0, -210.0, -250.0, -270.0, -280.0, -3e38, -3e38,
+                       -3e38]])
+    b = torch.zeros(14) if bias else None
+    for scale in (1.5, 1e10, 1e25, 3e38, -1e30):
+        for normalise in (False, True):
+            for k in (2, 14):
+                _check_route(x, k, score=score, bias=b, normalise=normalise, scale=scale)

@@ -754,3 +754,25 @@ def test_route_scores_below_float32_and_a_large_scale(score, bias):
         for normalise in (False, True):
             for k in (2, 14):
                 _check_route(x, k, score=score, bias=b, normalise=normalise, scale=scale)
+
+
+@pytest.mark.parametrize("T,E,K,N", [(50, 4, 512, 200), (7, 3, 1408, 130), (300, 16, 256, 400), (90, 40, 96, 1000)])
+@pytest.mark.parametrize("clamp", ["sym", "full"])
+def test_rows_of_shared_steps_do_not_depend_on_the_other_groups(T, E, K, N, clamp):
+    """The shares of K (groups of a few rows): the same pairs beside other ones, and beside other values, in
+    calls of the same size, bit for bit."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn((T, K), generator=g).to(torch.bfloat16).cuda()
+    w = torch.randn((E, N, K), generator=g).to(torch.bfloat16).cuda()
+    fmt = mxq.Format(K, _widths(K // 32, (4, 6, 8)), clamp=clamp)
+    wm, we = mxq.pack_experts(w, fmt)
+    ids = torch.randint(0, E, (T, 1), generator=g).int()
+    other = torch.randint(-1, E, (T, 1), generator=g).int()
+    other[::3] = ids[::3]
+    same = (ids == other)[:, 0].cuda()
+    z = torch.where(same[:, None], x, torch.randn((T, K), device="cuda").to(torch.bfloat16) * 50)
+    ys = []
+    for i, v in ((ids, x), (other, x), (other, z)):
+        plan = mxq.expert_plan(i.cuda(), E)
+        ys.append(mxq.gemm_experts(*mxq.quantize_act_experts(v, fmt, plan), wm, we, fmt, plan, N, dtype=torch.float32))
+    assert torch.equal(ys[0][same], ys[1][same]) and torch.equal(ys[0][same], ys[2][same])

@@ -145,3 +145,24 @@ def test_captured_and_replayed_in_place():
         torch.cuda.synchronize()
         assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
     assert torch.equal(q, q0) and torch.equal(k, k0)
+
+
+@pytest.mark.parametrize("D,rot,interleaved", [(128, 128, False), (128, 64, True), (66, 66, False)])
+def test_captured_with_the_results_in_place_of_other_inputs(D, rot, interleaved):
+    """One capture that overwrites q and k, replayed on other values (and positions), between eager calls."""
+    q, k, gains, pos, table = _inputs(20, 4, 2, D, rot)
+    mxq.rope_qk(q.clone(), k.clone(), pos, table, *gains, 1e-6, interleaved)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mxq.rope_qk(q, k, pos, table, *gains, 1e-6, interleaved, q_out=q, k_out=k)
+    for seed in range(1, 5):
+        q1, k1, _, pos1, _ = _inputs(20, 4, 2, D, rot, seed=seed)
+        want = mxq.rope_qk(q1, k1, pos1, table, *gains, 1e-6, interleaved)
+        q.copy_(q1)
+        k.copy_(k1)
+        pos.copy_(pos1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+        _check(q, q1, pos1, table, gains[0], 1e-6, interleaved)

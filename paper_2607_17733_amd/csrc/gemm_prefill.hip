@@ -700,7 +700,8 @@ void gemm_split_kernel(GemmArgs g, int mtiles, int ntiles, int nx) {
   int mt = 0, nt;
   const int32_t *pair = nullptr;
   if (BY) {
-    if (!take_expert<(TM == 1 ? 5 : 6)>(g, ntiles, nx, pair, nt)) return;
+    static_assert(!BY || TM == 1, "by experts 32 rows");
+    if (!take_expert<5>(g, ntiles, nx, pair, nt)) return;
   } else {
     const int pid = blockIdx.x;
     if (nx > 0) {

@@ -799,7 +799,7 @@ mxq_status mxq_combine_experts(const void *y, int y_f32, int64_t ldy, const int3
  * x[0..D-1] become
  *   r = 1 / sqrt(sum x^2 / D + eps),  v[d] = float32(float32(x[d] * r) * gain[d]),
  * r to 12 units of 2^-24 (40 beyond D = 512; in float64 where the squares add up to less
- * than 2^-80 or more than 2^120), and v is rotated as mxq_rope rotates x, its results
+ * than 2^-80 or more than 2^120, or eps is as large), and v is rotated as mxq_rope rotates x, its results
  * rounded once to bf16 (values at rot and above are bf16(v)).  A head of zeros gives
  * zeros, also with eps = 0.
  *   q_gain, k_gain  DEVICE bf16 [D], 16-byte aligned.

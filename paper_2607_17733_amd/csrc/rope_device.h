@@ -101,8 +101,8 @@ __device__ inline double sum_lanes(double v, int n) {
 }
 
 // 1 / sqrt(mean of the squares + eps) of a head, from the squares that each of its n
-// lanes has added up; f(T) adds the lane's own in T.  In float32 where the sum is far
-// from its limits (float64 for all heads made the arithmetic the bound: 4001 tokens of
+// lanes has added up; f(T) adds the lane's own in T.  In float32 where the sum and eps are
+// far from its limits (float64 for all heads made the arithmetic the bound: 4001 tokens of
 // 48 heads 24 -> 22 us), else in float64: a head of zeros has no direction, and stays
 // zero.
 struct HeadNorm {
@@ -113,7 +113,7 @@ template <typename F>
 __device__ inline HeadNorm head_norm(F f, int n, int D, float eps) {
   const float s = sum_lanes(f(0.f), n);
   HeadNorm h = {0.f, 0.0};
-  if (s > 0x1p-80f && s < 0x1p120f) {
+  if (s > 0x1p-80f && s < 0x1p120f && eps < 0x1p120f) {
     h.r = __builtin_amdgcn_rsqf(fmaf(s, 1.f / (float)D, eps));
   } else {                                                 // (all lanes of the head)
     const double m = sum_lanes(f(0.0), n) / (double)D + (double)eps;

@@ -166,3 +166,18 @@ def test_captured_with_the_results_in_place_of_other_inputs(D, rot, interleaved)
         torch.cuda.synchronize()
         assert torch.equal(q, want[0]) and torch.equal(k, want[1])
         _check(q, q1, pos1, table, gains[0], 1e-6, interleaved)
+
+
+@pytest.mark.parametrize("D", [128, 66])
+def test_the_largest_eps(D):
+    """The mean and eps add up beyond float32's largest."""
+    x = torch.full((3, 1, D), 2.0 ** 56, dtype=torch.bfloat16)
+    x[1] *= 2.0 ** -40
+    x[2] *= 2.0 ** 4
+    x[:, :, ::3] *= -1.5
+    pos = torch.tensor([0, 7, 99], dtype=torch.int32).cuda()
+    gain = torch.full((D,), 1.5, dtype=torch.bfloat16).cuda()
+    table = mxq.rope_table(mxq.rope_inv_freq(D)[0], 100)
+    for eps in (float(np.finfo(np.float32).max), 2.0 ** 127, 2.0 ** 100):
+        y, _ = mxq.rope_qk(x.cuda(), None, pos, table, gain, None, eps)
+        _check(y, x.cuda(), pos, table, gain, eps, False)

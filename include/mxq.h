@@ -768,6 +768,8 @@ mxq_status mxq_quantize_act_swiglu_experts(const mxq_fmt *fmt, const mxq_experts
  *                 from a rounding of their own.
  * A row's result does not depend on the other rows of its call; which kernel runs
  * goes by pairs, E and N, and the kernels differ in the order of their float32 sums.
+ * It is chosen as if every pair had an expert of these: where most have none, a call
+ * may take the kernel for larger groups than there are.
  * Errors: as mxq_gemm, and the plan's; MXQ_ERR_SHAPE also for more tiles (of 32 or
  * more rows, 128 columns) than a dispatch's 2^24 workgroups.
  */

@@ -26,9 +26,10 @@ __device__ inline int wave_scan(int v) {
 //
 // The tiles lie in order of the experts, `near` row tiles to a column tile; groups of
 // `near` go to the XCDs (workgroup pid to pid % 8) in turn, so that all have as many and
-// surplus workgroups come last.  (Longer runs, up to an eighth of all for each XCD,
-// were 10 % faster to 50 % slower; column tiles bound to an XCD up to a quarter slower
-// where their number is no multiple of 8.)  Every lane of the wave calls it.
+// surplus workgroups come last.  (An eighth of all tiles in one run for each XCD was 8 %
+// faster, 2048 tokens down 67 against 73 us, to 50 % slower, 333 tokens 42 against 28;
+// column tiles bound to XCDs, whose number is no multiple of 8, 55 against 48 for 64 tokens
+// among 128 experts.)  Every lane of the wave calls it.
 struct ExpertTile {
   int e, row0, rows, nt;
 };

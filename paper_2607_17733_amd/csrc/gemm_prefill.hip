@@ -1131,18 +1131,27 @@ hipError_t launch_gemm_prefill(const GemmArgs &a, hipStream_t stream) {
 // one per expert were empty.  Groups of 32 rows and more that come to 1.4 tiles of 128
 // rows per CU take the tiled kernel, others four shares of K over 32-row tiles.  us of
 // shares, tiled; tokens x experts x choices, K, N, 4-6-8 maps:
-//   4096 x 8 x 2, 4096, 28672 2522, 1517; 1000 x 32 x 4, 2048, 3584 92, 72; 1792, 2048 44,
-//   36; 2048, 1024 29, 26 (1.5 tiles per CU); 256 x 32 x 4, 2048, 3584 44, 42 (32 rows); 300
-//   x 4 x 2, 2048, 8192 28, 22 (1.5); 700 x 16 x 2, 8192, 4096 113, 116; 128 x 8 x 2, 4096,
-//   14336 70, 74 (32 rows)
-//   256 x 64 x 6, 2048, 2816 61, 63 (24 rows); 333 x 8 x 2, 4096, 4000 27, 30 (1.1); 400 x 8
-//   x 2, 4096, 4096 28, 34 (1.25); 64 x 128 x 8, 2048, 1536 48, about 80
-// Two shares of K were within 5 % of four everywhere that tiles are not taken (16 x 64 x 6,
-// 2048, 2816 33 against 35, 8 x 8 x 2, 4096, 28672 99 against 88); tiles of 256 rows, one
-// workgroup per CU, 1506 in the first case, but 448 against 414 for 2048 tokens.  The full
-// clamp's 12 KB weight stages leave a CU one tiled workgroup, of 256 rows then: 2048 x 8 x
-// 2, 4096, 14336 462 (of 128 rows about 590).  A kernel that streams weights for 16-row
-// tiles, as for single linears, took 51 for 64 x 128 x 8 and 94 for 8 x 8 x 2, 4096, 28672.
+//   4096 x 8 x 2, 4096, 28672 2540, 1490; 2048 x 8 x 2, 4096, 14336 498, 400; 2048 x 64 x 6,
+//   1408, 2048 89, 61; 1000 x 32 x 4, 2048, 3584 93, 69; 1792, 2048 44, 37; 2048, 1024 30,
+//   27 (1.5 tiles per CU); 300 x 4 x 2, 2048, 8192 28, 22 (1.5); 256 x 32 x 4, 2048, 3584 44,
+//   42 (32 rows)
+//   64 x 128 x 8, 2048, 1536 48, 57; 256 x 64 x 6, 2048, 2816 61, 63 (24 rows); 333 x 8 x 2,
+//   4096, 4000 28, 30 (1.1); 400 x 8 x 2, 4096, 4096 29, 34 (1.25)
+// It takes the slower side near its borders: of 32-row groups 128 x 8 x 2, 4096, 14336 70,
+// 74 (with more wide blocks 80, 89), and 700 x 16 x 2, 8192, 4096 113, 116.
+// Pairs that chose no expert here count as if they had: of 256 tokens x 8 choices, one in
+// eight of them among 16 experts, 2048, 3584, the rule takes tiles, 19, for shares' 16; of
+// 64 tokens both come to shares (16), of 1000 and more to tiles (23, shares 36; the live
+// pairs alone 23).
+// Two shares of K are 8 % faster (16 x 64 x 6, 2048, 2816 32.5 against 35; 400 x 8 x 2 27
+// against 29) to 14 % slower (700 x 16 x 2 129 against 113; 8 x 8 x 2, 4096, 28672 98 against
+// 88) where tiles are not taken or nearly so.  Tiles of 256 rows, one workgroup per CU, are
+// as fast in the first case (1480 to 1500, 128 rows 1477 to 1499) and slower in all others
+// (2048 tokens 431 against 400, 1000 87 against 69).  The full clamp's 12 KB weight stages
+// leave a CU one tiled workgroup, of 256 rows then: 2048 x 8 x 2, 4096, 14336 435, shares
+// 607; 1000 x 32 x 4, 2048, 3584 96, 110; but 128 x 8 x 2, 4096, 14336 171, shares 101.
+// A kernel that streams weights for 16-row tiles, as for single linears, took 51 for 64 x
+// 128 x 8 and 94 for 8 x 8 x 2, 4096, 28672.
 struct ExpertLaunch {
   bool tiled;
   int near;                // row tiles to a column tile that run together

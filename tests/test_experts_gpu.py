@@ -776,3 +776,75 @@ def test_rows_of_shared_steps_do_not_depend_on_the_other_groups(T, E, K, N, clam
         plan = mxq.expert_plan(i.cuda(), E)
         ys.append(mxq.gemm_experts(*mxq.quantize_act_experts(v, fmt, plan), wm, we, fmt, plan, N, dtype=torch.float32))
     assert torch.equal(ys[0][same], ys[1][same]) and torch.equal(ys[0][same], ys[2][same])
+
+
+# --------------------------------------------------------------------------
+# the largest counts: 2^26 pairs
+
+def _check_plan_on_device(ids, E, plan):
+    """first and pair against a stable sort on the device."""
+    f = ids.flatten().long()
+    f = torch.where((f >= 0) & (f < E), f, torch.full_like(f, E))
+    count = torch.bincount(f, minlength=E + 1)[:E]
+    first = torch.zeros(E + 1, dtype=torch.long, device=f.device)
+    first[1:] = torch.cumsum((count + 15) // 16 * 16, 0)
+    assert torch.equal(plan.first.long(), first)
+    order = torch.argsort(f, stable=True)[:int(count.sum())]
+    e = f[order]
+    del f
+    rank = torch.arange(order.numel(), device=e.device) - (torch.cumsum(count, 0) - count)[e]
+    want = torch.full((plan.rows,), -1, dtype=torch.int32, device=e.device)
+    want[first[e] + rank] = order.int()
+    assert torch.equal(plan.pair, want)
+
+
+@pytest.mark.parametrize("T,k,E", [(2 ** 26, 1, 1024), (2 ** 23, 8, 60), (2 ** 21, 32, 1000)])
+def test_plans_of_the_most_pairs(T, k, E):
+    say("plan", T, k, E)
+    g = torch.Generator(device="cuda").manual_seed(k)
+    ids = torch.randint(-1, E + 1, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    plan = mxq.expert_plan(ids, E)
+    _check_plan_on_device(ids, E, plan)
+
+
+@pytest.mark.parametrize("T,k,E", [(2 ** 24, 4, 6), (2 ** 21, 32, 70)])
+def test_routing_of_the_most_pairs(T, k, E):
+    say("route", T, k, E)
+    g = torch.Generator(device="cuda").manual_seed(E)
+    x = torch.randn((T, E), generator=g, device="cuda").to(torch.bfloat16)
+    ids, w, plan = mxq.route(x, k, score="sigmoid", normalise=False)
+    order = torch.sort(x.float(), dim=-1, descending=True, stable=True)[1][:, :k]
+    assert torch.equal(ids, order.int())
+    s = torch.sigmoid(x.gather(1, order).double())
+    assert bool(((w.double() - s).abs() <= 1e-6 * s).all())
+    _check_plan_on_device(ids, E, plan)
+
+
+def test_products_and_sums_of_the_most_pairs():
+    """2^26 pairs of 2^25 tokens: an image of 6.4 GB, a row of y for each."""
+    T, k, E, K, N = 2 ** 25, 2, 3, 32, 8
+    say("product", T, k, E, K, N)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((T, K), generator=g, device="cuda").to(torch.bfloat16)
+    w = torch.randn((E, N, K), generator=g, device="cuda").to(torch.bfloat16)
+    ids = torch.randint(-1, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    fmt = mxq.Format(K, [8])
+    plan = mxq.expert_plan(ids, E)
+    wm, we = mxq.pack_experts(w, fmt)
+    y = torch.full((T * k, N), 7.0, device="cuda")
+    mxq.gemm_experts(*mxq.quantize_act_experts(x, fmt, plan), wm, we, fmt, plan, N, out=y)
+    chosen = ids.flatten() >= 0
+    assert bool((y[~chosen] == 7.0).all()) and not bool((y[chosen] == 7.0).all(dim=1).any())
+    at = torch.cat([torch.arange(64), torch.randint(0, T * k, (400,), generator=torch.Generator().manual_seed(2)),
+                    torch.arange(T * k - 64, T * k)]).cuda()
+    f = ids.flatten()[at].cpu().numpy()
+    want, big = oe.product(bits_of(x[at // k]), bits_of(w), f, None, [8])
+    here = f >= 0
+    got = y[at].double().cpu().numpy()
+    assert np.all(np.abs(got[here] - want[here]) <= (K / 64 + 16) * 2.0 ** -23 * big[here])
+    weights = torch.rand((T, k), generator=g, device="cuda")
+    o = mxq.combine_experts(y, ids, weights, plan, residual=torch.ones((T, N), dtype=torch.bfloat16, device="cuda"),
+                            dtype=torch.float32)
+    terms = torch.where(chosen[:, None], weights.flatten()[:, None] * y, torch.zeros((), device="cuda")).view(T, k, N)
+    # (a rounding for each of three sums and the products')
+    assert bool(((o - (1 + terms.sum(1))).abs() <= 5 * 2.0 ** -24 * (1 + terms.abs().sum(1))).all())

@@ -100,8 +100,9 @@ __global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeRowsArgs a, int6
 // head (a power of two, so that their sum is an exchange within the wave), the
 // queries' heads before the keys'.  The values stay in registers between the two;
 // those of the partners of a rotation in halves are read again, from the cache.  Bytes
-// bound it: 4001 tokens of 48 heads, half of each rotated, 99 MB 21.7 us (4.6 TB/s; a
-// large copy moves 4.7 to 5.2); one token 3 us, the launch.
+// and vector instructions bound it alike: 4001 tokens of 48 heads, half of each rotated, 99
+// MB 21.5 us (4.6 TB/s; a large copy moves 4.7 to 5.2), and 280 instructions to a wave, which
+// the SIMDs issue in as long; one token 3 us, the launch.
 __global__ __launch_bounds__(kThreads) void rope_qk_kernel(RopeQkArgs a, int lg_lanes,
                                                            int64_t total) {
   const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;

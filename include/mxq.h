@@ -744,7 +744,8 @@ mxq_status mxq_expert_plan(const int32_t *ids, const mxq_experts *plan, void *st
  *   per_row  divides pairs.
  *   a_mant, a_exp  of mxq_act_bytes(fmt, R) and mxq_act_exp_bytes(fmt, R), R =
  *            mxq_expert_rows(pairs, E).
- * Errors: as those calls, and the plan's.
+ * Errors: as those calls, and the plan's; MXQ_ERR_SHAPE also for images of more
+ * threads than a dispatch's 2^32 (K = 4096 from 2^26 pairs on, 20480 from 2^23).
  */
 mxq_status mxq_quantize_act_experts(const mxq_fmt *fmt, const mxq_experts *plan,
                                     const int32_t *perms, const uint16_t *a, int64_t per_row,

@@ -164,7 +164,9 @@ mxq_status quantize_common(const mxq_fmt *fmt, const uint16_t *src, int64_t rows
   // the activation quantizer stages its rows in LDS: one row must fit
   if (mxq::quantize_act_lds(fmt->K, gain != nullptr) + (by ? mxq::kGroupLds : 0) > mxq::kMaxLds)
     return MXQ_ERR_UNSUPPORTED;
-  return launched(mxq::launch_quantize_act(a, (hipStream_t)stream));
+  const hipError_t e = mxq::launch_quantize_act(a, (hipStream_t)stream);
+  // (more threads than a dispatch's 2^32: long rows of tens of millions of pairs)
+  return e == hipErrorInvalidConfiguration ? MXQ_ERR_SHAPE : launched(e);
 }
 
 mxq_status gemm_args(const mxq_fmt *fmt, int64_t M, int64_t N, const uint8_t *a_mant,

@@ -983,6 +983,7 @@ hipError_t launch_quantize_act(const QuantArgs &args, hipStream_t stream) {
   // short, from twice (gates of size 1: 4000 rows of 1792 17.2, without it 17.5 us, 12288 of
   // 1408 33.7, 35.6; of size 8, near more rounding borders, 17.3, 23.7 and 33.5, 48.1)
   const int64_t grid = a.swiglu ? std::min<int64_t>(groups, (int64_t)rg.per_cu * cus) : groups;
+  if (grid * rg.threads > UINT32_MAX) return hipErrorInvalidConfiguration;
   int64_t lds = ((row_lds(a.K, a.rmsnorm != 0) << rg.lg) + 15) & ~15;
   a.silu_table = a.swiglu && a.vec16 && ((groups / grid * a.K) << rg.lg) >= (a.x.E ? 2 : 6) * kSiluN &&
                  lds + 2 * kSiluN + (a.x.E ? kGroupLds : 0) <= kMaxLds;

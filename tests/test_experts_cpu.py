@@ -267,3 +267,11 @@ def test_source_rows_are_those_of_the_tokens_or_of_the_pairs():
     for k in (0, -1, 5):
         with pytest.raises(mxq.MxqError):
             mxq.ExpertPlan(12, 4, k=k)
+
+
+def test_images_of_more_threads_than_a_dispatch_holds(L):
+    """Long rows of as many pairs as a plan allows: a group of rows to a workgroup, 2^32 threads and more."""
+    for blocks, pairs in ((640, 2 ** 23), (640, 2 ** 26), (128, 2 ** 26)):
+        f = mxq.Format(32 * blocks, [4] * blocks)
+        p = plan(pairs=pairs)
+        assert L.mxq_quantize_act_experts(f.ref, ref(p), None, FAKE, 2, 32 * blocks, FAKE, FAKE, None) == SHAPE
